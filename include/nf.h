@@ -604,6 +604,115 @@ nf_status nf_endpoint_guard(const nf_endpoint_model* model_host, int64_t n, int6
                             double* t_fp32_host, double* t_lowbit_host, int32_t* guard_ok_host);
 
 /*
+ * What a training step does on either side of the reduction (no paper
+ * counterpart): the embedding table's rows and their gradient, which fills
+ * the largest FP32-routed segment of a worker's row (§5.3), and the step of
+ * the low-bit-eligible matrices from their reduced gradient.
+ *
+ * Element types.  Sums, norms and statistics are held in 32 bits or more
+ * whatever the type; a 16-bit result is rounded once.
+ */
+enum { NF_TYPE_F32 = 0, NF_TYPE_BF16 = 1, NF_TYPE_F16 = 2 };
+
+/*
+ * Embedding lookup with scaling, for t in [0, T):
+ *   out[t][j] = scale * table[ids[t]][j], j in [0, d);  zeros where ids[t] is
+ *   outside [0, V) (a padded position carries -1).
+ * The product is taken in FP32.  table is V rows of d elements, table_ld
+ * apart; out is T rows, out_ld apart; both of any NF_TYPE_*, aligned to
+ * their elements.  ids: int32 (ids_bytes = 4) or int64 (8).  T = 0 or d = 0
+ * launches nothing.  NF_ERR_INVALID_ARG: V, T, d < 0, d > 2^24, T > 2^31 - 1,
+ * table_ld or out_ld < d, unknown types.
+ */
+nf_status nf_embedding_lookup(const void* table, int32_t table_type, int64_t table_ld, int64_t V, int64_t d,
+                              const void* ids, int32_t ids_bytes, int64_t T, float scale, void* out,
+                              int32_t out_type, int64_t out_ld, void* stream);
+
+/*
+ * Gradient of that lookup for W workers, each with T tokens of its own, into
+ * the V x d segment of its gradient row that holds the table:
+ *   grads[w*worker_stride + v*d + j] = scale * sum of dy[w][t][j] over the t
+ *   with ids[w][t] = v
+ * for every v in [0, V): rows without a token become zeros.  With
+ * accumulate != 0 the sums are added to what the segment holds and rows
+ * without a token are left alone.  Tokens outside [0, V), and those equal to
+ * padding_id (-1 for none), add to no row.  Each row's terms are added in
+ * FP32 in an order fixed by the sizes (tokens in ascending order in groups),
+ * without floating-point atomics: two calls give the same bits.
+ * `grads` is the segment in worker 0's row (a row's base plus the table's
+ * offset in it), 4-byte aligned.  dy[w] is T rows dy_ld apart, workers
+ * dy_stride elements apart; ids rows ids_stride apart.
+ * NF_ERR_INVALID_ARG: W outside [1, 255]; V < 0 or > 2^31 - 1; T < 0 or
+ * > 2^24; d < 0 or > 2^24; dy_ld < d; dy_stride < (T - 1) * dy_ld + d or
+ * ids_stride < T with W > 1; worker_stride < V * d with W > 1.
+ */
+size_t nf_embedding_workspace_bytes(int32_t W, int64_t T, int64_t V, int64_t d);
+nf_status nf_embedding_grad(const void* dy, int32_t dy_type, int64_t dy_ld, int64_t dy_stride, const void* ids,
+                            int32_t ids_bytes, int64_t ids_stride, int32_t W, int64_t T, int64_t V, int64_t d,
+                            float scale, int64_t padding_id, int32_t accumulate, float* grads,
+                            int64_t worker_stride, void* ws, size_t ws_bytes, void* stream);
+
+/* How nf_orthogonalize forms its products: of operands rounded once to FP16
+ * (11 bits), or each held as two FP16 numbers (22 bits, three products; a
+ * shorter side of at most 64 always takes these).  The result is within about 2e-3 of the exact one relative to its norm, or within
+ * about 1e-5 (FP32 products are no closer). */
+enum { NF_PRODUCTS_SINGLE = 0, NF_PRODUCTS_SPLIT = 1 };
+#define NF_ORTHOGONAL_MAX_STEPS 12
+typedef struct {
+  int32_t products;  /* NF_PRODUCTS_*                                          */
+  int32_t steps;     /* S in [1, NF_ORTHOGONAL_MAX_STEPS]                      */
+  float eps;         /* added to the norm, finite and >= 0                     */
+  float coef[NF_ORTHOGONAL_MAX_STEPS][3];  /* a, b, c of every step, finite    */
+} nf_orthogonal_params;
+
+/*
+ * Orthogonalisation by Newton-Schulz products of a batch of matrices (no
+ * paper counterpart; the step rule of the Muon optimiser).  For each G:
+ *   X = G / (||G||_F + eps)   (zeros where G is all zeros)
+ *   S times:  A = X X^T;  X = a X + (b A + c A A) X
+ * with X X^T on the shorter side (X^T X and X (...) where rows > cols: the
+ * same matrix).  The norm is an FP64 sum.  A matrix with a NaN or an
+ * infinity gives NaN everywhere; other matrices of the batch are unaffected.
+ * Coefficients must keep the singular values of X below 32, as any that
+ * converge do: products beyond the range of FP16 give NaN.
+ * src and dst: `batch` matrices of rows x cols, elements of a row adjacent,
+ * rows src_ld (dst_ld) and matrices src_stride (dst_stride) elements apart,
+ * of any NF_TYPE_*, aligned to their elements; dst may be src.
+ * NF_ERR_INVALID_ARG: sizes < 0, ld < cols, a stride < (rows-1)*ld + cols with
+ * batch > 1, bad parameters.  NF_ERR_UNSUPPORTED: a side > 2^17 or more than
+ * 2^30 tiles of work.  rows, cols or batch = 0 launches nothing.
+ */
+size_t nf_orthogonal_workspace_bytes(int64_t rows, int64_t cols, int64_t batch,
+                                     const nf_orthogonal_params* params_host);
+nf_status nf_orthogonalize(const void* src, int32_t src_type, int64_t src_ld, int64_t src_stride, void* dst,
+                           int32_t dst_type, int64_t dst_ld, int64_t dst_stride, int64_t rows, int64_t cols,
+                           int64_t batch, const nf_orthogonal_params* params_host, void* ws, size_t ws_bytes,
+                           void* stream);
+
+/* The step around it. */
+typedef struct {
+  float lr;            /* finite                                               */
+  float momentum;      /* mu, finite                                           */
+  float weight_decay;  /* finite                                               */
+  float scale;         /* of the orthogonalised matrix, finite                 */
+  int32_t nesterov;    /* 0 or 1                                               */
+} nf_matrix_step;
+
+/*
+ * One step of a batch of weight matrices from their (reduced) gradients, in
+ * place:
+ *   M = mu M + g;   U = g + mu M if nesterov, else M
+ *   w = (1 - lr weight_decay) w - lr scale orthogonalised(U)
+ * M is FP32, grad and weight any NF_TYPE_*; w is formed in FP32 and rounded
+ * once.  Layouts, requirements and errors as for nf_orthogonalize.
+ */
+nf_status nf_orthogonal_update(const void* grad, int32_t grad_type, int64_t grad_ld, int64_t grad_stride,
+                               float* momentum, int64_t momentum_ld, int64_t momentum_stride, void* weight,
+                               int32_t weight_type, int64_t weight_ld, int64_t weight_stride, int64_t rows,
+                               int64_t cols, int64_t batch, const nf_matrix_step* step_host,
+                               const nf_orthogonal_params* params_host, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Profiling hook (no paper counterpart).  When set on the calling thread,
  * nf_route_bucket and nf_route_buckets record these hipEvent_t handles (each
  * passed as void*) on their stream: before pass 1, after pass 1, after the

@@ -39,7 +39,12 @@ EXPORTS = ["nf_abi_version", "nf_last_error", "nf_mask_from_segments", "nf_works
            "nf_ternary_reduce", "nf_partial_counts", "nf_partial_count_reduce", "nf_stock_signcount",
            "nf_supervisor_init", "nf_supervisor_policy", "nf_supervisor_update", "nf_endpoint_guard",
            "nf_sliced_layout_sizes", "nf_sliced_layout", "nf_compact_signs", "nf_slice_workspace_bytes",
-           "nf_slice_scales", "nf_compact_signcount_reduce"]
+           "nf_slice_scales", "nf_compact_signcount_reduce",
+           "nf_embedding_lookup", "nf_embedding_workspace_bytes", "nf_embedding_grad",
+           "nf_orthogonal_workspace_bytes", "nf_orthogonalize", "nf_orthogonal_update"]
+NF_TYPE_F32, NF_TYPE_BF16, NF_TYPE_F16 = 0, 1, 2
+NF_PRODUCTS_SINGLE, NF_PRODUCTS_SPLIT = 0, 1
+NF_ORTHOGONAL_MAX_STEPS = 12
 NF_SUP_WARMUP, NF_SUP_LOWBIT, NF_SUP_COOLDOWN, NF_SUP_GUARD = 0, 1, 2, 3
 
 
@@ -86,6 +91,16 @@ class nf_endpoint_model(ctypes.Structure):
                 ("bits_per_element", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("net_bytes_per_s", ctypes.c_double), ("endpoint_bytes_per_s", ctypes.c_double),
                 ("latency_fp32_s", ctypes.c_double), ("latency_lowbit_s", ctypes.c_double)]
+
+
+class nf_orthogonal_params(ctypes.Structure):
+    _fields_ = [("products", ctypes.c_int32), ("steps", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("coef", ctypes.c_float * 3 * NF_ORTHOGONAL_MAX_STEPS)]
+
+
+class nf_matrix_step(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_float), ("momentum", ctypes.c_float), ("weight_decay", ctypes.c_float),
+                ("scale", ctypes.c_float), ("nesterov", ctypes.c_int32)]
 
 
 STATS_DTYPE = np.dtype([("nonfinite", "<u8"), ("sum_abs_elig", "<f8"), ("sum_sq", "<f8")])
@@ -165,6 +180,16 @@ def load(path=None):
         "nf_slice_scales": (ctypes.c_int, [_P, _I64, _I32, _P, _P, _P, _I64, _I64, _P, _P, _P, _SZ, _P]),
         "nf_compact_signcount_reduce": (ctypes.c_int, [_P, _I64, _I32, _I64, _P, _P, _P, _P, _I64, _I64, _P,
                                                         _I32, _P, _P, _P]),
+        "nf_embedding_lookup": (ctypes.c_int, [_P, _I32, _I64, _I64, _I64, _P, _I32, _I64, ctypes.c_float, _P,
+                                               _I32, _I64, _P]),
+        "nf_embedding_workspace_bytes": (_SZ, [_I32, _I64, _I64, _I64]),
+        "nf_embedding_grad": (ctypes.c_int, [_P, _I32, _I64, _I64, _P, _I32, _I64, _I32, _I64, _I64, _I64,
+                                             ctypes.c_float, _I64, _I32, _P, _I64, _P, _SZ, _P]),
+        "nf_orthogonal_workspace_bytes": (_SZ, [_I64, _I64, _I64, _P]),
+        "nf_orthogonalize": (ctypes.c_int, [_P, _I32, _I64, _I64, _P, _I32, _I64, _I64, _I64, _I64, _I64, _P, _P,
+                                            _SZ, _P]),
+        "nf_orthogonal_update": (ctypes.c_int, [_P, _I32, _I64, _I64, _P, _I64, _I64, _P, _I32, _I64, _I64, _I64,
+                                                _I64, _I64, _P, _P, _P, _SZ, _P]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -585,6 +610,125 @@ def nf_pass1_chunk_elems(W, n_total, bucket_n):
     cpb = ctypes.c_int64(0)
     e = int(load().nf_pass1_chunk_elems(W, n_total, bucket_n, ctypes.byref(cpb)))
     return e, int(cpb.value)
+
+
+# ---------------------------------------------- either side of the reduction
+
+def _type(t, name):
+    codes = {torch.float32: NF_TYPE_F32, torch.bfloat16: NF_TYPE_BF16, torch.float16: NF_TYPE_F16}
+    if t.dtype not in codes:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return codes[t.dtype]
+
+
+def _ids(t, name="ids"):
+    if t.dtype not in (torch.int32, torch.int64):
+        raise ValueError(f"{name} must be int32 or int64, got {t.dtype}")
+    if t.numel() > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must have unit stride in the last dimension")
+    return _dev_ptr(t, None, name), t.element_size()
+
+
+def _rows_of(t, name):
+    """(pointer, row stride) of a [rows, cols] tensor whose rows are contiguous."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be two-dimensional with unit stride in the last dimension")
+    return _dev_ptr(t, None, name), t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _matrices(t, shape, name):
+    """(pointer, row stride, matrix stride) of a [rows, cols] or [batch, rows, cols] tensor of that shape."""
+    if t.dim() not in (2, 3) or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name} must be [rows, cols] or [batch, rows, cols] with unit stride in the last dimension")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
+    rows, cols = t.shape[-2:]
+    ld = t.stride(-2) if rows > 1 else max(cols, 1)
+    stride = t.stride(0) if t.dim() == 3 and t.shape[0] > 1 else rows * ld
+    return _dev_ptr(t, None, name), ld, stride
+
+
+def nf_embedding_lookup(table, ids, out, scale=1.0, stream=None):
+    """out[t] = scale * table[ids[t]]; zeros for ids outside [0, V).  table:
+    [V, d], ids: [T], out: [T, d]."""
+    tp, tld = _rows_of(table, "table")
+    op, old = _rows_of(out, "out")
+    ip, ibytes = _ids(ids)
+    if ids.dim() != 1 or tuple(out.shape) != (ids.shape[0], table.shape[1]):
+        raise ValueError(f"out must be [{ids.numel()}, {table.shape[1]}] and ids one-dimensional")
+    _check(load().nf_embedding_lookup(tp, _type(table, "table"), tld, table.shape[0], table.shape[1], ip, ibytes,
+                                      ids.shape[0], float(scale), op, _type(out, "out"), old, _stream(stream)))
+
+
+def nf_embedding_workspace_bytes(W, T, V, d):
+    return int(load().nf_embedding_workspace_bytes(W, T, V, d))
+
+
+def nf_embedding_grad(dy, ids, grads, offset, V, ws, scale=1.0, padding_id=-1, accumulate=False, stream=None):
+    """The lookup's gradient for W workers into elements [offset, offset + V*d)
+    of their rows of grads.  dy: [W, T, d], ids: [W, T], grads: [W, stride]
+    float32."""
+    g, stride, W = _rows(grads)
+    if dy.dim() != 3 or (dy.shape[2] > 1 and dy.stride(2) != 1):
+        raise ValueError("dy must be [W, T, d] with unit stride in the last dimension")
+    T, d = dy.shape[1:]
+    ip, ibytes = _ids(ids)
+    if dy.shape[0] != W or tuple(ids.shape) != (W, T):
+        raise ValueError(f"dy must be [{W}, T, d] and ids [{W}, T], got {tuple(dy.shape)} and {tuple(ids.shape)}")
+    if offset < 0 or V < 0 or offset + V * d > grads.shape[1]:
+        raise ValueError(f"the table's segment [{offset}, {offset + V * d}) exceeds the rows of {grads.shape[1]}")
+    ld = dy.stride(1) if T > 1 else max(d, 1)
+    _check(load().nf_embedding_grad(_dev_ptr(dy, None, "dy"), _type(dy, "dy"), ld,
+                                    dy.stride(0) if W > 1 else T * ld, ip, ibytes, ids.stride(0) if W > 1 else T,
+                                    W, T, V, d, float(scale), int(padding_id), int(bool(accumulate)),
+                                    g + 4 * offset, stride, _dev_ptr(ws, torch.uint8, "ws"), ws.numel(),
+                                    _stream(stream)))
+
+
+def orthogonal(products=NF_PRODUCTS_SINGLE, steps=5, coef=(3.4445, -4.7750, 2.0315), eps=1e-7):
+    """Parameters of nf_orthogonalize.  coef: (a, b, c) for every step, or a
+    sequence of `steps` such triples."""
+    p = nf_orthogonal_params(products, steps, eps)
+    rows = [coef] * steps if np.ndim(coef) == 1 else list(coef)
+    if len(rows) != steps:
+        raise ValueError(f"{len(rows)} triples of coefficients for {steps} steps")
+    for k, row in enumerate(rows[:NF_ORTHOGONAL_MAX_STEPS]):
+        p.coef[k][:] = row
+    return p
+
+
+def matrix_step(lr, momentum=0.95, nesterov=True, weight_decay=0.0, scale=1.0):
+    return nf_matrix_step(lr, momentum, weight_decay, scale, int(bool(nesterov)))
+
+
+def nf_orthogonal_workspace_bytes(rows, cols, batch, params):
+    return int(load().nf_orthogonal_workspace_bytes(rows, cols, batch, ctypes.byref(params)))
+
+
+def nf_orthogonalize(src, dst, params, ws, stream=None):
+    """dst = src orthogonalised, every matrix of a [batch, rows, cols] tensor
+    (or one [rows, cols])."""
+    sp, sld, sst = _matrices(src, None, "src")
+    dp, dld, dst_stride = _matrices(dst, src.shape, "dst")
+    _check(load().nf_orthogonalize(sp, _type(src, "src"), sld, sst, dp, _type(dst, "dst"), dld, dst_stride,
+                                   src.shape[-2], src.shape[-1], src.shape[0] if src.dim() == 3 else 1,
+                                   ctypes.byref(params), _dev_ptr(ws, torch.uint8, "ws"), ws.numel(),
+                                   _stream(stream)))
+
+
+def nf_orthogonal_update(grad, momentum, weight, step, params, ws, stream=None):
+    """One step of the weight matrices in place: momentum (float32) takes the
+    gradient, weight the orthogonalised update."""
+    gp, gld, gst = _matrices(grad, None, "grad")
+    if momentum.dtype != torch.float32:
+        raise ValueError(f"momentum must be float32, got {momentum.dtype}")
+    mp, mld, mst = _matrices(momentum, grad.shape, "momentum")
+    wp, wld, wst = _matrices(weight, grad.shape, "weight")
+    _check(load().nf_orthogonal_update(gp, _type(grad, "grad"), gld, gst, mp, mld, mst, wp, _type(weight, "weight"),
+                                       wld, wst, grad.shape[-2], grad.shape[-1],
+                                       grad.shape[0] if grad.dim() == 3 else 1, ctypes.byref(step),
+                                       ctypes.byref(params), _dev_ptr(ws, torch.uint8, "ws"), ws.numel(),
+                                       _stream(stream)))
 
 
 # ------------------------------------------------------- result decoding
