@@ -15,6 +15,10 @@
 // flops: A and A A are symmetric, so tiles on and below the diagonal are
 // computed and mirrored.
 //
+// Operands lie in panels of 32 k: element (row, k) of a matrix of R rows is
+// at ((k / 32) R + row) 32 + k % 32.  A stage's BT rows are then one
+// contiguous piece of memory, whole cache lines, whatever the tile.
+//
 // What is held in which precision.  Operands of products are FP16 (11 bits;
 // in split mode a pair of FP16, 22 bits, and three products), sums FP32.  X
 // times 2^10 lies well inside FP16's range, since no entry exceeds the
@@ -32,6 +36,8 @@
 //     except in the last step, after which nothing is amplified any more.
 #include <math.h>
 
+#include <type_traits>
+
 #include "nf_internal.h"
 #include "nf_types.h"
 
@@ -41,10 +47,12 @@ namespace {
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float2v __attribute__((ext_vector_type(2)));
 
 constexpr float kScale = 1024.0f;         // X, A and B in FP16 are held times this
 constexpr float kInvScale = 1.0f / kScale;
-constexpr int kBK = 64;                   // k of one LDS tile
+constexpr int kBK = 32;                   // k of one stage: a panel
+constexpr int kStages = 4;                // LDS stages of k_prod
 constexpr int kNormThreads = 256;
 constexpr int kNormElems = 16384;         // elements of a norm partial, at least
 constexpr int kMaxParts = 256;
@@ -72,16 +80,18 @@ struct PrepArgs {
   int32_t lg_tx;       // k_norm: log2 of the threads across a row
   float eps;
   _Float16 *xh, *xl, *th, *tl;  // tl: split only
+  int32_t* arrived;    // to be zeroed
+  int64_t tiles;
 };
 
 struct ProdArgs {
-  const _Float16 *ph, *pl, *qh, *ql;  // P: [tm tiles x K], Q: [tn tiles x K], K adjacent
-  int64_t ldk;                        // of both, = K
+  const _Float16 *ph, *pl, *qh, *ql;  // P: tm tiles of rows, Q: tn tiles
+  int64_t ldk;                        // k of both
   int64_t pstride, qstride;           // a matrix of the batch
   int32_t tm, tn;                     // tiles
   float a, b, c;
-  _Float16 *oh, *ol;                  // GRAM: A, POLY: B (ld = rows); STEP: X^T
-  int64_t old, ostride;
+  _Float16 *oh, *ol;                  // GRAM: A, POLY: B; STEP: X^T
+  int64_t ostride;
   const _Float16 *ah, *al;            // POLY: A
   float* dA;                          // diagonals, [batch][Mp]
   float* dB;
@@ -92,6 +102,10 @@ struct ProdArgs {
   int32_t tall;
   int32_t update;                     // 1: dst holds weights
   float keep, rate;                   // w = keep w - rate o
+  int32_t vec;                        // dst takes 16-byte accesses
+  int32_t shares;                     // GRAM: blocks that share a tile's k
+  uint64_t* part;                     // their sums, [tile][share][BT x BT], two FP32 a word
+  int32_t* arrived;                   // [tile], zero between launches
 };
 
 __device__ __forceinline__ float load_elem(const View& v, int64_t off) {
@@ -99,13 +113,10 @@ __device__ __forceinline__ float load_elem(const View& v, int64_t off) {
   if (v.type == NF_TYPE_BF16) return to_f32(((const Bf16*)v.p)[off]);
   return (float)((const _Float16*)v.p)[off];
 }
-__device__ __forceinline__ void store_elem(const View& v, int64_t off, float x) {
-  if (v.type == NF_TYPE_F32)
-    ((float*)v.p)[off] = x;
-  else if (v.type == NF_TYPE_BF16)
-    ((Bf16*)v.p)[off] = from_f32<Bf16>(x);
-  else
-    ((_Float16*)v.p)[off] = (_Float16)x;
+
+// Where (row, k) of a matrix of R rows lies.
+__device__ __forceinline__ int64_t panel_at(int64_t row, int64_t k, int64_t R) {
+  return ((k / kBK) * R + row) * kBK + k % kBK;
 }
 
 // U at (r, c), the momentum already stepped.
@@ -135,6 +146,9 @@ __global__ __launch_bounds__(kNormThreads) void k_norm(PrepArgs a) {
   __shared__ double s[kNormThreads / 64];
   const int tx = 1 << a.lg_tx, ty = kNormThreads >> a.lg_tx;
   const int64_t b = blockIdx.y;
+  if (b == 0)
+    for (int64_t i = (int64_t)blockIdx.x * kNormThreads + threadIdx.x; i < a.tiles; i += (int64_t)gridDim.x * kNormThreads)
+      a.arrived[i] = 0;
   const int x = threadIdx.x & (tx - 1), y = threadIdx.x >> a.lg_tx;
   double sum = 0.0;
   for (int64_t r = (int64_t)blockIdx.x * ty + y; r < a.rows; r += (int64_t)gridDim.x * ty) {
@@ -171,8 +185,8 @@ __global__ __launch_bounds__(kNormThreads) void k_scale(PrepArgs a) {
   }
   __syncthreads();
   const int64_t size = a.Mp * a.Np;
-  // as it lies: X, or X^T where the caller's matrix is tall
-  const int64_t ld0 = a.tall ? a.Mp : a.Np, ld1 = a.tall ? a.Np : a.Mp;
+  // rows x cols as it lies: X, or X^T where the caller's matrix is tall
+  const int64_t R0 = a.tall ? a.Np : a.Mp, R1 = a.tall ? a.Mp : a.Np;
   _Float16* h0 = (a.tall ? a.th : a.xh) + b * size;
   _Float16* h1 = (a.tall ? a.xh : a.th) + b * size;
   _Float16* l0 = a.tall ? a.tl : a.xl;
@@ -180,10 +194,11 @@ __global__ __launch_bounds__(kNormThreads) void k_scale(PrepArgs a) {
   for (int i = y; i < 64; i += 4) {
     const float v = tile[i][x], w = tile[x][i];
     const _Float16 vh = (_Float16)v, wh = (_Float16)w;
-    h0[(r0 + i) * ld0 + c0 + x] = vh;
-    h1[(c0 + i) * ld1 + r0 + x] = wh;
-    if (l0) l0[b * size + (r0 + i) * ld0 + c0 + x] = (_Float16)(v - (float)vh);
-    if (l1) l1[b * size + (c0 + i) * ld1 + r0 + x] = (_Float16)(w - (float)wh);
+    const int64_t at0 = panel_at(r0 + i, c0 + x, R0), at1 = panel_at(c0 + i, r0 + x, R1);
+    h0[at0] = vh;
+    h1[at1] = wh;
+    if (l0) l0[b * size + at0] = (_Float16)(v - (float)vh);
+    if (l1) l1[b * size + at1] = (_Float16)(w - (float)wh);
   }
 }
 
@@ -192,165 +207,423 @@ __global__ __launch_bounds__(kNormThreads) void k_scale(PrepArgs a) {
 typedef const __attribute__((address_space(1))) void* gptr;
 typedef __attribute__((address_space(3))) void* lptr;
 
-// Rows row0 .. row0 + BT - 1, k in [k0, k0 + 64), of src into an LDS tile of
-// BT rows of 64: each wavefront moves eight rows (1 KiB) at a time straight
-// into LDS, lane l the 16 bytes that belong in the l-th slot.  Slot j of row
-// r holds the row's 16-byte piece j ^ (r / 2 % 8): the sixteen rows that a
-// fragment read touches then lie in sixteen different 16-byte columns of the
-// 64 banks.
+// BT rows of a panel (contiguous in src) into an LDS tile: each wavefront
+// moves sixteen rows (1 KiB) at a time straight into LDS, lane l the 16 bytes
+// that belong in the l-th slot.
+//
+// A fragment is sixteen rows of thirty-two: rows 8 q + e and, in the odd
+// fragment of a pair, 8 q + 4 + e (q, e in [0, 4)).  Of the products of two
+// pairs a lane then holds eight adjacent rows of eight columns, 16 bytes of
+// FP16 that belong together in memory, and four lanes a whole 64-byte row of
+// a panel.
+//
+// Slot j of row r holds the row's 16-byte piece j ^ swizzle(r).  A 16-byte
+// read of 64 lanes is served sixteen lanes at a time: lanes 0-3, 12-15, 20-23
+// and 24-27 (q = 0 and 3 of one piece, 1 and 2 of the next) and so on; with
+// this swizzle those, like lanes 0-15, touch sixteen different 16-byte
+// columns of the 64 banks.  (With r / 8 % 4 for a swizzle, two of them
+// collide: a conflict counted in every read.)
+__device__ __forceinline__ int swizzle(int row) {
+  const int q = row >> 3;
+  return ((q >> 1) & 1) | (((q ^ (q >> 1)) & 1) << 1);
+}
+
+// A lane's place in the 1 KiB that its wavefront moves (row: the first of them), and in the rows of a fragment.
+__device__ __forceinline__ int load_place(int row, int lane) {
+  return lane / 4 * kBK + ((lane % 4) ^ swizzle(row + lane / 4)) * 8;
+}
+__device__ __forceinline__ int read_place(int lane) {
+  const int row = lane % 16 / 4 * 8 + lane % 4;
+  return row * kBK + ((lane / 16) ^ swizzle(row)) * 8;
+}
+// Where fragment i's rows begin.
+__device__ __forceinline__ constexpr int fragment_at(int i) { return (i / 2 * 32 + i % 2 * 4) * kBK; }
+
 template <int BT, int NW>
-__device__ __forceinline__ void load_tile(const _Float16* src, int64_t row0, int64_t k0, int64_t ld, _Float16* lds,
-                                          int wave, int lane) {
+__device__ __forceinline__ void load_tile(const _Float16* src, _Float16* lds, int wave, int place) {
+  static_assert(NW % 2 == 0, "a wavefront's rows begin at the same place of 32 each time");
 #pragma unroll
-  for (int i = 0; i < BT / 8 / NW; ++i) {
-    const int rb = (i * NW + wave) * 8, r = rb + lane / 8;
-    const int piece = (lane % 8) ^ ((r >> 1) & 7);
-    __builtin_amdgcn_global_load_lds((gptr)(uintptr_t)(src + (row0 + r) * ld + k0 + piece * 8), (lptr)(lds + rb * kBK),
-                                     16, 0, 0);
+  for (int i = 0; i < BT / 16 / NW; ++i) {
+    const int rb = (i * NW + wave) * 16;
+    __builtin_amdgcn_global_load_lds((gptr)(uintptr_t)(src + rb * kBK + place), (lptr)(lds + rb * kBK), 16, 0, 0);
   }
 }
 
-__device__ __forceinline__ half8 fragment(const _Float16* lds, int row, int piece) {
-  return *(const half8*)(lds + row * kBK + ((piece ^ ((row >> 1) & 7)) * 8));
+template <int N>
+__device__ __forceinline__ void wait_loads() {  // until at most N of this wavefront's are under way
+  if (N == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  if (N == 2) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
+  if (N == 4) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+  if (N == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+  static_assert(N == 0 || N == 2 || N == 4 || N == 8, "");
+}
+
+__device__ __forceinline__ void block_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Lanes 4q .. 4q + 3 hold a 4 x 4 block by columns (element e of lane i:
+// row e, column i); after it by rows (element e of lane i: row i, column e).
+__device__ __forceinline__ half4 transpose4(half4 v, int lane) {
+  typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+  const u2 x = __builtin_bit_cast(u2, v);
+  // columns 2i, 2i + 1 of a row in one word: odd rows go to odd lanes
+  const uint32_t ox = (uint32_t)__builtin_amdgcn_mov_dpp((int)x[0], 0xB1, 0xf, 0xf, true);  // lane ^ 1
+  const uint32_t oy = (uint32_t)__builtin_amdgcn_mov_dpp((int)x[1], 0xB1, 0xf, 0xf, true);
+  const bool odd = lane & 1;
+  const uint32_t p = odd ? __builtin_amdgcn_perm(x[0], ox, 0x07060302) : __builtin_amdgcn_perm(ox, x[0], 0x05040100);
+  const uint32_t q = odd ? __builtin_amdgcn_perm(x[1], oy, 0x07060302) : __builtin_amdgcn_perm(oy, x[1], 0x05040100);
+  // p: row 0 or 1, q: row 2 or 3, of this lane's pair of columns; rows 2, 3 belong in lanes 2, 3
+  const bool high = lane & 2;
+  const uint32_t got = (uint32_t)__builtin_amdgcn_mov_dpp((int)(high ? p : q), 0x4E, 0xf, 0xf, true);  // lane ^ 2
+  const u2 o = {high ? got : p, high ? q : got};
+  return __builtin_bit_cast(half4, o);
+}
+
+// The same for FP32.
+__device__ __forceinline__ float dpp_xor1(float x) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0xB1, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float dpp_xor2(float x) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x4E, 0xf, 0xf, true));
+}
+__device__ __forceinline__ void transpose4(float (&v)[4], int lane) {
+  const bool odd = lane & 1, high = lane & 2;
+#pragma unroll
+  for (int e = 0; e < 4; e += 2) {
+    const float got = dpp_xor1(odd ? v[e] : v[e + 1]);
+    if (odd)
+      v[e] = got;
+    else
+      v[e + 1] = got;
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const float got = dpp_xor2(high ? v[e] : v[e + 2]);
+    if (high)
+      v[e] = got;
+    else
+      v[e + 2] = got;
+  }
+}
+
+// Rows 4 x + (0 .. 3) of a pair of columns of four, after transposition: row 4 x + lane % 4, eight columns.
+__device__ __forceinline__ half8 transpose8(half8 c0, half8 c1, int x, int lane) {
+  const half4 a = {c0[4 * x], c0[4 * x + 1], c0[4 * x + 2], c0[4 * x + 3]};
+  const half4 b = {c1[4 * x], c1[4 * x + 1], c1[4 * x + 2], c1[4 * x + 3]};
+  const half4 p = transpose4(a, lane), q = transpose4(b, lane);
+  return half8{p[0], p[1], p[2], p[3], q[0], q[1], q[2], q[3]};
+}
+
+template <typename T>
+struct alignas(16) Eight {
+  T v[8];
+};
+
+// Eight results of one row of the caller's matrix, columns c .. c + 7 of n.
+template <typename T>
+__device__ __forceinline__ void store_eight(const ProdArgs& a, int64_t off, int64_t c, int64_t n, const float (&o)[8]) {
+  T* p = (T*)a.dst.p + off;
+  if (a.vec && c + 7 < n) {
+    Eight<T> w;
+    if (a.update) w = *(const Eight<T>*)p;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      w.v[e] = from_f32<T>(a.update ? fmaf(a.keep, to_f32(w.v[e]), -a.rate * o[e]) : o[e]);
+    *(Eight<T>*)p = w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (c + e < n) p[e] = from_f32<T>(a.update ? fmaf(a.keep, to_f32(p[e]), -a.rate * o[e]) : o[e]);
+  }
+}
+
+// The last step's results into the caller's matrix: rows (long side) r .. r + 7 of columns (short side)
+// cq + 4 y + lane % 4, times the scale.  Eight adjacent elements of a row of it are rows here, or, where it is tall,
+// columns.
+__device__ __forceinline__ void store_last(const ProdArgs& a, int64_t b, int64_t r, int64_t rq, int64_t cq, int lane,
+                                           float (&v)[2][8]) {
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    float o[8];
+    if (a.tall) {
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        float w[4] = {v[y][4 * x], v[y][4 * x + 1], v[y][4 * x + 2], v[y][4 * x + 3]};
+        transpose4(w, lane);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[4 * y + e] = w[e] * kInvScale;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = v[x][e] * kInvScale;
+    }
+    const int64_t row = a.tall ? rq + 4 * x : cq + 4 * x + lane % 4, col = a.tall ? cq : r;
+    const int64_t rows = a.tall ? a.n : a.m, cols = a.tall ? a.m : a.n;
+    const int64_t off = b * a.dst.stride + row * a.dst.ld + col;
+    if (row < rows) {
+      if (a.dst.type == NF_TYPE_F32)
+        store_eight<float>(a, off, col, cols, o);
+      else if (a.dst.type == NF_TYPE_BF16)
+        store_eight<Bf16>(a, off, col, cols, o);
+      else
+        store_eight<_Float16>(a, off, col, cols, o);
+    }
+  }
 }
 
 // D = P Q^T over one BT x BT tile, WM x WN of it per wavefront.  Lane l of a
 // 16 x 16 part holds rows 4 (l / 16) .. + 3 of column l % 16.
+//
+// Four stages of 32 k in LDS, filled three ahead of use; fragments are read
+// from LDS one stage ahead of the products that use them.  One barrier a stage: a
+// wavefront that passes it has its loads of stage s + 1 in LDS, and has read
+// stage s - 1, whose place stage s + 3 takes.  In split mode a stage holds
+// both halves of both operands, and feeds three products.
 template <int BT, int WM, int WN, bool SPLIT, int EPI>
 __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
   constexpr int NW = BT / WM * (BT / WN);
+  constexpr int OPS = SPLIT ? 4 : 2;         // tiles of a stage: P, Q (, their low halves)
+  constexpr int LOADS = OPS * BT / 16 / NW;  // of a wavefront a stage
+  constexpr int MI = WM / 16, NJ = WN / 16;
   constexpr bool SYM = EPI == GRAM || EPI == POLY;
-  __shared__ __align__(16) _Float16 lds[2][2][BT * kBK];
+  constexpr bool SHARED = EPI == GRAM && BT < 256;  // tiles of 256 are taken only where there are many
+  __shared__ __align__(16) _Float16 lds[kStages][OPS][BT * kBK];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int64_t b = blockIdx.y;
+  // blocks go round the eight XCDs: each XCD takes a contiguous share of the tiles, matrix by matrix
+  int id;
+  {
+    const int total = gridDim.x, x = blockIdx.x & 7, each = total >> 3, more = total & 7;
+    id = x * each + min(x, more) + (blockIdx.x >> 3);
+  }
+  int share = 0;  // of the k
+  if (SHARED && a.shares > 1) {
+    share = id % a.shares;
+    id /= a.shares;
+  }
+  const int per = SYM ? a.tm * (a.tm + 1) / 2 : a.tm * a.tn;
+  const int64_t b = id / per;
+  const int tile = id;
+  id -= (int)b * per;
   int ti, tj;
   if (SYM) {  // tiles on and below the diagonal, row by row
-    const int q = blockIdx.x;
-    ti = (int)((sqrtf(8.0f * (float)q + 1.0f) - 1.0f) * 0.5f);
-    while (ti * (ti + 1) / 2 > q) --ti;
-    while ((ti + 1) * (ti + 2) / 2 <= q) ++ti;
-    tj = q - ti * (ti + 1) / 2;
-  } else {
-    ti = blockIdx.x / a.tn;
-    tj = blockIdx.x - ti * a.tn;
+    ti = (int)((sqrtf(8.0f * (float)id + 1.0f) - 1.0f) * 0.5f);
+    while (ti * (ti + 1) / 2 > id) --ti;
+    while ((ti + 1) * (ti + 2) / 2 <= id) ++ti;
+    tj = id - ti * (ti + 1) / 2;
+  } else {  // four rows of tiles at a time
+    const int g = id / (4 * a.tn), rows = min(4, a.tm - 4 * g);
+    const int in = id - g * 4 * a.tn;
+    ti = 4 * g + in % rows;
+    tj = in / rows;
   }
   const int wm = wave / (BT / WN) * WM, wn = wave % (BT / WN) * WN;
-  float4v acc[WM / 16][WN / 16] = {};
+  float4v acc[MI][NJ] = {};
 
-  const int nk = (int)(a.ldk / kBK);
-  const int steps = SPLIT ? 3 * nk : nk;
-  auto load = [&](int it, int buf) {
-    const int seg = SPLIT ? (it >= nk) + (it >= 2 * nk) : 0;
-    const int64_t k0 = (int64_t)(it - seg * nk) * kBK;
-    const _Float16* p = (seg == 2 ? a.pl : a.ph) + b * a.pstride;
-    const _Float16* q = (seg == 1 ? a.ql : a.qh) + b * a.qstride;
-    load_tile<BT, NW>(p, (int64_t)ti * BT, k0, a.ldk, lds[buf][0], wave, lane);
-    load_tile<BT, NW>(q, (int64_t)tj * BT, k0, a.ldk, lds[buf][1], wave, lane);
+  // stages [first, first + stages), an even number of them
+  int first = 0, stages = (int)(a.ldk / kBK);
+  if (SHARED && a.shares > 1) {
+    const int pairs = stages / 2;
+    first = (int)((int64_t)pairs * share / a.shares) * 2;
+    stages = (int)((int64_t)pairs * (share + 1) / a.shares) * 2 - first;
+  }
+  const int64_t prow = (int64_t)a.tm * BT, qrow = SYM ? prow : (int64_t)a.tn * BT;
+  const int load_at = load_place(wave * 16, lane), read_at = read_place(lane);
+  const int64_t pat = b * a.pstride + (int64_t)ti * BT * kBK, qat = b * a.qstride + (int64_t)tj * BT * kBK;
+  auto load = [&](int s) {
+    const int64_t p = pat + (first + s) * prow * kBK, q = qat + (first + s) * qrow * kBK;
+    auto& to = lds[s % kStages];
+    load_tile<BT, NW>(a.ph + p, to[0], wave, load_at);
+    load_tile<BT, NW>(a.qh + q, to[1], wave, load_at);
+    if constexpr (SPLIT) {
+      load_tile<BT, NW>(a.pl + p, to[2], wave, load_at);
+      load_tile<BT, NW>(a.ql + q, to[3], wave, load_at);
+    }
   };
-  load(0, 0);
-  for (int it = 0; it < steps; ++it) {
-    // the loads of this tile have landed in every wavefront, and every
-    // wavefront is done with the buffer that the next ones go to
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    const int buf = it & 1;
-    if (it + 1 < steps) load(it + 1, buf ^ 1);
+  struct Frags {
+    half8 p[OPS / 2][MI], q[OPS / 2][NJ];
+  };
+  auto read = [&](int s, Frags& f) {
+    const auto& from = lds[s % kStages];
 #pragma unroll
-    for (int ks = 0; ks < kBK / 32; ++ks) {
-      half8 pf[WM / 16], qf[WN / 16];
+    for (int h = 0; h < OPS / 2; ++h) {
 #pragma unroll
-      for (int i = 0; i < WM / 16; ++i) pf[i] = fragment(lds[buf][0], wm + 16 * i + lane % 16, ks * 4 + lane / 16);
+      for (int i = 0; i < MI; ++i) f.p[h][i] = *(const half8*)(from[2 * h] + wm * kBK + fragment_at(i) + read_at);
 #pragma unroll
-      for (int j = 0; j < WN / 16; ++j) qf[j] = fragment(lds[buf][1], wn + 16 * j + lane % 16, ks * 4 + lane / 16);
+      for (int j = 0; j < NJ; ++j) f.q[h][j] = *(const half8*)(from[2 * h + 1] + wn * kBK + fragment_at(j) + read_at);
+    }
+  };
+  auto multiply = [&](const Frags& f) {
+    auto products = [&](const half8(&p)[MI], const half8(&q)[NJ]) {
 #pragma unroll
-      for (int i = 0; i < WM / 16; ++i)
+      for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int j = 0; j < WN / 16; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pf[i], qf[j], acc[i][j], 0, 0, 0);
+        for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i], q[j], acc[i][j], 0, 0, 0);
+    };
+    products(f.p[0], f.q[0]);
+    if constexpr (SPLIT) {  // low by low is beyond the 22 bits
+      products(f.p[0], f.q[1]);
+      products(f.p[1], f.q[0]);
+    }
+  };
+  // Stage s: at most `flying` loads stay under way (those of stage s + 2).  Without branches, so that the compiler
+  // knows which reads are outstanding and waits for those of this stage only.
+  auto step = [&](auto flying, auto loads, int s, Frags& now, Frags& next) {
+    wait_loads<decltype(flying)::value>();
+    block_barrier();
+    if (decltype(loads)::value) load(s + 3);
+    read(s + 1, next);
+    multiply(now);
+  };
+  using std::integral_constant;
+  const integral_constant<int, LOADS> two;
+  const integral_constant<int, 0> none;
+  const integral_constant<int, 1> more;
+  Frags f0, f1;
+  load(0);
+  load(1);  // stages is even: sides are multiples of 64
+  if (stages > 2) {
+    load(2);
+    wait_loads<2 * LOADS>();
+  } else {
+    wait_loads<LOADS>();
+  }
+  block_barrier();
+  read(0, f0);
+  if (stages > 2) {
+    int s = 0;
+    for (; s + 4 < stages; s += 2) {
+      step(two, more, s, f0, f1);
+      step(two, more, s + 1, f1, f0);
+    }
+    step(two, more, s, f0, f1);
+    step(two, none, s + 1, f1, f0);
+  }
+  step(none, none, stages - 2, f0, f1);
+  multiply(f1);
+
+  if constexpr (SHARED) {
+    if (a.shares > 1) {
+      // Each share's sums go to memory; the block that is last to arrive adds them up, in the order of the shares.
+      // They are written and read past the caches of the XCDs (relaxed atomics of the card's scope), so that no
+      // block has to write back or drop a whole cache: with fences this launch took four times as long.
+      constexpr int N = MI * NJ * 2 * NW * 64;  // 8-byte words of a tile
+      uint64_t* part = a.part + (int64_t)tile * a.shares * N;
+      const int at = wave * MI * NJ * 128 + lane;
+#pragma unroll
+      for (int i = 0; i < MI * NJ * 2; ++i) {
+        const float4v v = acc[i / 2 / NJ][i / 2 % NJ];
+        const float2v w = {v[i % 2 * 2], v[i % 2 * 2 + 1]};
+        __hip_atomic_store(part + (int64_t)share * N + at + i * 64, __builtin_bit_cast(uint64_t, w), __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // they have arrived
+      __shared__ int last;
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        last = __hip_atomic_fetch_add(a.arrived + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.shares - 1;
+        if (last) __hip_atomic_store(a.arrived + tile, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+      __syncthreads();
+      if (!last) return;
+#pragma unroll
+      for (int i = 0; i < MI * NJ; ++i) acc[i / NJ][i % NJ] = float4v{};
+      for (int k = 0; k < a.shares; ++k) {
+#pragma unroll
+        for (int i = 0; i < MI * NJ * 2; ++i) {
+          const uint64_t u = __hip_atomic_load(part + (int64_t)k * N + at + i * 64, __ATOMIC_RELAXED,
+                                               __HIP_MEMORY_SCOPE_AGENT);
+          const float2v w = __builtin_bit_cast(float2v, u);
+          acc[i / 2 / NJ][i / 2 % NJ][i % 2 * 2] += w[0];
+          acc[i / 2 / NJ][i / 2 % NJ][i % 2 * 2 + 1] += w[1];
+        }
+      }
     }
   }
 
+  // Two pairs of fragments at a time: rows r .. r + 7 of columns c and c + 4; transposed, rows rq and rq + 4 of
+  // columns cq .. cq + 7.
 #pragma unroll
-  for (int i = 0; i < WM / 16; ++i) {
+  for (int i = 0; i < MI; i += 2) {
 #pragma unroll
-    for (int j = 0; j < WN / 16; ++j) {
-      const int64_t r = (int64_t)ti * BT + wm + 16 * i + lane / 16 * 4;  // and the three after it
-      const int64_t c = (int64_t)tj * BT + wn + 16 * j + lane % 16;
-      const float4v d = acc[i][j];
-      if (EPI == GRAM || EPI == POLY) {
-        float v[4];
+    for (int j = 0; j < NJ; j += 2) {
+      const int64_t r = (int64_t)ti * BT + wm + 16 * i + lane / 16 * 8;
+      const int64_t cq = (int64_t)tj * BT + wn + 16 * j + lane % 16 / 4 * 8;
+      const int64_t rq = r + lane % 4;
+      float v[2][8];  // [column][row]
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int64_t c = cq + 4 * y + lane % 4;
+        float d[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[e] = acc[i + e / 4][j + y][e % 4];
         if (EPI == GRAM) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            v[e] = d[e] * kInvScale;  // A times the scale
+          for (int e = 0; e < 8; ++e) {
+            v[y][e] = d[e] * kInvScale;  // A times the scale
             if (r + e == c) {
-              a.dA[b * a.Mp + c] = v[e] * kInvScale;
-              v[e] = 0.0f;
+              a.dA[b * a.Mp + c] = v[y][e] * kInvScale;
+              v[y][e] = 0.0f;
             }
           }
-        } else {
-          const half4 oh = *(const half4*)(a.ah + b * a.ostride + c * a.old + r);
-          half4 ol = {};
-          if (SPLIT) ol = *(const half4*)(a.al + b * a.ostride + c * a.old + r);
+        } else if (EPI == POLY) {
+          const int64_t at = b * a.ostride + panel_at(c, r, a.Mp);
+          const half8 oh = *(const half8*)(a.ah + at);
+          half8 ol = {};
+          if (SPLIT) ol = *(const half8*)(a.al + at);
           const float dc = a.dA[b * a.Mp + c];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
+          for (int e = 0; e < 8; ++e) {
             const float dr = a.dA[b * a.Mp + r + e], o = (float)oh[e] + (float)ol[e];
             // (D + O)^2 = D^2 + D O + O D + O O
-            v[e] = fmaf(a.c, fmaf(dr + dc, o, d[e] * kInvScale), a.b * o);
+            v[y][e] = fmaf(a.c, fmaf(dr + dc, o, d[e] * kInvScale), a.b * o);
             if (r + e == c) {
               a.dB[b * a.Mp + c] = fmaf(a.c, fmaf(dc, dc, d[e] * kInvScale * kInvScale), a.b * dc);
-              v[e] = 0.0f;
+              v[y][e] = 0.0f;
             }
           }
-        }
-        half4 h, l;
+        } else {  // rows are the long side, columns the short one
+          const int64_t at = b * a.Mp * a.Np + panel_at(c, r, a.Mp);
+          const half8 xh = *(const half8*)(a.xh + at), xl = *(const half8*)(a.xl + at);
+          const float q = a.dB[b * a.Mp + c];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          h[e] = (_Float16)v[e];
-          l[e] = (_Float16)(v[e] - (float)h[e]);
-        }
-        *(half4*)(a.oh + b * a.ostride + c * a.old + r) = h;
-        if (SPLIT) *(half4*)(a.ol + b * a.ostride + c * a.old + r) = l;
-        if (ti != tj) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            a.oh[b * a.ostride + (r + e) * a.old + c] = h[e];
-            if (SPLIT) a.ol[b * a.ostride + (r + e) * a.old + c] = l[e];
+          for (int e = 0; e < 8; ++e) {
+            const float h = (float)xh[e], x = h + (float)xl[e];
+            v[y][e] = fmaf(a.a, x, fmaf(q, SPLIT || EPI == LAST ? x : h, d[e] * kInvScale));
           }
         }
-      } else {  // rows are the long side, columns the short one
-        const int64_t at = b * a.Mp * a.Np + c * a.Np + r;
-        const half4 xh = *(const half4*)(a.xh + at), xl = *(const half4*)(a.xl + at);
-        const float q = a.dB[b * a.Mp + c];
-        float v[4];
+      }
+      if (EPI == LAST) {
+        store_last(a, b, r, rq, cq, lane, v);
+        continue;
+      }
+      half8 h[2], l[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float h = (float)xh[e], x = h + (float)xl[e];
-          v[e] = fmaf(a.a, x, fmaf(q, SPLIT || EPI == LAST ? x : h, d[e] * kInvScale));
+      for (int y = 0; y < 2; ++y) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          h[y][e] = (_Float16)v[y][e];
+          l[y][e] = (_Float16)(v[y][e] - (float)h[y][e]);
         }
-        if (EPI == STEP) {
-          half4 h, l;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            h[e] = (_Float16)v[e];
-            l[e] = (_Float16)(v[e] - (float)h[e]);
-          }
-          *(half4*)(a.xh + at) = h;
-          *(half4*)(a.xl + at) = l;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            a.oh[b * a.ostride + (r + e) * a.old + c] = h[e];
-            if (SPLIT) a.ol[b * a.ostride + (r + e) * a.old + c] = l[e];
-          }
-        } else if (c < a.m) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (r + e >= a.n) break;
-            const float o = v[e] * kInvScale;
-            const int64_t off = b * a.dst.stride + (a.tall ? (r + e) * a.dst.ld + c : c * a.dst.ld + r + e);
-            store_elem(a.dst, off, a.update ? fmaf(a.keep, load_elem(a.dst, off), -a.rate * o) : o);
-          }
+        const int64_t c = cq + 4 * y + lane % 4;
+        if (SYM) {
+          const int64_t at = b * a.ostride + panel_at(c, r, a.Mp);
+          *(half8*)(a.oh + at) = h[y];
+          if (SPLIT) *(half8*)(a.ol + at) = l[y];
+        } else {
+          const int64_t at = b * a.Mp * a.Np + panel_at(c, r, a.Mp);
+          *(half8*)(a.xh + at) = h[y];
+          *(half8*)(a.xl + at) = l[y];
         }
+      }
+      if (SYM && ti == tj) continue;  // the block on the diagonal has both halves
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int64_t to = b * a.ostride + panel_at(rq + 4 * x, cq, SYM ? a.Mp : a.Np);
+        *(half8*)(a.oh + to) = transpose8(h[0], h[1], x, lane);
+        if (SPLIT) *(half8*)(a.ol + to) = transpose8(l[0], l[1], x, lane);
       }
     }
   }
@@ -362,8 +635,29 @@ struct Plan {
   int64_t rows, cols, batch, m, n, Mp, Np;
   int tall, tile, nparts, lg_tx;
   bool split;
+  int shares;      // of a GRAM tile's k
+  int64_t tiles;   // GRAM's, if it has shares
+  size_t gpart, arrived;
   size_t part, dA, dB, xh, xl, th[2], tl[2], ah, al, bh, bl, total;
 };
+
+constexpr int64_t kCUs = 256;
+
+// The largest tile that still fills the card, by the tiles of a STEP.
+int tile_of(int64_t m, int64_t n, int64_t batch, bool split) {
+  auto tiles = [&](int64_t t) { return batch * ceil_div(m, t) * ceil_div(n, t); };
+  if (m <= 64) return 64;
+  if (!split && tiles(256) >= 2 * kCUs) return 256;
+  if (tiles(128) >= kCUs) return 128;
+  return 64;
+}
+
+// Blocks that share the k of a GRAM tile: as many as fill the card, each with eight stages at least.
+int shares_of(int64_t tiles, int64_t stages, int tile) {
+  const int64_t want = 2 * kCUs / tiles, most = stages / 8;
+  const int64_t n = want < most ? want : most;
+  return tile == 256 || n < 1 ? 1 : (int)n;
+}
 
 // Sizes are checked by the caller.
 Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split) {
@@ -374,12 +668,12 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split) {
   p.tall = rows > cols;
   p.m = p.tall ? cols : rows;
   p.n = p.tall ? rows : cols;
-  p.tile = p.m <= 64 ? 64 : 128;
-  p.Mp = ceil_div(p.m, p.tile) * p.tile;
-  p.Np = ceil_div(p.n, p.tile) * p.tile;
   // a short side of few rows has few roundings to average out (3.4e-3 measured at 1 x 7), and costs launches,
   // not products: always in pairs
   p.split = split || p.m <= 64;
+  p.tile = tile_of(p.m, p.n, batch, p.split);
+  p.Mp = ceil_div(p.m, p.tile) * p.tile;
+  p.Np = ceil_div(p.n, p.tile) * p.tile;
   p.nparts = (int)(ceil_div(rows * cols, kNormElems) < kMaxParts ? ceil_div(rows * cols, kNormElems) : kMaxParts);
   while (p.lg_tx < 8 && (1 << p.lg_tx) < cols) ++p.lg_tx;
   size_t at = 0;
@@ -404,17 +698,28 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split) {
     p.al = take(a);
     p.bl = take(a);
   }
+  const int64_t tm = p.Mp / p.tile, tiles = batch * (tm * (tm + 1) / 2);
+  p.shares = shares_of(tiles, p.Np / kBK, p.tile);
+  if (p.shares > 1) {
+    p.gpart = take((size_t)(4 * tiles * p.shares * p.tile * p.tile));
+    p.arrived = take((size_t)(4 * tiles));
+    p.tiles = tiles;
+  }
   p.total = at;
   return p;
 }
 
 template <int EPI, bool SPLIT>
 hipError_t launch_prod(const Plan& p, const ProdArgs& a, int64_t tiles, hipStream_t s) {
-  const dim3 grid((unsigned)tiles, (unsigned)p.batch);
+  const unsigned grid = (unsigned)(tiles * p.batch * (EPI == GRAM ? a.shares : 1));
   if (p.tile == 64)
-    k_prod<64, 32, 32, true, EPI><<<grid, 256, 0, s>>>(a);
+    k_prod<64, 32, 32, SPLIT, EPI><<<grid, 256, 0, s>>>(a);
+  else if (SPLIT)
+    k_prod<128, 64, 32, true, EPI><<<grid, 512, 0, s>>>(a);
+  else if (p.tile == 128)
+    k_prod<128, 64, 64, false, EPI><<<grid, 256, 0, s>>>(a);
   else
-    k_prod<128, 64, 64, SPLIT, EPI><<<grid, 256, 0, s>>>(a);
+    k_prod<256, 128, 64, false, EPI><<<grid, 512, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -423,7 +728,14 @@ hipError_t launch_prod(const Plan& p, const ProdArgs& a, int64_t tiles, hipStrea
   return p.split ? launch_prod<EPI, true>(p, a, tiles, s) : launch_prod<EPI, false>(p, a, tiles, s);
 }
 
+// Whether eight adjacent elements, at every eighth column, are aligned for 16-byte accesses.
+bool by_eights(const View& v, int64_t batch) {
+  const int64_t unit = 16 / (int64_t)type_bytes(v.type);
+  return (uintptr_t)v.p % 16 == 0 && v.ld % unit == 0 && (batch == 1 || v.stride % unit == 0);
+}
+
 hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_params& o, void* ws, hipStream_t s) {
+  last.vec = by_eights(last.dst, p.batch);
   unsigned char* w = static_cast<unsigned char*>(ws);
   auto half = [&](size_t at) { return reinterpret_cast<_Float16*>(w + at); };
   pa.rows = p.rows;
@@ -439,6 +751,8 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
   pa.xl = half(p.xl);
   pa.th = half(p.th[0]);
   pa.tl = p.split ? half(p.tl[0]) : nullptr;
+  pa.arrived = reinterpret_cast<int32_t*>(w + p.arrived);
+  pa.tiles = p.tiles;
   k_norm<<<dim3((unsigned)p.nparts, (unsigned)p.batch), kNormThreads, 0, s>>>(pa);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -460,6 +774,9 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
     g.m = p.m;
     g.n = p.n;
     g.tall = p.tall;
+    g.shares = p.shares;
+    g.part = reinterpret_cast<uint64_t*>(w + p.gpart);
+    g.arrived = reinterpret_cast<int32_t*>(w + p.arrived);
     g.xh = half(p.xh);
     g.xl = half(p.xl);
 
@@ -468,9 +785,9 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
     x.pl = x.ql = half(p.xl);
     x.ldk = p.Np;
     x.pstride = x.qstride = p.Mp * p.Np;
+    x.tm = x.tn = (int32_t)tm;
     x.oh = half(p.ah);
     x.ol = p.split ? half(p.al) : nullptr;
-    x.old = p.Mp;
     x.ostride = p.Mp * p.Mp;
     if ((e = launch_prod<GRAM>(p, x, sym, s)) != hipSuccess) return e;
 
@@ -495,7 +812,6 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
     x.tn = (int32_t)tm;
     x.oh = half(p.th[from ^ 1]);
     x.ol = p.split ? half(p.tl[from ^ 1]) : nullptr;
-    x.old = p.Mp;
     x.ostride = p.Mp * p.Np;
     e = k + 1 < o.steps ? launch_prod<STEP>(p, x, tn * tm, s) : launch_prod<LAST>(p, x, tn * tm, s);
     if (e != hipSuccess) return e;
