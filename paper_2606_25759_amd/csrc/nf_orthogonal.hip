@@ -54,8 +54,8 @@ constexpr float kInvScale = 1.0f / kScale;
 constexpr int kBK = 32;                   // k of one stage: a panel
 constexpr int kStages = 4;                // LDS stages of k_prod
 constexpr int kNormThreads = 256;
-constexpr int kNormElems = 16384;         // elements of a norm partial, at least
-constexpr int kMaxParts = 256;
+constexpr int kNormElems = 4096;          // elements of a norm partial, at least
+constexpr int kMaxParts = 1024;           // of a matrix
 
 enum { GRAM, POLY, STEP, LAST };
 
@@ -77,7 +77,8 @@ struct PrepArgs {
   int64_t Mp, Np;      // padded short and long side
   double* part;        // [batch][nparts]
   int32_t nparts;
-  int32_t lg_tx;       // k_norm: log2 of the threads across a row
+  int32_t lg_tx;       // k_norm: log2 of the threads across a row, four elements each
+  int32_t vec;         // four adjacent elements are aligned to their size
   float eps;
   _Float16 *xh, *xl, *th, *tl;  // tl: split only
   int32_t* arrived;    // to be zeroed
@@ -108,10 +109,32 @@ struct ProdArgs {
   int32_t* arrived;                   // [tile], zero between launches
 };
 
-__device__ __forceinline__ float load_elem(const View& v, int64_t off) {
-  if (v.type == NF_TYPE_F32) return ((const float*)v.p)[off];
-  if (v.type == NF_TYPE_BF16) return to_f32(((const Bf16*)v.p)[off]);
-  return (float)((const _Float16*)v.p)[off];
+template <typename T>
+struct alignas(4 * sizeof(T)) Four {
+  T v[4];
+};
+
+// Elements c .. c + 3 of n of a row at p + off; zeros past the row's end.
+template <typename T>
+__device__ __forceinline__ float4v load_four(const void* p, int64_t off, int64_t c, int64_t n, bool vec) {
+  const T* q = (const T*)p + off;
+  float4v v = {};
+  if (vec && c + 3 < n) {
+    const Four<T> w = *(const Four<T>*)q;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = to_f32(w.v[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < n) v[e] = to_f32(q[e]);
+  }
+  return v;
+}
+
+__device__ __forceinline__ float4v load_four(const View& g, int64_t off, int64_t c, int64_t n, bool vec) {
+  if (g.type == NF_TYPE_F32) return load_four<float>(g.p, off, c, n, vec);
+  if (g.type == NF_TYPE_BF16) return load_four<Bf16>(g.p, off, c, n, vec);
+  return load_four<_Float16>(g.p, off, c, n, vec);
 }
 
 // Where (row, k) of a matrix of R rows lies.
@@ -119,18 +142,21 @@ __device__ __forceinline__ int64_t panel_at(int64_t row, int64_t k, int64_t R) {
   return ((k / kBK) * R + row) * kBK + k % kBK;
 }
 
-// U at (r, c), the momentum already stepped.
-__device__ __forceinline__ float value_of(const PrepArgs& a, int64_t b, int64_t r, int64_t c) {
-  float m = 0.0f;
+// U at columns c .. c + 3 of row r, the momentum already stepped.
+__device__ __forceinline__ float4v value_of(const PrepArgs& a, int64_t b, int64_t r, int64_t c) {
+  float4v m = {};
   if (a.mom) {
-    m = a.mom[b * a.mom_stride + r * a.mom_ld + c];
+    m = load_four<float>(a.mom, b * a.mom_stride + r * a.mom_ld + c, c, a.cols, a.vec);
     if (!a.nesterov) return m;
   }
-  const float g = load_elem(a.g, b * a.g.stride + r * a.g.ld + c);
-  return a.mom ? fmaf(a.mu, m, g) : g;
+  float4v u = load_four(a.g, b * a.g.stride + r * a.g.ld + c, c, a.cols, a.vec);
+  if (a.mom)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] = fmaf(a.mu, m[e], u[e]);
+  return u;
 }
 
-// The block's sum of x in a fixed order, in thread 0.
+// The block's sum of x in a fixed order, in every thread.
 __device__ double block_sum(double x, double* s) {
   for (int o = 32; o; o >>= 1) x += __shfl_down(x, o);
   if (threadIdx.x % 64 == 0) s[threadIdx.x / 64] = x;
@@ -152,15 +178,25 @@ __global__ __launch_bounds__(kNormThreads) void k_norm(PrepArgs a) {
   const int x = threadIdx.x & (tx - 1), y = threadIdx.x >> a.lg_tx;
   double sum = 0.0;
   for (int64_t r = (int64_t)blockIdx.x * ty + y; r < a.rows; r += (int64_t)gridDim.x * ty) {
-    for (int64_t c = x; c < a.cols; c += tx) {
-      float u = load_elem(a.g, b * a.g.stride + r * a.g.ld + c);
+    for (int64_t c = 4 * x; c < a.cols; c += 4 * tx) {
+      float4v u = load_four(a.g, b * a.g.stride + r * a.g.ld + c, c, a.cols, a.vec);
       if (a.mom) {
-        float* mp = a.mom + b * a.mom_stride + r * a.mom_ld + c;
-        const float m = fmaf(a.mu, *mp, u);
-        *mp = m;
-        u = a.nesterov ? fmaf(a.mu, m, u) : m;
+        const int64_t off = b * a.mom_stride + r * a.mom_ld + c;
+        float4v m = load_four<float>(a.mom, off, c, a.cols, a.vec);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[e] = fmaf(a.mu, m[e], u[e]);
+        if (a.vec && c + 3 < a.cols) {
+          *(float4v*)(a.mom + off) = m;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (c + e < a.cols) a.mom[off + e] = m[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[e] = a.nesterov ? fmaf(a.mu, m[e], u[e]) : m[e];
       }
-      sum += (double)u * (double)u;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += (double)u[e] * (double)u[e];
     }
   }
   sum = block_sum(sum, s);
@@ -173,17 +209,12 @@ __global__ __launch_bounds__(kNormThreads) void k_scale(PrepArgs a) {
   __shared__ double s[kNormThreads / 64];
   __shared__ float tile[64][65];
   const int64_t b = blockIdx.z;
-  const double ss = block_sum(threadIdx.x < a.nparts ? a.part[b * a.nparts + threadIdx.x] : 0.0, s);
-  const double norm = sqrt(ss) + (double)a.eps;
+  double part = 0.0;
+  for (int i = threadIdx.x; i < a.nparts; i += kNormThreads) part += a.part[b * a.nparts + i];
+  const double norm = sqrt(block_sum(part, s)) + (double)a.eps;
   const double inv = norm > 0.0 || norm != norm ? (double)kScale / norm : 0.0;
   const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
-  const int x = threadIdx.x % 64, y = threadIdx.x / 64;
-  for (int i = y; i < 64; i += 4) {
-    float v = 0.0f;
-    if (r0 + i < a.rows && c0 + x < a.cols) v = (float)((double)value_of(a, b, r0 + i, c0 + x) * inv);
-    tile[i][x] = v;
-  }
-  __syncthreads();
+  const int x = threadIdx.x % 16 * 4, y = threadIdx.x / 16;
   const int64_t size = a.Mp * a.Np;
   // rows x cols as it lies: X, or X^T where the caller's matrix is tall
   const int64_t R0 = a.tall ? a.Np : a.Mp, R1 = a.tall ? a.Mp : a.Np;
@@ -191,14 +222,30 @@ __global__ __launch_bounds__(kNormThreads) void k_scale(PrepArgs a) {
   _Float16* h1 = (a.tall ? a.xh : a.th) + b * size;
   _Float16* l0 = a.tall ? a.tl : a.xl;
   _Float16* l1 = a.tall ? a.xl : a.tl;
-  for (int i = y; i < 64; i += 4) {
-    const float v = tile[i][x], w = tile[x][i];
-    const _Float16 vh = (_Float16)v, wh = (_Float16)w;
-    const int64_t at0 = panel_at(r0 + i, c0 + x, R0), at1 = panel_at(c0 + i, r0 + x, R1);
-    h0[at0] = vh;
-    h1[at1] = wh;
-    if (l0) l0[b * size + at0] = (_Float16)(v - (float)vh);
-    if (l1) l1[b * size + at1] = (_Float16)(w - (float)wh);
+  auto store = [&](_Float16* hi, _Float16* lo, int64_t at, float4v v) {
+    half4 h, l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      h[e] = (_Float16)v[e];
+      l[e] = (_Float16)(v[e] - (float)h[e]);
+    }
+    *(half4*)(hi + at) = h;
+    if (lo) *(half4*)(lo + b * size + at) = l;
+  };
+#pragma unroll
+  for (int i = 0; i < 64; i += 16) {
+    const int64_t r = r0 + y + i;
+    float4v v = {};
+    if (r < a.rows && c0 + x < a.cols) v = value_of(a, b, r, c0 + x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) tile[y + i][x + e] = v[e] = (float)((double)v[e] * inv);
+    store(h0, l0, panel_at(r, c0 + x, R0), v);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 64; i += 16) {
+    const float4v v = {tile[x][y + i], tile[x + 1][y + i], tile[x + 2][y + i], tile[x + 3][y + i]};
+    store(h1, l1, panel_at(c0 + y + i, r0 + x, R1), v);
   }
 }
 
@@ -382,14 +429,13 @@ __device__ __forceinline__ void store_last(const ProdArgs& a, int64_t b, int64_t
 // wavefront that passes it has its loads of stage s + 1 in LDS, and has read
 // stage s - 1, whose place stage s + 3 takes.  In split mode a stage holds
 // both halves of both operands, and feeds three products.
-template <int BT, int WM, int WN, bool SPLIT, int EPI>
+template <int BT, int WM, int WN, bool SPLIT, int EPI, bool SHARED = false>
 __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
   constexpr int NW = BT / WM * (BT / WN);
   constexpr int OPS = SPLIT ? 4 : 2;         // tiles of a stage: P, Q (, their low halves)
   constexpr int LOADS = OPS * BT / 16 / NW;  // of a wavefront a stage
   constexpr int MI = WM / 16, NJ = WN / 16;
   constexpr bool SYM = EPI == GRAM || EPI == POLY;
-  constexpr bool SHARED = EPI == GRAM && BT < 256;  // tiles of 256 are taken only where there are many
   __shared__ __align__(16) _Float16 lds[kStages][OPS][BT * kBK];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   // blocks go round the eight XCDs: each XCD takes a contiguous share of the tiles, matrix by matrix
@@ -399,7 +445,7 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
     id = x * each + min(x, more) + (blockIdx.x >> 3);
   }
   int share = 0;  // of the k
-  if (SHARED && a.shares > 1) {
+  if (SHARED) {
     share = id % a.shares;
     id /= a.shares;
   }
@@ -424,7 +470,7 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
 
   // stages [first, first + stages), an even number of them
   int first = 0, stages = (int)(a.ldk / kBK);
-  if (SHARED && a.shares > 1) {
+  if (SHARED) {
     const int pairs = stages / 2;
     first = (int)((int64_t)pairs * share / a.shares) * 2;
     stages = (int)((int64_t)pairs * (share + 1) / a.shares) * 2 - first;
@@ -505,37 +551,45 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
   multiply(f1);
 
   if constexpr (SHARED) {
-    if (a.shares > 1) {
-      // Each share's sums go to memory; the block that is last to arrive adds them up, in the order of the shares.
-      // They are written and read past the caches of the XCDs (relaxed atomics of the card's scope), so that no
-      // block has to write back or drop a whole cache: with fences this launch took four times as long.
-      constexpr int N = MI * NJ * 2 * NW * 64;  // 8-byte words of a tile
-      uint64_t* part = a.part + (int64_t)tile * a.shares * N;
-      const int at = wave * MI * NJ * 128 + lane;
+    // Each share's sums go to memory; the block that is last to arrive adds them up, in the order of the shares.
+    // They are written and read past the caches of the XCDs (relaxed atomics of the card's scope), so that no
+    // block has to write back or drop a whole cache: with fences this launch took four times as long.
+    constexpr int N = MI * NJ * 2 * NW * 64;    // 8-byte words of a tile
+    constexpr int kAtOnce = BT == 64 ? 4 : 1;  // shares under way
+    uint64_t* part = a.part + (int64_t)tile * a.shares * N;
+    const int at = wave * MI * NJ * 128 + lane;
 #pragma unroll
-      for (int i = 0; i < MI * NJ * 2; ++i) {
-        const float4v v = acc[i / 2 / NJ][i / 2 % NJ];
-        const float2v w = {v[i % 2 * 2], v[i % 2 * 2 + 1]};
-        __hip_atomic_store(part + (int64_t)share * N + at + i * 64, __builtin_bit_cast(uint64_t, w), __ATOMIC_RELAXED,
-                           __HIP_MEMORY_SCOPE_AGENT);
-      }
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // they have arrived
-      __shared__ int last;
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        last = __hip_atomic_fetch_add(a.arrived + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.shares - 1;
-        if (last) __hip_atomic_store(a.arrived + tile, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      }
-      __syncthreads();
-      if (!last) return;
+    for (int i = 0; i < MI * NJ * 2; ++i) {
+      const float4v v = acc[i / 2 / NJ][i / 2 % NJ];
+      const float2v w = {v[i % 2 * 2], v[i % 2 * 2 + 1]};
+      __hip_atomic_store(part + (int64_t)share * N + at + i * 64, __builtin_bit_cast(uint64_t, w), __ATOMIC_RELAXED,
+                         __HIP_MEMORY_SCOPE_AGENT);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // they have arrived
+    __shared__ int last;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      last = __hip_atomic_fetch_add(a.arrived + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.shares - 1;
+      if (last) __hip_atomic_store(a.arrived + tile, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!last) return;
 #pragma unroll
-      for (int i = 0; i < MI * NJ; ++i) acc[i / NJ][i % NJ] = float4v{};
-      for (int k = 0; k < a.shares; ++k) {
+    for (int i = 0; i < MI * NJ; ++i) acc[i / NJ][i % NJ] = float4v{};
+    for (int k = 0; k < a.shares; k += kAtOnce) {
+      uint64_t u[kAtOnce][MI * NJ * 2];
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q)
+#pragma unroll
+        for (int i = 0; i < MI * NJ * 2; ++i)
+          u[q][i] = __hip_atomic_load(part + (int64_t)min(k + q, a.shares - 1) * N + at + i * 64, __ATOMIC_RELAXED,
+                                      __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) {
+        if (k + q >= a.shares) break;
 #pragma unroll
         for (int i = 0; i < MI * NJ * 2; ++i) {
-          const uint64_t u = __hip_atomic_load(part + (int64_t)k * N + at + i * 64, __ATOMIC_RELAXED,
-                                               __HIP_MEMORY_SCOPE_AGENT);
-          const float2v w = __builtin_bit_cast(float2v, u);
+          const float2v w = __builtin_bit_cast(float2v, u[q][i]);
           acc[i / 2 / NJ][i / 2 % NJ][i % 2 * 2] += w[0];
           acc[i / 2 / NJ][i / 2 % NJ][i % 2 * 2 + 1] += w[1];
         }
@@ -652,11 +706,15 @@ int tile_of(int64_t m, int64_t n, int64_t batch, bool split) {
   return 64;
 }
 
-// Blocks that share the k of a GRAM tile: as many as fill the card, each with eight stages at least.
+// Blocks that share the k of a GRAM tile, as far as the tiles leave the card empty.  A stage takes about 0.25 us and
+// adding up a share 0.35 us, so their sum is least at the square root of 0.7 of the stages.  256 x 2304: 12.7 us with
+// 9 shares, 13.6 with 18, 36 with one; 1000 x 1601 (136 tiles of 64): 17.6 us with 3, 30 with one.
 int shares_of(int64_t tiles, int64_t stages, int tile) {
-  const int64_t want = 2 * kCUs / tiles, most = stages / 8;
-  const int64_t n = want < most ? want : most;
-  return tile == 256 || n < 1 ? 1 : (int)n;
+  if (tile == 256) return 1;
+  const int64_t free = (tile == 64 ? 2 : 1) * kCUs / tiles;
+  const int64_t best = (int64_t)sqrt(0.7 * (double)stages);
+  const int64_t n = free < best ? free : best;
+  return n < 1 ? 1 : (int)n;
 }
 
 // Sizes are checked by the caller.
@@ -675,7 +733,7 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split) {
   p.Mp = ceil_div(p.m, p.tile) * p.tile;
   p.Np = ceil_div(p.n, p.tile) * p.tile;
   p.nparts = (int)(ceil_div(rows * cols, kNormElems) < kMaxParts ? ceil_div(rows * cols, kNormElems) : kMaxParts);
-  while (p.lg_tx < 8 && (1 << p.lg_tx) < cols) ++p.lg_tx;
+  while (p.lg_tx < 8 && (4 << p.lg_tx) < cols) ++p.lg_tx;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t o = at;
@@ -711,7 +769,18 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split) {
 
 template <int EPI, bool SPLIT>
 hipError_t launch_prod(const Plan& p, const ProdArgs& a, int64_t tiles, hipStream_t s) {
-  const unsigned grid = (unsigned)(tiles * p.batch * (EPI == GRAM ? a.shares : 1));
+  const unsigned grid = (unsigned)(tiles * p.batch);
+  if constexpr (EPI == GRAM) {
+    if (p.shares > 1) {
+      if (p.tile == 64)
+        k_prod<64, 32, 32, SPLIT, EPI, true><<<grid * p.shares, 256, 0, s>>>(a);
+      else if (SPLIT)
+        k_prod<128, 64, 32, true, EPI, true><<<grid * p.shares, 512, 0, s>>>(a);
+      else
+        k_prod<128, 64, 64, false, EPI, true><<<grid * p.shares, 256, 0, s>>>(a);
+      return hipGetLastError();
+    }
+  }
   if (p.tile == 64)
     k_prod<64, 32, 32, SPLIT, EPI><<<grid, 256, 0, s>>>(a);
   else if (SPLIT)
@@ -728,6 +797,10 @@ hipError_t launch_prod(const Plan& p, const ProdArgs& a, int64_t tiles, hipStrea
   return p.split ? launch_prod<EPI, true>(p, a, tiles, s) : launch_prod<EPI, false>(p, a, tiles, s);
 }
 
+bool by_fours(const View& v, int64_t batch) {
+  return (uintptr_t)v.p % (4 * type_bytes(v.type)) == 0 && v.ld % 4 == 0 && (batch == 1 || v.stride % 4 == 0);
+}
+
 // Whether eight adjacent elements, at every eighth column, are aligned for 16-byte accesses.
 bool by_eights(const View& v, int64_t batch) {
   const int64_t unit = 16 / (int64_t)type_bytes(v.type);
@@ -735,6 +808,8 @@ bool by_eights(const View& v, int64_t batch) {
 }
 
 hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_params& o, void* ws, hipStream_t s) {
+  pa.vec = by_fours(pa.g, p.batch) &&
+           (!pa.mom || by_fours(View{pa.mom, pa.mom_ld, pa.mom_stride, NF_TYPE_F32}, p.batch));
   last.vec = by_eights(last.dst, p.batch);
   unsigned char* w = static_cast<unsigned char*>(ws);
   auto half = [&](size_t at) { return reinterpret_cast<_Float16*>(w + at); };
