@@ -5,7 +5,7 @@
 //   k_sort      tiles of a worker's tokens sorted by id in LDS (stable, so
 //               tokens of one id stay in their order), while the launch's
 //               other blocks zero the workers' segments
-//   k_merge     pairs of sorted runs into one, until a worker has one run
+//   k_merge     up to kRuns sorted runs into one
 //   k_partial   sums of the stretches of kChunk sorted tokens that are all of
 //               one id: a frequent token's rows are summed by many wavefronts
 //   k_rows_sum  a wavefront per kOwn sorted tokens and 256 columns: the rows
@@ -15,6 +15,8 @@
 // segment written once and dy read once.  The order in which a row's terms
 // are added depends on the sorted tokens alone, so results are reproducible
 // bit for bit.
+#include <type_traits>
+
 #include "nf_internal.h"
 #include "nf_types.h"
 
@@ -73,7 +75,10 @@ __global__ __launch_bounds__(kThreadsE) void k_lookup(LookupArgs a) {
 
 constexpr int kChunk = 64;  // sorted tokens of a partial sum
 constexpr int kOwn = 16;    // sorted tokens of a wavefront of k_rows_sum
-constexpr int kCols = 256;  // columns of a wavefront
+constexpr int kRuns = 16;   // sorted runs of a merge
+// From this many tokens on, k_partial is run; with fewer, the wavefront that has a frequent id's first token adds all
+// its rows (16 batches of 16 at most).
+constexpr int64_t kPartialTokens = 256;
 
 struct GradArgs {
   const void* dy;
@@ -95,9 +100,11 @@ struct GradArgs {
   int32_t bits;             // of V
 };
 
-// Zeroes n floats at p with the blocks b of nb: whole 16-byte pieces, and
+// Zeroes n floats at p with the blocks b of nb: whole 16-byte pieces, 64 KiB
+// of them at a time (5.6 TB/s; 4.7 when all blocks write side by side), and
 // what lies before the first and after the last one.
 __device__ void fill_zero(float* p, int64_t n, int64_t b, int64_t nb) {
+  constexpr int64_t kPiece = 4096;
   const int64_t head = min((int64_t)((-(intptr_t)p) & 15) / 4, n);
   const int64_t n4 = (n - head) / 4, tail = n - head - 4 * n4;
   if (b == 0) {
@@ -105,7 +112,10 @@ __device__ void fill_zero(float* p, int64_t n, int64_t b, int64_t nb) {
     if (threadIdx.x < tail) p[n - 1 - threadIdx.x] = 0.0f;
   }
   float4* q = (float4*)(p + head);
-  for (int64_t i = b * blockDim.x + threadIdx.x; i < n4; i += nb * blockDim.x) q[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int64_t at = b * kPiece; at < n4; at += nb * kPiece) {
+    const int64_t end = min(at + kPiece, n4);
+    for (int64_t i = at + threadIdx.x; i < end; i += blockDim.x) q[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
 }
 
 // Least-significant-digit radix sort of up to THREADS * ITEMS tokens, 8 bits
@@ -211,189 +221,234 @@ __global__ __launch_bounds__(THREADS) void k_sort(GradArgs a) {
   }
 }
 
-// Runs of a.run tokens, two and two: a token goes behind those of its own run
-// before it and those of the other run with a smaller id (of the earlier run:
-// or the same).
+// Groups of kRuns runs of a.run tokens: a token goes behind those of its own
+// run before it and those of every other run with a smaller id (of the
+// earlier runs: or the same).  Neighbours in a run have neighbouring ids, so
+// a wavefront's searches touch the same few lines.
 __global__ __launch_bounds__(kThreadsE) void k_merge(GradArgs a) {
   const int64_t i = (int64_t)blockIdx.x * kThreadsE + threadIdx.x;
   if (i >= a.T) return;
   const uint32_t* key = a.key + (int64_t)blockIdx.y * a.T;
-  const int64_t r = i / a.run, base = r / 2 * 2 * a.run;
-  const int64_t o0 = min((r ^ 1) * a.run, a.T), o1 = min(o0 + a.run, a.T);
-  const uint32_t k = key[i], limit = k + (r & 1);  // ids below it go first; k <= V < 2^31
-  int64_t lo = o0, hi = o1;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) / 2;
-    if (key[mid] < limit)
-      lo = mid + 1;
-    else
-      hi = mid;
+  const int T = (int)a.T, len = (int)a.run;  // at most 2^24 and 2^28
+  const int run = (int)(i / len), r = run % kRuns;
+  const int64_t base = (int64_t)(run - r) * len;
+  const int others = (int)min((int64_t)kRuns, (T - base + len - 1) / len) - 1;  // runs of the group but its own
+  const uint32_t k = key[i];
+  int64_t to = base + i - (int64_t)run * len;
+  constexpr int kAtOnce = 4;
+  for (int q0 = 0; q0 < others; q0 += kAtOnce) {
+    int lo[kAtOnce], hi[kAtOnce];
+#pragma unroll
+    for (int e = 0; e < kAtOnce; ++e) {
+      const int q = q0 + e < r ? q0 + e : q0 + e + 1;  // not its own
+      lo[e] = (int)min(base + (int64_t)q * len, (int64_t)T);
+      // past the group's runs (kRuns - 1 is no multiple of kAtOnce) there may be the next group's
+      hi[e] = q0 + e < others ? (int)min((int64_t)lo[e] + len, (int64_t)T) : lo[e];
+      to -= lo[e];
+    }
+    for (;;) {
+      bool busy = false;
+#pragma unroll
+      for (int e = 0; e < kAtOnce; ++e) {
+        const int mid = (lo[e] + hi[e]) / 2;
+        const bool open = lo[e] < hi[e];
+        const bool before = key[open ? mid : 0] < k + (q0 + e < r ? 1u : 0u);  // k <= V < 2^31
+        if (open && before) lo[e] = mid + 1;
+        if (open && !before) hi[e] = mid;
+        busy |= open;
+      }
+      if (!__any(busy)) break;
+    }
+#pragma unroll
+    for (int e = 0; e < kAtOnce; ++e) to += lo[e];
   }
-  const int64_t to = base + (i - r * a.run) + (lo - o0);
   a.key2[(int64_t)blockIdx.y * a.T + to] = k;
   a.order2[(int64_t)blockIdx.y * a.T + to] = a.order[(int64_t)blockIdx.y * a.T + i];
 }
 
 // ---------------------------------------------------------------- the sums
 
-// A lane's four columns of a wavefront's 256: adjacent where rows allow
-// 4-element accesses, else 64 apart.
-template <bool VEC>
-__device__ __forceinline__ int column(int c0, int lane, int e) {
-  return VEC ? c0 + 4 * lane + e : c0 + 64 * e + lane;
+// A lane's N adjacent columns of a row (four; one where rows have fewer than
+// four), at any element's address: the card reads and writes across
+// alignment.
+template <typename T, int N>
+struct __attribute__((packed)) Near {
+  T v[N];
+};
+
+// A block's columns are an even share of a row's, in whole lanes; the last
+// lane that has any takes the last N (its neighbour may have some of them
+// too, and comes to the same values), so that no access needs a condition.
+struct Columns {
+  int at;     // of this lane
+  bool mine;  // false: `at` is another lane's too, and this one stores nothing
+};
+template <int N>
+__device__ __forceinline__ Columns columns_of(int d, int lane) {
+  const int width = ((d + gridDim.y - 1) / gridDim.y + N - 1) / N * N;
+  const int end = min((int)(blockIdx.y + 1) * width, d), c = blockIdx.y * width + N * lane;
+  return {max(min(c, end - N), 0), c < end};
 }
 
-template <typename D, bool VEC>
-__device__ __forceinline__ float4 load_row(const D* row, int c0, int lane, int d) {
-  float v[4] = {0.f, 0.f, 0.f, 0.f};
-  if (VEC) {
-    if (c0 + 4 * lane < d) {
-      const Pack<D, 4> p = *(const Pack<D, 4>*)(row + c0 + 4 * lane);
+template <typename D, int N>
+__device__ __forceinline__ Near<D, N> load_row(const D* row, Columns c) {
+  return *(const Near<D, N>*)(row + c.at);
+}
+
+template <typename D, int N>
+__device__ __forceinline__ void add_to(float (&s)[N], const Near<D, N>& x) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = to_f32(p.v[e]);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (c0 + 64 * e + lane < d) v[e] = to_f32(row[c0 + 64 * e + lane]);
-  }
-  return make_float4(v[0], v[1], v[2], v[3]);
+  for (int e = 0; e < N; ++e) s[e] += to_f32(x.v[e]);
 }
 
-__device__ __forceinline__ void add4(float4& s, const float4& x) {
-  s.x += x.x;
-  s.y += x.y;
-  s.z += x.z;
-  s.w += x.w;
-}
+constexpr int kDepth = 16;  // rows under way
 
-template <bool VEC>
-__device__ __forceinline__ void store_row(float* row, int c0, int lane, int d, float4 s, float scale, bool add) {
-  float v[4] = {s.x * scale, s.y * scale, s.z * scale, s.w * scale};
-  if (VEC) {
-    if (c0 + 4 * lane < d) {
-      float4* p = (float4*)(row + c0 + 4 * lane);
-      if (add) {
-        const float4 o = *p;
-        v[0] += o.x;
-        v[1] += o.y;
-        v[2] += o.z;
-        v[3] += o.w;
-      }
-      *p = make_float4(v[0], v[1], v[2], v[3]);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int c = c0 + 64 * e + lane;
-      if (c < d) row[c] = add ? row[c] + v[e] : v[e];
-    }
-  }
-}
-
-constexpr int kDepth = 8;  // rows in flight
-
-// s += the rows of sorted tokens [p, q) (q - p <= 64), in order.
-template <typename D, bool VEC>
-__device__ __forceinline__ void add_rows(const GradArgs& a, const D* dy, const uint32_t* order, int64_t p, int64_t q, int c0,
-                                         int lane, float4& s) {
-  const uint32_t mine = order[min(p + lane, q - 1)];
-  const int n = (int)(q - p);
+// s += the rows that row(i) names, i in [0, n), in order; past the last, it is named again and not added.
+template <typename D, int N, typename F>
+__device__ __forceinline__ void add_rows(int n, Columns c, float (&s)[N], F row) {
   for (int i = 0; i < n; i += kDepth) {
-    float4 x[kDepth];
+    Near<D, N> x[kDepth];
 #pragma unroll
-    for (int k = 0; k < kDepth; ++k) {
-      x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (i + k < n) x[k] = load_row<D, VEC>(dy + (int64_t)__builtin_amdgcn_readlane(mine, i + k) * a.dy_ld, c0, lane, a.d);
-    }
+    for (int k = 0; k < kDepth; ++k) x[k] = load_row<D, N>(row(min(i + k, n - 1)), c);
 #pragma unroll
     for (int k = 0; k < kDepth; ++k)
-      if (i + k < n) add4(s, x[k]);
+      if (i + k < n) add_to(s, x[k]);
   }
 }
 
-// Chunk of kChunk sorted tokens of one id: their sum.
-template <typename D, bool VEC>
-__global__ __launch_bounds__(64) void k_partial(GradArgs a) {
-  const int lane = threadIdx.x, w = blockIdx.z, c0 = blockIdx.y * kCols;
+// Those of sorted tokens [p, q), q - p <= 64.
+template <typename D, int N>
+__device__ __forceinline__ void add_tokens(const GradArgs& a, const D* dy, const uint32_t* order, int64_t p, int64_t q,
+                                           Columns c, int lane, float (&s)[N]) {
+  const uint32_t token = order[min(p + lane, q - 1)];
+  add_rows<D, N>((int)(q - p), c, s,
+                 [&](int i) { return dy + (int64_t)(uint32_t)__builtin_amdgcn_readlane(token, i) * a.dy_ld; });
+}
+
+// Chunk of kChunk sorted tokens of one id: their sum.  Each of four
+// wavefronts adds a quarter of the rows, in order; the quarters are added in
+// order.
+template <typename D, int N>
+__global__ __launch_bounds__(kThreadsE) void k_partial(GradArgs a) {
+  constexpr int kParts = kThreadsE / 64, kRowsEach = kChunk / kParts;
   const int64_t p = (int64_t)blockIdx.x * kChunk;  // p + kChunk <= T
+  const int w = blockIdx.z;
   const uint32_t* key = a.key + (int64_t)w * a.T;
   const uint32_t k = key[p];
   if (k != key[p + kChunk - 1] || k >= (uint32_t)a.V) return;
-  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-  add_rows<D, VEC>(a, (const D*)a.dy + (int64_t)w * a.dy_stride, a.order + (int64_t)w * a.T, p, p + kChunk, c0, lane, s);
-  float* out = a.part + ((int64_t)w * gridDim.x + blockIdx.x) * a.d;
-  const float v[4] = {s.x, s.y, s.z, s.w};
+  __shared__ float sums[kParts][64][N];
+  const int lane = threadIdx.x % 64, part = threadIdx.x / 64;
+  const Columns c = columns_of<N>(a.d, lane);
+  float s[N] = {};
+  add_tokens<D, N>(a, (const D*)a.dy + (int64_t)w * a.dy_stride, a.order + (int64_t)w * a.T, p + part * kRowsEach,
+                   p + (part + 1) * kRowsEach, c, lane, s);
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (column<VEC>(c0, lane, e) < a.d) out[column<VEC>(c0, lane, e)] = v[e];
+  for (int e = 0; e < N; ++e) sums[part][lane][e] = s[e];
+  __syncthreads();
+  if (part || !c.mine) return;
+  Near<float, N> v;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    v.v[e] = s[e];
+    for (int q = 1; q < kParts; ++q) v.v[e] += sums[q][lane][e];
+  }
+  *(Near<float, N>*)(a.part + ((int64_t)w * gridDim.x + blockIdx.x) * a.d + c.at) = v;
 }
 
 // Sorted tokens [p0, p0 + kOwn): every id whose first token is one of them.
-template <typename D, bool VEC>
+// The rows of all of them are asked for at once: an id does not wait for the
+// one before it.
+template <typename D, int N, bool ADD>
 __global__ __launch_bounds__(64) void k_rows_sum(GradArgs a) {
-  const int lane = threadIdx.x, w = blockIdx.z, c0 = blockIdx.y * kCols;
-  const int64_t p0 = (int64_t)blockIdx.x * kOwn, p1 = min(p0 + kOwn, a.T);
+  const int lane = threadIdx.x, w = blockIdx.z;
+  const Columns c = columns_of<N>(a.d, lane);
+  const int64_t p0 = (int64_t)blockIdx.x * kOwn;
+  const int count = (int)min((int64_t)kOwn, a.T - p0);
   const uint32_t* key = a.key + (int64_t)w * a.T;
   const uint32_t* order = a.order + (int64_t)w * a.T;
   const D* dy = (const D*)a.dy + (int64_t)w * a.dy_stride;
-  const float* part = a.part + (int64_t)w * (a.T / kChunk) * a.d;
   float* grads = a.grads + (int64_t)w * a.worker_stride;
-  // lane i < kOwn + 1: the id before position p0 + i, and at it
-  const int64_t at = p0 + lane;
-  const uint32_t none = 0xffffffffu;
-  const uint32_t here = lane <= kOwn && at < a.T ? key[at] : none;
-  const uint32_t prev = lane < kOwn && at > 0 && at - 1 < a.T ? key[at - 1] : none;
-  // the positions where an id that belongs to a row begins
-  uint64_t begins = __ballot(lane < kOwn && at < p1 && here != prev && here < (uint32_t)a.V);
-  const uint64_t changes = __ballot(lane <= kOwn && lane > 0 && at <= p1 && here != prev) | 1ull << kOwn;
-  while (begins) {
-    const int i = __builtin_ctzll(begins);
-    begins &= begins - 1;
-    const uint32_t id = __builtin_amdgcn_readlane(here, i);
-    int64_t p = p0 + i;
-    // the first change after i, or the end of what this wavefront looked at
-    int64_t q = p0 + __builtin_ctzll(changes >> (i + 1)) + i + 1;
-    q = min(q, a.T);
-    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (q < p1 || q == a.T || key[q] != id) {
-      add_rows<D, VEC>(a, dy, order, p, q, c0, lane, s);
+  const uint32_t none = 0xffffffffu, V = (uint32_t)a.V;
+  // lane i <= kOwn: the id at position p0 + i, and before it
+  const uint32_t token = order[p0 + min(lane, count - 1)];
+  const uint32_t here = lane <= kOwn && p0 + lane < a.T ? key[p0 + lane] : none;
+  uint32_t prev = __shfl_up(here, 1);
+  if (lane == 0) prev = p0 > 0 ? key[p0 - 1] : none;
+  const uint64_t begins = __ballot(lane < count && here != prev && here < V);
+  if (!begins) return;
+  const int first = __builtin_ctzll(begins);
+  // positions that an id from `first` on has; those of no row come last
+  const int end = __popcll(__ballot(lane < count && here < V));
+  Near<D, N> x[kOwn];
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i)
+    x[i] = load_row<D, N>(
+        dy + (int64_t)(uint32_t)__builtin_amdgcn_readlane(token, min(max(i, first), end - 1)) * a.dy_ld, c);
+  auto row_of = [&](int i) {
+    const uint32_t id = (uint32_t)__builtin_amdgcn_readlane(here, min(max(i, first), end - 1));
+    return (Near<float, N>*)(grads + (int64_t)id * a.d + c.at);
+  };
+  // what the rows hold is asked for with the rest: a load behind a store would wait for it
+  Near<float, N> old[ADD ? kOwn : 1] = {};
+  if constexpr (ADD) {
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) old[i] = *row_of(i);
+  }
+  float s[N] = {};
+  auto finish = [&](int i) {  // the id that began at position i
+    Near<float, N> v = ADD ? old[i] : old[0];
+#pragma unroll
+    for (int e = 0; e < N; ++e) v.v[e] += s[e] * a.scale;
+    if (c.mine) *row_of(i) = v;
+  };
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+    if (i < first || i >= end) continue;
+    if (begins >> i & 1) {
+      if (i > first) finish(i - 1);  // of the same id as the one before this
+#pragma unroll
+      for (int e = 0; e < N; ++e) s[e] = 0.0f;
+    }
+    add_to(s, x[i]);
+  }
+  const uint32_t id = (uint32_t)__builtin_amdgcn_readlane(here, end - 1);
+  int64_t p = p0 + end;
+  if (end == kOwn && p < a.T && (uint32_t)__builtin_amdgcn_readlane(here, kOwn) == id) {
+    // it runs on: to the next multiple of kChunk, then whole chunks by their sums, then what is left
+    auto run_on = [&](int64_t limit) {  // of the next 64 positions, those before `limit` with this id
+      return p + __popcll(__ballot(p + lane < limit && key[min(p + lane, a.T - 1)] == id));
+    };
+    if (a.T < kPartialTokens) {
+      for (int64_t q; (q = run_on(a.T)) > p; p = q) add_tokens<D, N>(a, dy, order, p, q, c, lane, s);
     } else {
-      // it runs on: to the next multiple of kChunk, whole chunks by their sums, and what is left
-      int64_t edge = min((p / kChunk + 1) * kChunk, a.T);
-      q = p + __popcll(__ballot(p + lane < edge && key[min(p + lane, a.T - 1)] == id));
-      add_rows<D, VEC>(a, dy, order, p, q, c0, lane, s);
+      const int64_t edge = min((p + kChunk - 1) / kChunk * kChunk, a.T);
+      int64_t q = run_on(edge);
+      if (q > p) add_tokens<D, N>(a, dy, order, p, q, c, lane, s);
       p = q;
-      if (p == edge && p < a.T) {
+      if (p == edge) {
         for (;;) {
           const int64_t last = p + (int64_t)lane * kChunk + kChunk - 1;
           const int n = __popcll(__ballot(last < a.T && key[min(last, a.T - 1)] == id));
-          for (int c = 0; c < n; c += kDepth) {
-            float4 x[kDepth];
-#pragma unroll
-            for (int e = 0; e < kDepth; ++e) {
-              x[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-              if (c + e < n) {
-                const float* row = part + (p / kChunk + c + e) * a.d;
-                float v[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) v[u] = column<VEC>(c0, lane, u) < a.d ? row[column<VEC>(c0, lane, u)] : 0.0f;
-                x[e] = make_float4(v[0], v[1], v[2], v[3]);
-              }
-            }
-#pragma unroll
-            for (int e = 0; e < kDepth; ++e)
-              if (c + e < n) add4(s, x[e]);
-          }
+          const float* part = a.part + ((int64_t)w * (a.T / kChunk) + p / kChunk) * a.d;
+          add_rows<float, N>(n, c, s, [&](int i) { return part + (int64_t)i * a.d; });
           p += (int64_t)n * kChunk;
           if (n < 64) break;
         }
-        q = p + __popcll(__ballot(p + lane < a.T && key[min(p + lane, a.T - 1)] == id));
-        if (q > p) add_rows<D, VEC>(a, dy, order, p, q, c0, lane, s);
+        q = run_on(a.T);
+        if (q > p) add_tokens<D, N>(a, dy, order, p, q, c, lane, s);
       }
     }
-    store_row<VEC>(grads + (int64_t)id * a.d, c0, lane, a.d, s, a.scale, a.accumulate);
   }
+  // the last id: `end` is not known when this is compiled, so what its row held is found among the others' again
+  Near<float, N> v = {};
+  if constexpr (ADD) {
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i)
+      if (i == end - 1) v = old[i];
+  }
+#pragma unroll
+  for (int e = 0; e < N; ++e) v.v[e] += s[e] * a.scale;
+  if (c.mine) *row_of(end - 1) = v;
 }
 
 // ------------------------------------------------------------------- hosts
@@ -405,9 +460,9 @@ struct GradPlan {
 
 GradPlan plan_of(int32_t W, int64_t T, int64_t d) {
   GradPlan p = {};
-  p.cap = T <= 1024 ? 1024 : T <= 4096 ? 4096 : 16384;
+  p.cap = T <= 1024 ? 1024 : 4096;
   p.tiles = (int)ceil_div(T, p.cap);
-  for (int64_t run = p.cap; run < T; run *= 2) ++p.passes;
+  for (int64_t run = p.cap; run < T; run *= kRuns) ++p.passes;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t o = at;
@@ -421,7 +476,7 @@ GradPlan plan_of(int32_t W, int64_t T, int64_t d) {
     p.key[1] = take(n);
     p.order[1] = take(n);
   }
-  p.part = take((size_t)W * (size_t)(T / kChunk) * (size_t)d * 4);
+  if (T >= kPartialTokens) p.part = take((size_t)W * (size_t)(T / kChunk) * (size_t)d * 4);
   p.total = at;
   return p;
 }
@@ -443,22 +498,16 @@ const char* check_grad_sizes(int32_t W, int64_t T, int64_t V, int64_t d) {
   return nullptr;
 }
 
-template <typename D>
-void launch_sums(const GradArgs& a, bool vec, hipStream_t s) {
-  const unsigned slices = (unsigned)ceil_div(a.d, kCols);
-  const int64_t chunks = a.T / kChunk;
-  if (chunks) {
-    const dim3 grid((unsigned)chunks, slices, (unsigned)a.W);
-    if (vec)
-      k_partial<D, true><<<grid, 64, 0, s>>>(a);
-    else
-      k_partial<D, false><<<grid, 64, 0, s>>>(a);
-  }
+template <typename D, int N>
+void launch_sums(const GradArgs& a, hipStream_t s) {
+  const unsigned slices = (unsigned)ceil_div(a.d, 64 * N);
+  if (a.T >= kPartialTokens)
+    k_partial<D, N><<<dim3((unsigned)(a.T / kChunk), slices, (unsigned)a.W), kThreadsE, 0, s>>>(a);
   const dim3 grid((unsigned)ceil_div(a.T, kOwn), slices, (unsigned)a.W);
-  if (vec)
-    k_rows_sum<D, true><<<grid, 64, 0, s>>>(a);
+  if (a.accumulate)
+    k_rows_sum<D, N, true><<<grid, 64, 0, s>>>(a);
   else
-    k_rows_sum<D, false><<<grid, 64, 0, s>>>(a);
+    k_rows_sum<D, N, false><<<grid, 64, 0, s>>>(a);
 }
 
 // Blocks that zero a worker's segment: 64 KiB each at least, 4,096 in all at most.
@@ -562,14 +611,12 @@ nf_status nf_embedding_grad(const void* dy, int32_t dy_type, int64_t dy_ld, int6
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (p.cap == 1024)
     launch_sort<256, 4>(a, s);
-  else if (p.cap == 4096)
-    launch_sort<1024, 4>(a, s);
   else
-    launch_sort<1024, 16>(a, s);
+    launch_sort<1024, 4>(a, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || T == 0) return finish(e);
   a.run = p.cap;
-  for (int k = 0; k < p.passes; ++k, a.run *= 2) {
+  for (int k = 0; k < p.passes; ++k, a.run *= kRuns) {
     const int to = (k + 1) & 1;
     a.key = words(p.key[to ^ 1]);
     a.order = words(p.order[to ^ 1]);
@@ -580,11 +627,13 @@ nf_status nf_embedding_grad(const void* dy, int32_t dy_type, int64_t dy_ld, int6
     a.key = a.key2;
     a.order = a.order2;
   }
-  // four adjacent elements at a time where every row of dy and of the table allows it
-  const size_t four = 4 * type_bytes(dy_type);
-  const bool vec = d % 4 == 0 && dy_ld % 4 == 0 && (W == 1 || (dy_stride % 4 == 0 && worker_stride % 4 == 0)) &&
-                   (uintptr_t)dy % four == 0 && (uintptr_t)grads % 16 == 0;
-  with_type(dy_type, [&](auto* tp) { launch_sums<std::remove_pointer_t<decltype(tp)>>(a, vec, s); });
+  with_type(dy_type, [&](auto* tp) {
+    using D = std::remove_pointer_t<decltype(tp)>;
+    if (d < 4)
+      launch_sums<D, 1>(a, s);
+    else
+      launch_sums<D, 4>(a, s);
+  });
   return finish(hipGetLastError());
 }
 
