@@ -6,10 +6,11 @@
 //               tokens of one id stay in their order), while the launch's
 //               other blocks zero the workers' segments
 //   k_merge     up to kRuns sorted runs into one
-//   k_partial   sums of the stretches of kChunk sorted tokens that are all of
-//               one id: a frequent token's rows are summed by many wavefronts
 //   k_rows_sum  a wavefront per kOwn sorted tokens and 256 columns: the rows
-//               of every id that begins there
+//               of every id that lies in them whole, and sums of those that
+//               begin before or end after them
+//   k_join      the rows of the latter: a frequent token's rows are read by
+//               many wavefronts, and none reads more than kOwn
 //
 // All are bound by memory traffic: the gradient's floor is the dense FP32
 // segment written once and dy read once.  The order in which a row's terms
@@ -73,12 +74,8 @@ __global__ __launch_bounds__(kThreadsE) void k_lookup(LookupArgs a) {
 
 // -------------------------------------------------------------------- sort
 
-constexpr int kChunk = 64;  // sorted tokens of a partial sum
-constexpr int kOwn = 16;    // sorted tokens of a wavefront of k_rows_sum
-constexpr int kRuns = 16;   // sorted runs of a merge
-// From this many tokens on, k_partial is run; with fewer, the wavefront that has a frequent id's first token adds all
-// its rows (16 batches of 16 at most).
-constexpr int64_t kPartialTokens = 256;
+constexpr int kOwn = 16;   // sorted tokens of a wavefront of k_rows_sum
+constexpr int kRuns = 16;  // sorted runs of a merge
 
 struct GradArgs {
   const void* dy;
@@ -94,7 +91,7 @@ struct GradArgs {
   int64_t worker_stride;
   uint32_t *key, *order;    // [W][T]: sorted runs; key V: a token that adds to no row
   uint32_t *key2, *order2;  // k_merge's result
-  float* part;              // [W][T / kChunk][d]
+  float* part;              // [W][ceil(T / kOwn)][2][d]: sums of an id that began before, and of one that goes on
   int64_t run;              // tokens of a sorted run
   int32_t tiles;            // k_sort: runs of a worker
   int32_t bits;             // of V
@@ -301,63 +298,8 @@ __device__ __forceinline__ void add_to(float (&s)[N], const Near<D, N>& x) {
   for (int e = 0; e < N; ++e) s[e] += to_f32(x.v[e]);
 }
 
-constexpr int kDepth = 16;  // rows under way
-
-// s += the rows that row(i) names, i in [0, n), in order; past the last, it is named again and not added.
-template <typename D, int N, typename F>
-__device__ __forceinline__ void add_rows(int n, Columns c, float (&s)[N], F row) {
-  for (int i = 0; i < n; i += kDepth) {
-    Near<D, N> x[kDepth];
-#pragma unroll
-    for (int k = 0; k < kDepth; ++k) x[k] = load_row<D, N>(row(min(i + k, n - 1)), c);
-#pragma unroll
-    for (int k = 0; k < kDepth; ++k)
-      if (i + k < n) add_to(s, x[k]);
-  }
-}
-
-// Those of sorted tokens [p, q), q - p <= 64.
-template <typename D, int N>
-__device__ __forceinline__ void add_tokens(const GradArgs& a, const D* dy, const uint32_t* order, int64_t p, int64_t q,
-                                           Columns c, int lane, float (&s)[N]) {
-  const uint32_t token = order[min(p + lane, q - 1)];
-  add_rows<D, N>((int)(q - p), c, s,
-                 [&](int i) { return dy + (int64_t)(uint32_t)__builtin_amdgcn_readlane(token, i) * a.dy_ld; });
-}
-
-// Chunk of kChunk sorted tokens of one id: their sum.  Each of four
-// wavefronts adds a quarter of the rows, in order; the quarters are added in
-// order.
-template <typename D, int N>
-__global__ __launch_bounds__(kThreadsE) void k_partial(GradArgs a) {
-  constexpr int kParts = kThreadsE / 64, kRowsEach = kChunk / kParts;
-  const int64_t p = (int64_t)blockIdx.x * kChunk;  // p + kChunk <= T
-  const int w = blockIdx.z;
-  const uint32_t* key = a.key + (int64_t)w * a.T;
-  const uint32_t k = key[p];
-  if (k != key[p + kChunk - 1] || k >= (uint32_t)a.V) return;
-  __shared__ float sums[kParts][64][N];
-  const int lane = threadIdx.x % 64, part = threadIdx.x / 64;
-  const Columns c = columns_of<N>(a.d, lane);
-  float s[N] = {};
-  add_tokens<D, N>(a, (const D*)a.dy + (int64_t)w * a.dy_stride, a.order + (int64_t)w * a.T, p + part * kRowsEach,
-                   p + (part + 1) * kRowsEach, c, lane, s);
-#pragma unroll
-  for (int e = 0; e < N; ++e) sums[part][lane][e] = s[e];
-  __syncthreads();
-  if (part || !c.mine) return;
-  Near<float, N> v;
-#pragma unroll
-  for (int e = 0; e < N; ++e) {
-    v.v[e] = s[e];
-    for (int q = 1; q < kParts; ++q) v.v[e] += sums[q][lane][e];
-  }
-  *(Near<float, N>*)(a.part + ((int64_t)w * gridDim.x + blockIdx.x) * a.d + c.at) = v;
-}
-
-// Sorted tokens [p0, p0 + kOwn): every id whose first token is one of them.
-// The rows of all of them are asked for at once: an id does not wait for the
-// one before it.
+// Sorted tokens [p0, p0 + kOwn).  Their rows are asked for at once: an id
+// does not wait for the one before it.
 template <typename D, int N, bool ADD>
 __global__ __launch_bounds__(64) void k_rows_sum(GradArgs a) {
   const int lane = threadIdx.x, w = blockIdx.z;
@@ -365,29 +307,26 @@ __global__ __launch_bounds__(64) void k_rows_sum(GradArgs a) {
   const int64_t p0 = (int64_t)blockIdx.x * kOwn;
   const int count = (int)min((int64_t)kOwn, a.T - p0);
   const uint32_t* key = a.key + (int64_t)w * a.T;
-  const uint32_t* order = a.order + (int64_t)w * a.T;
   const D* dy = (const D*)a.dy + (int64_t)w * a.dy_stride;
   float* grads = a.grads + (int64_t)w * a.worker_stride;
   const uint32_t none = 0xffffffffu, V = (uint32_t)a.V;
   // lane i <= kOwn: the id at position p0 + i, and before it
-  const uint32_t token = order[p0 + min(lane, count - 1)];
+  const uint32_t token = a.order[(int64_t)w * a.T + p0 + min(lane, count - 1)];
   const uint32_t here = lane <= kOwn && p0 + lane < a.T ? key[p0 + lane] : none;
   uint32_t prev = __shfl_up(here, 1);
   if (lane == 0) prev = p0 > 0 ? key[p0 - 1] : none;
-  const uint64_t begins = __ballot(lane < count && here != prev && here < V);
-  if (!begins) return;
-  const int first = __builtin_ctzll(begins);
-  // positions that an id from `first` on has; those of no row come last
-  const int end = __popcll(__ballot(lane < count && here < V));
+  const uint64_t begins = __ballot(lane < count && here != prev);
+  const int end = __popcll(__ballot(lane < count && here < V));  // those of no row come last
+  if (end == 0) return;
+  const bool goes_on = end == kOwn && __builtin_amdgcn_readlane(here, kOwn) == __builtin_amdgcn_readlane(here, kOwn - 1);
+  auto row_of = [&](int i) {
+    const uint32_t id = (uint32_t)__builtin_amdgcn_readlane(here, min(i, end - 1));
+    return (Near<float, N>*)(grads + (int64_t)id * a.d + c.at);
+  };
   Near<D, N> x[kOwn];
 #pragma unroll
   for (int i = 0; i < kOwn; ++i)
-    x[i] = load_row<D, N>(
-        dy + (int64_t)(uint32_t)__builtin_amdgcn_readlane(token, min(max(i, first), end - 1)) * a.dy_ld, c);
-  auto row_of = [&](int i) {
-    const uint32_t id = (uint32_t)__builtin_amdgcn_readlane(here, min(max(i, first), end - 1));
-    return (Near<float, N>*)(grads + (int64_t)id * a.d + c.at);
-  };
+    x[i] = load_row<D, N>(dy + (int64_t)(uint32_t)__builtin_amdgcn_readlane(token, min(i, end - 1)) * a.dy_ld, c);
   // what the rows hold is asked for with the rest: a load behind a store would wait for it
   Near<float, N> old[ADD ? kOwn : 1] = {};
   if constexpr (ADD) {
@@ -395,60 +334,79 @@ __global__ __launch_bounds__(64) void k_rows_sum(GradArgs a) {
     for (int i = 0; i < kOwn; ++i) old[i] = *row_of(i);
   }
   float s[N] = {};
-  auto finish = [&](int i) {  // the id that began at position i
-    Near<float, N> v = ADD ? old[i] : old[0];
-#pragma unroll
-    for (int e = 0; e < N; ++e) v.v[e] += s[e] * a.scale;
-    if (c.mine) *row_of(i) = v;
-  };
+  bool whole = begins & 1;  // the id at hand began here
 #pragma unroll
   for (int i = 0; i < kOwn; ++i) {
-    if (i < first || i >= end) continue;
-    if (begins >> i & 1) {
-      if (i > first) finish(i - 1);  // of the same id as the one before this
-#pragma unroll
-      for (int e = 0; e < N; ++e) s[e] = 0.0f;
-    }
+    if (i >= end) continue;
     add_to(s, x[i]);
-  }
-  const uint32_t id = (uint32_t)__builtin_amdgcn_readlane(here, end - 1);
-  int64_t p = p0 + end;
-  if (end == kOwn && p < a.T && (uint32_t)__builtin_amdgcn_readlane(here, kOwn) == id) {
-    // it runs on: to the next multiple of kChunk, then whole chunks by their sums, then what is left
-    auto run_on = [&](int64_t limit) {  // of the next 64 positions, those before `limit` with this id
-      return p + __popcll(__ballot(p + lane < limit && key[min(p + lane, a.T - 1)] == id));
-    };
-    if (a.T < kPartialTokens) {
-      for (int64_t q; (q = run_on(a.T)) > p; p = q) add_tokens<D, N>(a, dy, order, p, q, c, lane, s);
+    const bool last = i == end - 1;
+    if (!last && !(begins >> (i + 1) & 1)) continue;
+    Near<float, N> v;
+    if (whole && !(last && goes_on)) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) v.v[e] = s[e] * a.scale + (ADD ? old[ADD ? i : 0].v[e] : 0.0f);
+      if (c.mine) *row_of(i) = v;
     } else {
-      const int64_t edge = min((p + kChunk - 1) / kChunk * kChunk, a.T);
-      int64_t q = run_on(edge);
-      if (q > p) add_tokens<D, N>(a, dy, order, p, q, c, lane, s);
-      p = q;
-      if (p == edge) {
-        for (;;) {
-          const int64_t last = p + (int64_t)lane * kChunk + kChunk - 1;
-          const int n = __popcll(__ballot(last < a.T && key[min(last, a.T - 1)] == id));
-          const float* part = a.part + ((int64_t)w * (a.T / kChunk) + p / kChunk) * a.d;
-          add_rows<float, N>(n, c, s, [&](int i) { return part + (int64_t)i * a.d; });
-          p += (int64_t)n * kChunk;
-          if (n < 64) break;
-        }
-        q = run_on(a.T);
-        if (q > p) add_tokens<D, N>(a, dy, order, p, q, c, lane, s);
-      }
+#pragma unroll
+      for (int e = 0; e < N; ++e) v.v[e] = s[e];
+      float* part = a.part + (((int64_t)w * gridDim.x + blockIdx.x) * 2 + whole) * a.d;
+      if (c.mine) *(Near<float, N>*)(part + c.at) = v;
     }
+    whole = true;
+#pragma unroll
+    for (int e = 0; e < N; ++e) s[e] = 0.0f;
   }
-  // the last id: `end` is not known when this is compiled, so what its row held is found among the others' again
+}
+
+// The id that begins in kOwn tokens and goes on after them: its sums in order,
+// an even share of them to each wavefront, the shares in order.
+constexpr int kThreadsJ = 512;
+constexpr int kDepth = 8;  // sums under way
+template <int N, bool ADD>
+__global__ __launch_bounds__(kThreadsJ) void k_join(GradArgs a) {
+  constexpr int kParts = kThreadsJ / 64;
+  const int64_t p0 = (int64_t)blockIdx.x * kOwn;  // p0 + kOwn < T
+  const int w = blockIdx.z, lane = threadIdx.x % 64, part = threadIdx.x / 64;
+  const uint32_t* key = a.key + (int64_t)w * a.T;
+  const uint32_t id = key[p0 + kOwn - 1];
+  if (id != key[p0 + kOwn] || id >= (uint32_t)a.V || (p0 > 0 && key[p0 - 1] == id)) return;
+  const Columns c = columns_of<N>(a.d, lane);
+  Near<float, N>* row = (Near<float, N>*)(a.grads + (int64_t)w * a.worker_stride + (int64_t)id * a.d + c.at);
   Near<float, N> v = {};
-  if constexpr (ADD) {
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i)
-      if (i == end - 1) v = old[i];
+  if (ADD) v = *row;
+  // the pieces after this one that begin with it
+  int more = 0;
+  for (;;) {
+    const int64_t p = p0 + (int64_t)(1 + more + lane) * kOwn;
+    const int n = __popcll(__ballot(p < a.T && key[min(p, a.T - 1)] == id));
+    more += n;
+    if (n < 64) break;
   }
+  const int pieces = more + 1, from = pieces * part / kParts, to = pieces * (part + 1) / kParts;
+  const float* sums = a.part + ((int64_t)w * ((a.T + kOwn - 1) / kOwn) + blockIdx.x) * 2 * a.d;
+  float s[N] = {};
+  for (int i = from; i < to; i += kDepth) {
+    Near<float, N> x[kDepth];
 #pragma unroll
-  for (int e = 0; e < N; ++e) v.v[e] += s[e] * a.scale;
-  if (c.mine) *row_of(end - 1) = v;
+    for (int k = 0; k < kDepth; ++k) {
+      const int q = min(i + k, to - 1);
+      x[k] = *(const Near<float, N>*)(sums + (2 * (int64_t)q + (q == 0)) * a.d + c.at);
+    }
+#pragma unroll
+    for (int k = 0; k < kDepth; ++k)
+      if (i + k < to) add_to(s, x[k]);
+  }
+  __shared__ float shares[kParts][64][N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) shares[part][lane][e] = s[e];
+  __syncthreads();
+  if (part || !c.mine) return;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    for (int q = 1; q < kParts; ++q) s[e] += shares[q][lane][e];
+    v.v[e] = s[e] * a.scale + v.v[e];
+  }
+  *row = v;
 }
 
 // ------------------------------------------------------------------- hosts
@@ -476,7 +434,7 @@ GradPlan plan_of(int32_t W, int64_t T, int64_t d) {
     p.key[1] = take(n);
     p.order[1] = take(n);
   }
-  if (T >= kPartialTokens) p.part = take((size_t)W * (size_t)(T / kChunk) * (size_t)d * 4);
+  p.part = take((size_t)W * (size_t)ceil_div(T, kOwn) * (size_t)d * 8);
   p.total = at;
   return p;
 }
@@ -498,16 +456,19 @@ const char* check_grad_sizes(int32_t W, int64_t T, int64_t V, int64_t d) {
   return nullptr;
 }
 
+template <typename D, int N, bool ADD>
+void launch_sums(const GradArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)ceil_div(a.T, kOwn), (unsigned)ceil_div(a.d, 64 * N), (unsigned)a.W);
+  k_rows_sum<D, N, ADD><<<grid, 64, 0, s>>>(a);
+  if (grid.x > 1) k_join<N, ADD><<<dim3(grid.x - 1, grid.y, grid.z), kThreadsJ, 0, s>>>(a);
+}
+
 template <typename D, int N>
 void launch_sums(const GradArgs& a, hipStream_t s) {
-  const unsigned slices = (unsigned)ceil_div(a.d, 64 * N);
-  if (a.T >= kPartialTokens)
-    k_partial<D, N><<<dim3((unsigned)(a.T / kChunk), slices, (unsigned)a.W), kThreadsE, 0, s>>>(a);
-  const dim3 grid((unsigned)ceil_div(a.T, kOwn), slices, (unsigned)a.W);
   if (a.accumulate)
-    k_rows_sum<D, N, true><<<grid, 64, 0, s>>>(a);
+    launch_sums<D, N, true>(a, s);
   else
-    k_rows_sum<D, N, false><<<grid, 64, 0, s>>>(a);
+    launch_sums<D, N, false>(a, s);
 }
 
 // Blocks that zero a worker's segment: 64 KiB each at least, 4,096 in all at most.
