@@ -358,55 +358,87 @@ __global__ __launch_bounds__(64) void k_rows_sum(GradArgs a) {
   }
 }
 
-// The id that begins in kOwn tokens and goes on after them: its sums in order,
-// an even share of them to each wavefront, the shares in order.
-constexpr int kThreadsJ = 512;
+// Ids that begin in kOwn tokens and go on after them, a wavefront each: their
+// sums in order.  One of more than kAlone sums is left to the whole block: an
+// even share of them to each wavefront, and the shares in order.
 constexpr int kDepth = 8;  // sums under way
-template <int N, bool ADD>
-__global__ __launch_bounds__(kThreadsJ) void k_join(GradArgs a) {
-  constexpr int kParts = kThreadsJ / 64;
-  const int64_t p0 = (int64_t)blockIdx.x * kOwn;  // p0 + kOwn < T
-  const int w = blockIdx.z, lane = threadIdx.x % 64, part = threadIdx.x / 64;
-  const uint32_t* key = a.key + (int64_t)w * a.T;
-  const uint32_t id = key[p0 + kOwn - 1];
-  if (id != key[p0 + kOwn] || id >= (uint32_t)a.V || (p0 > 0 && key[p0 - 1] == id)) return;
-  const Columns c = columns_of<N>(a.d, lane);
-  Near<float, N>* row = (Near<float, N>*)(a.grads + (int64_t)w * a.worker_stride + (int64_t)id * a.d + c.at);
-  Near<float, N> v = {};
-  if (ADD) v = *row;
-  // the pieces after this one that begin with it
-  int more = 0;
-  for (;;) {
-    const int64_t p = p0 + (int64_t)(1 + more + lane) * kOwn;
-    const int n = __popcll(__ballot(p < a.T && key[min(p, a.T - 1)] == id));
-    more += n;
-    if (n < 64) break;
-  }
-  const int pieces = more + 1, from = pieces * part / kParts, to = pieces * (part + 1) / kParts;
-  const float* sums = a.part + ((int64_t)w * ((a.T + kOwn - 1) / kOwn) + blockIdx.x) * 2 * a.d;
-  float s[N] = {};
+constexpr int kAlone = 4 * kDepth;
+
+template <int N>
+__device__ __forceinline__ void add_sums(const float* sums, int from, int to, int64_t d, Columns c, float (&s)[N]) {
   for (int i = from; i < to; i += kDepth) {
     Near<float, N> x[kDepth];
 #pragma unroll
     for (int k = 0; k < kDepth; ++k) {
-      const int q = min(i + k, to - 1);
-      x[k] = *(const Near<float, N>*)(sums + (2 * (int64_t)q + (q == 0)) * a.d + c.at);
+      const int q = min(i + k, to - 1);  // the first is of the id that goes on, the others of one that began before
+      x[k] = *(const Near<float, N>*)(sums + (2 * (int64_t)q + (q == 0)) * d + c.at);
     }
 #pragma unroll
     for (int k = 0; k < kDepth; ++k)
       if (i + k < to) add_to(s, x[k]);
   }
-  __shared__ float shares[kParts][64][N];
+}
+
+template <int N, bool ADD>
+__global__ __launch_bounds__(kThreadsE) void k_join(GradArgs a) {
+  constexpr int kWaves = kThreadsE / 64;
+  __shared__ int left[kWaves];  // sums that are left to the block
+  __shared__ float shares[kWaves][64][N];
+  const int w = blockIdx.z, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const uint32_t* key = a.key + (int64_t)w * a.T;
+  const int64_t own = (a.T + kOwn - 1) / kOwn, own0 = (int64_t)blockIdx.x * kWaves;
+  const Columns c = columns_of<N>(a.d, lane);
+  float* grads = a.grads + (int64_t)w * a.worker_stride + c.at;
+  const float* part = a.part + (int64_t)w * own * 2 * a.d;
+  auto write = [&](uint32_t id, const float(&s)[N]) {
+    if (!c.mine) return;
+    Near<float, N>* row = (Near<float, N>*)(grads + (int64_t)id * a.d);
+    Near<float, N> v = {};
+    if (ADD) v = *row;
 #pragma unroll
-  for (int e = 0; e < N; ++e) shares[part][lane][e] = s[e];
-  __syncthreads();
-  if (part || !c.mine) return;
-#pragma unroll
-  for (int e = 0; e < N; ++e) {
-    for (int q = 1; q < kParts; ++q) s[e] += shares[q][lane][e];
-    v.v[e] = s[e] * a.scale + v.v[e];
+    for (int e = 0; e < N; ++e) v.v[e] = s[e] * a.scale + v.v[e];
+    *row = v;
+  };
+  int pieces = 0;
+  const int64_t p0 = (own0 + wave) * kOwn;
+  if (p0 + kOwn < a.T) {
+    // lane 0: the id before these tokens, 1: their last one, 2: the one after them
+    const int64_t at = p0 + (lane == 0 ? -1 : kOwn - 2 + min(lane, 2));
+    const uint32_t k = at >= 0 ? key[at] : 0xffffffffu;
+    const uint32_t id = __builtin_amdgcn_readlane(k, 1);
+    if (id == (uint32_t)__builtin_amdgcn_readlane(k, 2) && id < (uint32_t)a.V &&
+        id != (uint32_t)__builtin_amdgcn_readlane(k, 0)) {
+      for (pieces = 1;;) {  // and those after it that begin with it
+        const int64_t p = p0 + (int64_t)(pieces + lane) * kOwn;
+        const int n = __popcll(__ballot(p < a.T && key[min(p, a.T - 1)] == id));
+        pieces += n;
+        if (n < 64) break;
+      }
+      if (pieces <= kAlone) {
+        float s[N] = {};
+        add_sums<N>(part + (own0 + wave) * 2 * a.d, 0, pieces, a.d, c, s);
+        write(id, s);
+      }
+    }
   }
-  *row = v;
+  if (lane == 0) left[wave] = pieces > kAlone ? pieces : 0;
+  __syncthreads();
+  for (int q = 0; q < kWaves; ++q) {
+    const int n = left[q];
+    if (n == 0) continue;
+    float s[N] = {};
+    add_sums<N>(part + (own0 + q) * 2 * a.d, n * wave / kWaves, n * (wave + 1) / kWaves, a.d, c, s);
+#pragma unroll
+    for (int e = 0; e < N; ++e) shares[wave][lane][e] = s[e];
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        for (int u = 1; u < kWaves; ++u) s[e] += shares[u][lane][e];
+      write(key[(own0 + q) * kOwn + kOwn - 1], s);
+    }
+    __syncthreads();
+  }
 }
 
 // ------------------------------------------------------------------- hosts
@@ -460,7 +492,7 @@ template <typename D, int N, bool ADD>
 void launch_sums(const GradArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)ceil_div(a.T, kOwn), (unsigned)ceil_div(a.d, 64 * N), (unsigned)a.W);
   k_rows_sum<D, N, ADD><<<grid, 64, 0, s>>>(a);
-  if (grid.x > 1) k_join<N, ADD><<<dim3(grid.x - 1, grid.y, grid.z), kThreadsJ, 0, s>>>(a);
+  if (grid.x > 1) k_join<N, ADD><<<dim3((grid.x + 3) / 4, grid.y, grid.z), kThreadsE, 0, s>>>(a);
 }
 
 template <typename D, int N>
