@@ -8,6 +8,8 @@
 //   k_prod     one product P Q^T on the matrix cores with an epilogue:
 //                GRAM  A = X X^T
 //                POLY  B = b A + c A A
+//                BOTH  GRAM and POLY where A is one tile (a short side of at
+//                      most 128): five launches less
 //                STEP  X = a X + B X
 //                LAST  the same, into the caller's matrix or weights
 //
@@ -57,7 +59,7 @@ constexpr int kNormThreads = 256;
 constexpr int kNormElems = 4096;          // elements of a norm partial, at least
 constexpr int kMaxParts = 1024;           // of a matrix
 
-enum { GRAM, POLY, STEP, LAST };
+enum { GRAM, POLY, STEP, LAST, BOTH };
 
 // One matrix of the caller's, seen as rows x cols.
 struct View {
@@ -435,7 +437,7 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
   constexpr int OPS = SPLIT ? 4 : 2;         // tiles of a stage: P, Q (, their low halves)
   constexpr int LOADS = OPS * BT / 16 / NW;  // of a wavefront a stage
   constexpr int MI = WM / 16, NJ = WN / 16;
-  constexpr bool SYM = EPI == GRAM || EPI == POLY;
+  constexpr bool SYM = EPI == GRAM || EPI == POLY || EPI == BOTH;
   __shared__ __align__(16) _Float16 lds[kStages][OPS][BT * kBK];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   // blocks go round the eight XCDs: each XCD takes a contiguous share of the tiles, matrix by matrix
@@ -491,15 +493,18 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
   struct Frags {
     half8 p[OPS / 2][MI], q[OPS / 2][NJ];
   };
-  auto read = [&](int s, Frags& f) {
-    const auto& from = lds[s % kStages];
+  auto read_from = [&](const _Float16* ph, const _Float16* qh, const _Float16* pl, const _Float16* ql, Frags& f) {
 #pragma unroll
     for (int h = 0; h < OPS / 2; ++h) {
 #pragma unroll
-      for (int i = 0; i < MI; ++i) f.p[h][i] = *(const half8*)(from[2 * h] + wm * kBK + fragment_at(i) + read_at);
+      for (int i = 0; i < MI; ++i) f.p[h][i] = *(const half8*)((h ? pl : ph) + wm * kBK + fragment_at(i) + read_at);
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) f.q[h][j] = *(const half8*)(from[2 * h + 1] + wn * kBK + fragment_at(j) + read_at);
+      for (int j = 0; j < NJ; ++j) f.q[h][j] = *(const half8*)((h ? ql : qh) + wn * kBK + fragment_at(j) + read_at);
     }
+  };
+  auto read = [&](int s, Frags& f) {
+    const auto& from = lds[s % kStages];
+    read_from(from[0], from[1], from[2 % OPS], from[3 % OPS], f);
   };
   auto multiply = [&](const Frags& f) {
     auto products = [&](const half8(&p)[MI], const half8(&q)[NJ]) {
@@ -597,6 +602,44 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
     }
   }
 
+  // BOTH: A times the scale in FP32, its diagonal apart; its FP16 matrix stays in LDS, panel by panel, for A A
+  float4v whole[EPI == BOTH ? MI : 1][EPI == BOTH ? NJ : 1];
+  __shared__ float diagonal[EPI == BOTH ? BT : 1];
+  if constexpr (EPI == BOTH) {
+    static_assert(BT / kBK <= kStages, "a panel takes the place of a stage");
+    __syncthreads();  // the stages are read
+#pragma unroll
+    for (int i = 0; i < MI; i += 2) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const int r = wm + 16 * i + lane / 16 * 8;
+        const int c = wn + j / 2 * 32 + lane % 16 / 4 * 8 + j % 2 * 4 + lane % 4;
+        half8 h, l;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float v = acc[i + e / 4][j][e % 4] * kInvScale;
+          if (r + e == c) {
+            diagonal[c] = v * kInvScale;
+            v = 0.0f;
+          }
+          whole[i + e / 4][j][e % 4] = v;
+          h[e] = (_Float16)v;
+          l[e] = (_Float16)(v - (float)h[e]);
+        }
+        const int at = c * kBK + ((r % kBK / 8) ^ swizzle(c)) * 8;
+        *(half8*)(lds[r / kBK][0] + at) = h;
+        if constexpr (SPLIT) *(half8*)(lds[r / kBK][2] + at) = l;
+        acc[i][j] = acc[i + 1][j] = float4v{};
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < BT / kBK; ++s) {
+      read_from(lds[s][0], lds[s][0], SPLIT ? lds[s][2 % OPS] : nullptr, SPLIT ? lds[s][2 % OPS] : nullptr, f0);
+      multiply(f0);
+    }
+  }
+
   // Two pairs of fragments at a time: rows r .. r + 7 of columns c and c + 4; transposed, rows rq and rq + 4 of
   // columns cq .. cq + 7.
 #pragma unroll
@@ -622,15 +665,18 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
               v[y][e] = 0.0f;
             }
           }
-        } else if (EPI == POLY) {
+        } else if (EPI == POLY || EPI == BOTH) {
           const int64_t at = b * a.ostride + panel_at(c, r, a.Mp);
-          const half8 oh = *(const half8*)(a.ah + at);
-          half8 ol = {};
-          if (SPLIT) ol = *(const half8*)(a.al + at);
-          const float dc = a.dA[b * a.Mp + c];
+          half8 oh = {}, ol = {};
+          if (EPI == POLY) oh = *(const half8*)(a.ah + at);
+          if (EPI == POLY && SPLIT) ol = *(const half8*)(a.al + at);
+          const float* dA = EPI == BOTH ? diagonal : a.dA + b * a.Mp;
+          const float dc = dA[c];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float dr = a.dA[b * a.Mp + r + e], o = (float)oh[e] + (float)ol[e];
+            const float dr = dA[r + e];
+            const float o = EPI == BOTH ? whole[EPI == BOTH ? i + e / 4 : 0][EPI == BOTH ? j + y : 0][e % 4]
+                                        : (float)oh[e] + (float)ol[e];
             // (D + O)^2 = D^2 + D O + O D + O O
             v[y][e] = fmaf(a.c, fmaf(dr + dc, o, d[e] * kInvScale), a.b * o);
             if (r + e == c) {
@@ -700,7 +746,7 @@ constexpr int64_t kCUs = 256;
 // The largest tile that still fills the card, by the tiles of a STEP.
 int tile_of(int64_t m, int64_t n, int64_t batch, bool split) {
   auto tiles = [&](int64_t t) { return batch * ceil_div(m, t) * ceil_div(n, t); };
-  if (m <= 64) return 64;
+  if (m <= 128) return m <= 64 ? 64 : 128;  // A is one tile
   if (!split && tiles(256) >= 2 * kCUs) return 256;
   if (tiles(128) >= kCUs) return 128;
   return 64;
@@ -748,12 +794,13 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split) {
   p.xl = take(x);
   p.th[0] = take(x);
   p.th[1] = take(x);
-  p.ah = take(a);
+  const bool one = p.Mp == p.tile;  // A never leaves its block
+  if (!one) p.ah = take(a);
   p.bh = take(a);
   if (p.split) {
     p.tl[0] = take(x);
     p.tl[1] = take(x);
-    p.al = take(a);
+    if (!one) p.al = take(a);
     p.bl = take(a);
   }
   const int64_t tm = p.Mp / p.tile, tiles = batch * (tm * (tm + 1) / 2);
@@ -770,7 +817,7 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split) {
 template <int EPI, bool SPLIT>
 hipError_t launch_prod(const Plan& p, const ProdArgs& a, int64_t tiles, hipStream_t s) {
   const unsigned grid = (unsigned)(tiles * p.batch);
-  if constexpr (EPI == GRAM) {
+  if constexpr (EPI == GRAM || EPI == BOTH) {
     if (p.shares > 1) {
       if (p.tile == 64)
         k_prod<64, 32, 32, SPLIT, EPI, true><<<grid * p.shares, 256, 0, s>>>(a);
@@ -787,7 +834,7 @@ hipError_t launch_prod(const Plan& p, const ProdArgs& a, int64_t tiles, hipStrea
     k_prod<128, 64, 32, true, EPI><<<grid, 512, 0, s>>>(a);
   else if (p.tile == 128)
     k_prod<128, 64, 64, false, EPI><<<grid, 256, 0, s>>>(a);
-  else
+  else if constexpr (EPI != BOTH)
     k_prod<256, 128, 64, false, EPI><<<grid, 512, 0, s>>>(a);
   return hipGetLastError();
 }
@@ -864,15 +911,20 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
     x.oh = half(p.ah);
     x.ol = p.split ? half(p.al) : nullptr;
     x.ostride = p.Mp * p.Mp;
-    if ((e = launch_prod<GRAM>(p, x, sym, s)) != hipSuccess) return e;
-
-    x.ph = x.qh = x.ah = half(p.ah);  // B = b A + c A A
-    x.pl = x.ql = x.al = p.split ? half(p.al) : nullptr;
-    x.ldk = p.Mp;
-    x.pstride = x.qstride = p.Mp * p.Mp;
-    x.oh = half(p.bh);
-    x.ol = p.split ? half(p.bl) : nullptr;
-    if ((e = launch_prod<POLY>(p, x, sym, s)) != hipSuccess) return e;
+    if (tm == 1) {
+      x.oh = half(p.bh);
+      x.ol = p.split ? half(p.bl) : nullptr;
+      if ((e = launch_prod<BOTH>(p, x, sym, s)) != hipSuccess) return e;
+    } else {
+      if ((e = launch_prod<GRAM>(p, x, sym, s)) != hipSuccess) return e;
+      x.ph = x.qh = x.ah = half(p.ah);  // B = b A + c A A
+      x.pl = x.ql = x.al = p.split ? half(p.al) : nullptr;
+      x.ldk = p.Mp;
+      x.pstride = x.qstride = p.Mp * p.Mp;
+      x.oh = half(p.bh);
+      x.ol = p.split ? half(p.bl) : nullptr;
+      if ((e = launch_prod<POLY>(p, x, sym, s)) != hipSuccess) return e;
+    }
 
     const int from = k & 1;  // X^T <- X^T B: rows of the long side
     x = g;
