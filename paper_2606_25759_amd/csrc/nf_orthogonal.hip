@@ -9,7 +9,7 @@
 //                GRAM  A = X X^T
 //                POLY  B = b A + c A A
 //                BOTH  GRAM and POLY where A is one tile (a short side of at
-//                      most 128): five launches less
+//                      most 64): a launch less a step
 //                STEP  X = a X + B X
 //                LAST  the same, into the caller's matrix or weights
 //
@@ -733,7 +733,8 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
 
 struct Plan {
   int64_t rows, cols, batch, m, n, Mp, Np;
-  int tall, tile, nparts, lg_tx;
+  int tall, nparts, lg_tx;
+  int tile, gram_tile, poly_tile;  // of STEP and LAST, GRAM and BOTH, POLY
   bool split;
   int shares;      // of a GRAM tile's k
   int64_t tiles;   // GRAM's, if it has shares
@@ -743,24 +744,60 @@ struct Plan {
 
 constexpr int64_t kCUs = 256;
 
-// The largest tile that still fills the card, by the tiles of a STEP.
-int tile_of(int64_t m, int64_t n, int64_t batch, bool split) {
-  auto tiles = [&](int64_t t) { return batch * ceil_div(m, t) * ceil_div(n, t); };
-  if (m <= 128) return m <= 64 ? 64 : 128;  // A is one tile
-  if (!split && tiles(256) >= 2 * kCUs) return 256;
-  if (tiles(128) >= kCUs) return 128;
-  return 64;
+// Microseconds that a launch's tiles take for one stage of 32 k, by how they fill the card: one block a CU with tiles
+// of 256 (one of 128 in split mode), two of 128 (64 in split mode), four of 64.  From the time of whole calls of
+// 1 to 24 matrices of 512 to 4,096 with each tile forced; a full card does 1.25 PFLOP/s of products with tiles of
+// 256, 0.98 with 128 and 0.87 with 64 (in split mode 1.3 with 128 and 1.1 with 64), but smaller tiles fill it sooner:
+// one matrix of 1000 x 1601 takes 194 us with tiles of 64, 273 with 128 and 536 with 256; four of 2048 x 2048 take
+// 1,209, 1,030 and 933 us.
+double stage_us(int tile, bool split, int64_t tiles) {
+  const int per = (tile == 64 ? 4 : tile == 128 ? 2 : 1) / (split ? 2 : 1);
+  // of a card with 1, 2, .. `per` blocks a CU
+  static const double k64[4] = {0.20, 0.25, 0.31, 0.40}, k128[2] = {0.36, 0.60}, k256[1] = {0.87};
+  static const double s64[2] = {0.28, 0.45}, s128[1] = {0.62};
+  const double* us = split ? (tile == 64 ? s64 : s128) : tile == 64 ? k64 : tile == 128 ? k128 : k256;
+  const int64_t a_cu = ceil_div(tiles, kCUs), full = a_cu / per, rest = a_cu % per;
+  return (double)full * us[per - 1] + (rest ? us[rest - 1] : 0.0);
 }
 
 // Blocks that share the k of a GRAM tile, as far as the tiles leave the card empty.  A stage takes about 0.25 us and
 // adding up a share 0.35 us, so their sum is least at the square root of 0.7 of the stages.  256 x 2304: 12.7 us with
 // 9 shares, 13.6 with 18, 36 with one; 1000 x 1601 (136 tiles of 64): 17.6 us with 3, 30 with one.
 int shares_of(int64_t tiles, int64_t stages, int tile) {
-  if (tile == 256) return 1;
-  const int64_t free = (tile == 64 ? 2 : 1) * kCUs / tiles;
+  if (tile == 256) return 1;  // built without
+  const int64_t free = (tile == 64 ? 2 : 1) * kCUs / (tiles > 0 ? tiles : 1);
   const int64_t best = (int64_t)sqrt(0.7 * (double)stages);
   const int64_t n = free < best ? free : best;
   return n < 1 ? 1 : (int)n;
+}
+
+int64_t below_diagonal(int64_t tm) { return tm * (tm + 1) / 2; }
+
+// The tiles of each product: the cheapest for a STEP, whose tile the sides are padded to, then for the others the
+// cheapest of those that divide it.
+void choose_tiles(Plan* p) {
+  const int most = p->split ? 128 : 256;
+  p->tile = p->gram_tile = p->poly_tile = 64;
+  if (p->m <= 64) return;  // A is one tile
+  auto padded = [](int64_t x, int t) { return ceil_div(x, t) * t; };
+  double best = 0.0;
+  for (int t = 64; t <= most; t *= 2) {
+    const int64_t M = padded(p->m, t), N = padded(p->n, t);
+    const double us = stage_us(t, p->split, p->batch * (M / t) * (N / t)) * (double)(M / kBK);
+    if (t == 64 || us < best) best = us, p->tile = t;
+  }
+  const int64_t M = padded(p->m, p->tile), N = padded(p->n, p->tile);
+  double best_gram = 0.0, best_poly = 0.0;
+  for (int t = 64; t <= p->tile; t *= 2) {
+    const int64_t tiles = p->batch * below_diagonal(M / t);
+    const int shares = shares_of(tiles, N / kBK, t);
+    // (a share is added up in 0.35 us with tiles of 64, in four times that with 128)
+    const double gram = stage_us(t, p->split, tiles * shares) * (double)(N / kBK) / shares +
+                        (shares > 1 ? 0.35 * shares * (t / 64) * (t / 64) : 0.0);
+    const double poly = stage_us(t, p->split, tiles) * (double)(M / kBK);
+    if (t == 64 || gram < best_gram) best_gram = gram, p->gram_tile = t;
+    if (t == 64 || poly < best_poly) best_poly = poly, p->poly_tile = t;
+  }
 }
 
 // Sizes are checked by the caller.
@@ -775,7 +812,7 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split) {
   // a short side of few rows has few roundings to average out (3.4e-3 measured at 1 x 7), and costs launches,
   // not products: always in pairs
   p.split = split || p.m <= 64;
-  p.tile = tile_of(p.m, p.n, batch, p.split);
+  choose_tiles(&p);
   p.Mp = ceil_div(p.m, p.tile) * p.tile;
   p.Np = ceil_div(p.n, p.tile) * p.tile;
   p.nparts = (int)(ceil_div(rows * cols, kNormElems) < kMaxParts ? ceil_div(rows * cols, kNormElems) : kMaxParts);
@@ -794,7 +831,7 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split) {
   p.xl = take(x);
   p.th[0] = take(x);
   p.th[1] = take(x);
-  const bool one = p.Mp == p.tile;  // A never leaves its block
+  const bool one = p.m <= 64;  // A never leaves its block
   if (!one) p.ah = take(a);
   p.bh = take(a);
   if (p.split) {
@@ -803,10 +840,10 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split) {
     if (!one) p.al = take(a);
     p.bl = take(a);
   }
-  const int64_t tm = p.Mp / p.tile, tiles = batch * (tm * (tm + 1) / 2);
-  p.shares = shares_of(tiles, p.Np / kBK, p.tile);
+  const int64_t tiles = batch * below_diagonal(p.Mp / p.gram_tile);
+  p.shares = shares_of(tiles, p.Np / kBK, p.gram_tile);
   if (p.shares > 1) {
-    p.gpart = take((size_t)(4 * tiles * p.shares * p.tile * p.tile));
+    p.gpart = take((size_t)(4 * tiles * p.shares * p.gram_tile * p.gram_tile));
     p.arrived = take((size_t)(4 * tiles));
     p.tiles = tiles;
   }
@@ -817,30 +854,35 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split) {
 template <int EPI, bool SPLIT>
 hipError_t launch_prod(const Plan& p, const ProdArgs& a, int64_t tiles, hipStream_t s) {
   const unsigned grid = (unsigned)(tiles * p.batch);
-  if constexpr (EPI == GRAM || EPI == BOTH) {
-    if (p.shares > 1) {
-      if (p.tile == 64)
-        k_prod<64, 32, 32, SPLIT, EPI, true><<<grid * p.shares, 256, 0, s>>>(a);
-      else if (SPLIT)
-        k_prod<128, 64, 32, true, EPI, true><<<grid * p.shares, 512, 0, s>>>(a);
-      else
-        k_prod<128, 64, 64, false, EPI, true><<<grid * p.shares, 256, 0, s>>>(a);
-      return hipGetLastError();
-    }
+  const int tile = EPI == GRAM || EPI == BOTH ? p.gram_tile : EPI == POLY ? p.poly_tile : p.tile;
+  if constexpr (EPI == BOTH) {
+    if (p.shares > 1)
+      k_prod<64, 32, 32, true, EPI, true><<<grid * p.shares, 256, 0, s>>>(a);
+    else
+      k_prod<64, 32, 32, true, EPI><<<grid, 256, 0, s>>>(a);
+  } else if (EPI == GRAM && p.shares > 1) {
+    if (tile == 64)
+      k_prod<64, 32, 32, SPLIT, EPI, EPI == GRAM><<<grid * p.shares, 256, 0, s>>>(a);
+    else if (SPLIT)
+      k_prod<128, 64, 32, true, EPI, EPI == GRAM><<<grid * p.shares, 512, 0, s>>>(a);
+    else
+      k_prod<128, 64, 64, false, EPI, EPI == GRAM><<<grid * p.shares, 256, 0, s>>>(a);
+  } else {
+    if (tile == 64)
+      k_prod<64, 32, 32, SPLIT, EPI><<<grid, 256, 0, s>>>(a);
+    else if (SPLIT)
+      k_prod<128, 64, 32, true, EPI><<<grid, 512, 0, s>>>(a);
+    else if (tile == 128)
+      k_prod<128, 64, 64, false, EPI><<<grid, 256, 0, s>>>(a);
+    else
+      k_prod<256, 128, 64, false, EPI><<<grid, 512, 0, s>>>(a);
   }
-  if (p.tile == 64)
-    k_prod<64, 32, 32, SPLIT, EPI><<<grid, 256, 0, s>>>(a);
-  else if (SPLIT)
-    k_prod<128, 64, 32, true, EPI><<<grid, 512, 0, s>>>(a);
-  else if (p.tile == 128)
-    k_prod<128, 64, 64, false, EPI><<<grid, 256, 0, s>>>(a);
-  else if constexpr (EPI != BOTH)
-    k_prod<256, 128, 64, false, EPI><<<grid, 512, 0, s>>>(a);
   return hipGetLastError();
 }
 
 template <int EPI>
 hipError_t launch_prod(const Plan& p, const ProdArgs& a, int64_t tiles, hipStream_t s) {
+  if constexpr (EPI == BOTH) return launch_prod<EPI, true>(p, a, tiles, s);
   return p.split ? launch_prod<EPI, true>(p, a, tiles, s) : launch_prod<EPI, false>(p, a, tiles, s);
 }
 
@@ -883,7 +925,7 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
   k_scale<<<dim3((unsigned)(cp / 64), (unsigned)(rp / 64), (unsigned)p.batch), kNormThreads, 0, s>>>(pa);
   if ((e = hipGetLastError()) != hipSuccess) return e;
 
-  const int64_t tm = p.Mp / p.tile, tn = p.Np / p.tile, sym = tm * (tm + 1) / 2;
+  const int64_t tm = p.Mp / p.tile, tn = p.Np / p.tile;
   for (int k = 0; k < o.steps; ++k) {
     ProdArgs g = last;
     g.a = o.coef[k][0];
@@ -907,23 +949,24 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
     x.pl = x.ql = half(p.xl);
     x.ldk = p.Np;
     x.pstride = x.qstride = p.Mp * p.Np;
-    x.tm = x.tn = (int32_t)tm;
+    x.tm = x.tn = (int32_t)(p.Mp / p.gram_tile);
     x.oh = half(p.ah);
     x.ol = p.split ? half(p.al) : nullptr;
     x.ostride = p.Mp * p.Mp;
-    if (tm == 1) {
+    if (p.m <= 64) {
       x.oh = half(p.bh);
       x.ol = p.split ? half(p.bl) : nullptr;
-      if ((e = launch_prod<BOTH>(p, x, sym, s)) != hipSuccess) return e;
+      if ((e = launch_prod<BOTH>(p, x, 1, s)) != hipSuccess) return e;
     } else {
-      if ((e = launch_prod<GRAM>(p, x, sym, s)) != hipSuccess) return e;
+      if ((e = launch_prod<GRAM>(p, x, below_diagonal(x.tm), s)) != hipSuccess) return e;
       x.ph = x.qh = x.ah = half(p.ah);  // B = b A + c A A
       x.pl = x.ql = x.al = p.split ? half(p.al) : nullptr;
       x.ldk = p.Mp;
       x.pstride = x.qstride = p.Mp * p.Mp;
       x.oh = half(p.bh);
       x.ol = p.split ? half(p.bl) : nullptr;
-      if ((e = launch_prod<POLY>(p, x, sym, s)) != hipSuccess) return e;
+      x.tm = x.tn = (int32_t)(p.Mp / p.poly_tile);
+      if ((e = launch_prod<POLY>(p, x, below_diagonal(x.tm), s)) != hipSuccess) return e;
     }
 
     const int from = k & 1;  // X^T <- X^T B: rows of the long side
