@@ -76,6 +76,10 @@ __global__ __launch_bounds__(kThreadsE) void k_lookup(LookupArgs a) {
 
 constexpr int kOwn = 16;   // sorted tokens of a wavefront of k_rows_sum
 constexpr int kRuns = 16;  // sorted runs of a merge
+// Up to so many tokens of a worker, the wavefront that an id begins in adds all its rows itself (kOwn at a time), and
+// there is no k_join: a launch less, 2.8 us of the 20 that 4 x 197 tokens take, against 16 rows after each other at
+// most.
+constexpr int64_t kAloneTokens = 256;
 
 struct GradArgs {
   const void* dy;
@@ -97,11 +101,12 @@ struct GradArgs {
   int32_t bits;             // of V
 };
 
-// Zeroes n floats at p with the blocks b of nb: whole 16-byte pieces, 64 KiB
-// of them at a time (5.6 TB/s; 4.7 when all blocks write side by side), and
-// what lies before the first and after the last one.
+// Zeroes n floats at p with the blocks b of nb: whole 16-byte pieces, four a
+// thread and adjacent in the block (64 KiB of 1,024 threads: 5.6 TB/s; 4.7
+// when all blocks write side by side), and what lies before the first and
+// after the last one.
 __device__ void fill_zero(float* p, int64_t n, int64_t b, int64_t nb) {
-  constexpr int64_t kPiece = 4096;
+  const int64_t kPiece = 4 * blockDim.x;
   const int64_t head = min((int64_t)((-(intptr_t)p) & 15) / 4, n);
   const int64_t n4 = (n - head) / 4, tail = n - head - 4 * n4;
   if (b == 0) {
@@ -300,7 +305,7 @@ __device__ __forceinline__ void add_to(float (&s)[N], const Near<D, N>& x) {
 
 // Sorted tokens [p0, p0 + kOwn).  Their rows are asked for at once: an id
 // does not wait for the one before it.
-template <typename D, int N, bool ADD>
+template <typename D, int N, bool ADD, bool ALONE>
 __global__ __launch_bounds__(64) void k_rows_sum(GradArgs a) {
   const int lane = threadIdx.x, w = blockIdx.z;
   const Columns c = columns_of<N>(a.d, lane);
@@ -318,6 +323,7 @@ __global__ __launch_bounds__(64) void k_rows_sum(GradArgs a) {
   const uint64_t begins = __ballot(lane < count && here != prev);
   const int end = __popcll(__ballot(lane < count && here < V));  // those of no row come last
   if (end == 0) return;
+  if (ALONE && !(begins & ((1ull << end) - 1))) return;
   const bool goes_on = end == kOwn && __builtin_amdgcn_readlane(here, kOwn) == __builtin_amdgcn_readlane(here, kOwn - 1);
   auto row_of = [&](int i) {
     const uint32_t id = (uint32_t)__builtin_amdgcn_readlane(here, min(i, end - 1));
@@ -342,11 +348,28 @@ __global__ __launch_bounds__(64) void k_rows_sum(GradArgs a) {
     const bool last = i == end - 1;
     if (!last && !(begins >> (i + 1) & 1)) continue;
     Near<float, N> v;
-    if (whole && !(last && goes_on)) {
+    if (ALONE && whole && last && goes_on) {
+      const uint32_t id = __builtin_amdgcn_readlane(here, kOwn);
+      for (int64_t p = p0 + kOwn;;) {
+        const int n = __popcll(__ballot(lane < kOwn && p + lane < a.T && key[min(p + lane, a.T - 1)] == id));
+        if (n == 0) break;
+        const uint32_t more = a.order[(int64_t)w * a.T + min(p + lane, a.T - 1)];
+        Near<D, N> y[kOwn];
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k)
+          y[k] = load_row<D, N>(dy + (int64_t)(uint32_t)__builtin_amdgcn_readlane(more, min(k, n - 1)) * a.dy_ld, c);
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k)
+          if (k < n) add_to(s, y[k]);
+        p += n;
+        if (n < kOwn) break;
+      }
+    }
+    if (whole && (ALONE || !(last && goes_on))) {
 #pragma unroll
       for (int e = 0; e < N; ++e) v.v[e] = s[e] * a.scale + (ADD ? old[ADD ? i : 0].v[e] : 0.0f);
       if (c.mine) *row_of(i) = v;
-    } else {
+    } else if (!ALONE) {
 #pragma unroll
       for (int e = 0; e < N; ++e) v.v[e] = s[e];
       float* part = a.part + (((int64_t)w * gridDim.x + blockIdx.x) * 2 + whole) * a.d;
@@ -466,7 +489,7 @@ GradPlan plan_of(int32_t W, int64_t T, int64_t d) {
     p.key[1] = take(n);
     p.order[1] = take(n);
   }
-  p.part = take((size_t)W * (size_t)ceil_div(T, kOwn) * (size_t)d * 8);
+  if (T > kAloneTokens) p.part = take((size_t)W * (size_t)ceil_div(T, kOwn) * (size_t)d * 8);
   p.total = at;
   return p;
 }
@@ -491,8 +514,12 @@ const char* check_grad_sizes(int32_t W, int64_t T, int64_t V, int64_t d) {
 template <typename D, int N, bool ADD>
 void launch_sums(const GradArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)ceil_div(a.T, kOwn), (unsigned)ceil_div(a.d, 64 * N), (unsigned)a.W);
-  k_rows_sum<D, N, ADD><<<grid, 64, 0, s>>>(a);
-  if (grid.x > 1) k_join<N, ADD><<<dim3((grid.x + 3) / 4, grid.y, grid.z), kThreadsE, 0, s>>>(a);
+  if (a.T <= kAloneTokens) {
+    k_rows_sum<D, N, ADD, true><<<grid, 64, 0, s>>>(a);
+    return;
+  }
+  k_rows_sum<D, N, ADD, false><<<grid, 64, 0, s>>>(a);
+  k_join<N, ADD><<<dim3((grid.x + 3) / 4, grid.y, grid.z), kThreadsE, 0, s>>>(a);
 }
 
 template <typename D, int N>
@@ -503,16 +530,16 @@ void launch_sums(const GradArgs& a, hipStream_t s) {
     launch_sums<D, N, false>(a, s);
 }
 
-// Blocks that zero a worker's segment: 64 KiB each at least, 4,096 in all at most.
-int64_t fill_blocks(const GradArgs& a) {
+// Blocks that zero a worker's segment: a piece each at least, 4,096 in all at most.
+int64_t fill_blocks(const GradArgs& a, int threads) {
   if (a.accumulate) return 0;
-  const int64_t want = ceil_div(a.V * a.d * 4, 65536), most = 4096 / a.W;
+  const int64_t want = ceil_div(a.V * a.d, 16 * threads), most = 4096 / a.W;
   return want < most ? want : most;
 }
 
 template <int THREADS, int ITEMS>
 void launch_sort(const GradArgs& a, hipStream_t s) {
-  const int64_t blocks = (int64_t)a.W * (a.tiles + fill_blocks(a));
+  const int64_t blocks = (int64_t)a.W * (a.tiles + fill_blocks(a, THREADS));
   if (blocks) k_sort<THREADS, ITEMS><<<(unsigned)blocks, THREADS, 0, s>>>(a);
 }
 

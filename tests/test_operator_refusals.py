@@ -66,7 +66,10 @@ def test_orthogonal():
     how = nf.orthogonal()
     ref = ctypes.byref(how)
     need = nf.nf_orthogonal_workspace_bytes(40, 30, 2, how)
-    assert need > 0 and nf.nf_orthogonal_workspace_bytes(40, 30, 2, nf.orthogonal(products=nf.NF_PRODUCTS_SPLIT)) > need
+    assert need > 0
+    split = nf.orthogonal(products=nf.NF_PRODUCTS_SPLIT)  # (a short side of at most 64 always takes these products)
+    assert nf.nf_orthogonal_workspace_bytes(40, 30, 2, split) == need
+    assert nf.nf_orthogonal_workspace_bytes(300, 200, 2, split) > nf.nf_orthogonal_workspace_bytes(300, 200, 2, how) > 0
 
     def params(**kw):
         p = nf.orthogonal()
