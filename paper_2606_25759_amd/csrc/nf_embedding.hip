@@ -40,14 +40,10 @@ __device__ __forceinline__ int64_t id_at(const void* ids, int32_t ids64, int64_t
   return ids64 ? ((const int64_t*)ids)[i] : (int64_t)((const int32_t*)ids)[i];
 }
 
-template <typename T, int N>
-struct alignas(sizeof(T) * N <= 16 ? sizeof(T) * N : 16) Pack {
-  T v[N];
-};
-
 constexpr int kThreadsE = 256;
 
-// N = 8: rows and bases aligned for 16-byte (FP32: two 16-byte) accesses.
+// Eight elements of a row a thread (one where rows have fewer), the last ones
+// of a row where they are: the thread before may have some of them too.
 template <typename A, typename B, int N>
 __global__ __launch_bounds__(kThreadsE) void k_lookup(LookupArgs a) {
   const int tx = 1 << a.lg_tx, ty = kThreadsE >> a.lg_tx;
@@ -59,16 +55,17 @@ __global__ __launch_bounds__(kThreadsE) void k_lookup(LookupArgs a) {
   const A* row = (const A*)a.table + (in ? id : 0) * a.table_ld;
   B* out = (B*)a.out + t * a.out_ld;
   for (int j = x * N; j < a.d; j += tx * N) {
-    Pack<B, N> o;
+    const int at = min(j, a.d - N);
+    Near<B, N> o;
     if (in) {
-      const Pack<A, N> p = *(const Pack<A, N>*)(row + j);
+      const Near<A, N> p = *(const Near<A, N>*)(row + at);
 #pragma unroll
       for (int e = 0; e < N; ++e) o.v[e] = from_f32<B>(to_f32(p.v[e]) * a.scale);
     } else {
 #pragma unroll
       for (int e = 0; e < N; ++e) o.v[e] = from_f32<B>(0.0f);
     }
-    *(Pack<B, N>*)(out + j) = o;
+    *(Near<B, N>*)(out + at) = o;
   }
 }
 
@@ -270,15 +267,8 @@ __global__ __launch_bounds__(kThreadsE) void k_merge(GradArgs a) {
 
 // ---------------------------------------------------------------- the sums
 
-// A lane's N adjacent columns of a row (four; one where rows have fewer than
-// four), at any element's address: the card reads and writes across
-// alignment.
-template <typename T, int N>
-struct __attribute__((packed)) Near {
-  T v[N];
-};
-
-// A block's columns are an even share of a row's, in whole lanes; the last
+// A block's columns are an even share of a row's, N adjacent ones a lane (four;
+// one where rows have fewer than four); the last
 // lane that has any takes the last N (its neighbour may have some of them
 // too, and comes to the same values), so that no access needs a condition.
 struct Columns {
@@ -561,16 +551,15 @@ nf_status nf_embedding_lookup(const void* table, int32_t table_type, int64_t tab
   if ((uintptr_t)table % type_bytes(table_type) || (uintptr_t)out % type_bytes(out_type) || (uintptr_t)ids % ids_bytes)
     return set_error(NF_ERR_ALIGNMENT, "table, ids or out not aligned to its elements");
   LookupArgs a = {table, ids, out, table_ld, out_ld, V, T, (int32_t)d, ids_bytes == 8, scale, 0};
-  auto wide = [&](const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 8 == 0; };
-  const bool vec = d % 8 == 0 && wide(table, table_ld) && wide(out, out_ld);
-  while (a.lg_tx < 8 && (1 << a.lg_tx) * (vec ? 8 : 1) < d) ++a.lg_tx;
+  const int each = d < 8 ? 1 : 8;
+  while (a.lg_tx < 8 && (each << a.lg_tx) < d) ++a.lg_tx;
   const unsigned blocks = (unsigned)ceil_div(T, kThreadsE >> a.lg_tx);
   hipStream_t s = static_cast<hipStream_t>(stream);
   with_type(table_type, [&](auto* tp) {
     with_type(out_type, [&](auto* op) {
       using A = std::remove_pointer_t<decltype(tp)>;
       using B = std::remove_pointer_t<decltype(op)>;
-      if (vec)
+      if (each == 8)
         k_lookup<A, B, 8><<<blocks, kThreadsE, 0, s>>>(a);
       else
         k_lookup<A, B, 1><<<blocks, kThreadsE, 0, s>>>(a);

@@ -80,7 +80,6 @@ struct PrepArgs {
   double* part;        // [batch][nparts]
   int32_t nparts;
   int32_t lg_tx;       // k_norm: log2 of the threads across a row, four elements each
-  int32_t vec;         // four adjacent elements are aligned to their size
   float eps;
   _Float16 *xh, *xl, *th, *tl;  // tl: split only
   int32_t* arrived;    // to be zeroed
@@ -105,24 +104,18 @@ struct ProdArgs {
   int32_t tall;
   int32_t update;                     // 1: dst holds weights
   float keep, rate;                   // w = keep w - rate o
-  int32_t vec;                        // dst takes 16-byte accesses
   int32_t shares;                     // GRAM: blocks that share a tile's k
   uint64_t* part;                     // their sums, [tile][share][BT x BT], two FP32 a word
   int32_t* arrived;                   // [tile], zero between launches
 };
 
+// Elements c .. c + 3 of n of a row, the first at p + off; zeros past the row's end.
 template <typename T>
-struct alignas(4 * sizeof(T)) Four {
-  T v[4];
-};
-
-// Elements c .. c + 3 of n of a row at p + off; zeros past the row's end.
-template <typename T>
-__device__ __forceinline__ float4v load_four(const void* p, int64_t off, int64_t c, int64_t n, bool vec) {
+__device__ __forceinline__ float4v load_four(const void* p, int64_t off, int64_t c, int64_t n) {
   const T* q = (const T*)p + off;
   float4v v = {};
-  if (vec && c + 3 < n) {
-    const Four<T> w = *(const Four<T>*)q;
+  if (c + 3 < n) {
+    const Near<T, 4> w = *(const Near<T, 4>*)q;
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = to_f32(w.v[e]);
   } else {
@@ -133,10 +126,10 @@ __device__ __forceinline__ float4v load_four(const void* p, int64_t off, int64_t
   return v;
 }
 
-__device__ __forceinline__ float4v load_four(const View& g, int64_t off, int64_t c, int64_t n, bool vec) {
-  if (g.type == NF_TYPE_F32) return load_four<float>(g.p, off, c, n, vec);
-  if (g.type == NF_TYPE_BF16) return load_four<Bf16>(g.p, off, c, n, vec);
-  return load_four<_Float16>(g.p, off, c, n, vec);
+__device__ __forceinline__ float4v load_four(const View& g, int64_t off, int64_t c, int64_t n) {
+  if (g.type == NF_TYPE_F32) return load_four<float>(g.p, off, c, n);
+  if (g.type == NF_TYPE_BF16) return load_four<Bf16>(g.p, off, c, n);
+  return load_four<_Float16>(g.p, off, c, n);
 }
 
 // Where (row, k) of a matrix of R rows lies.
@@ -148,10 +141,10 @@ __device__ __forceinline__ int64_t panel_at(int64_t row, int64_t k, int64_t R) {
 __device__ __forceinline__ float4v value_of(const PrepArgs& a, int64_t b, int64_t r, int64_t c) {
   float4v m = {};
   if (a.mom) {
-    m = load_four<float>(a.mom, b * a.mom_stride + r * a.mom_ld + c, c, a.cols, a.vec);
+    m = load_four<float>(a.mom, b * a.mom_stride + r * a.mom_ld + c, c, a.cols);
     if (!a.nesterov) return m;
   }
-  float4v u = load_four(a.g, b * a.g.stride + r * a.g.ld + c, c, a.cols, a.vec);
+  float4v u = load_four(a.g, b * a.g.stride + r * a.g.ld + c, c, a.cols);
   if (a.mom)
 #pragma unroll
     for (int e = 0; e < 4; ++e) u[e] = fmaf(a.mu, m[e], u[e]);
@@ -181,14 +174,14 @@ __global__ __launch_bounds__(kNormThreads) void k_norm(PrepArgs a) {
   double sum = 0.0;
   for (int64_t r = (int64_t)blockIdx.x * ty + y; r < a.rows; r += (int64_t)gridDim.x * ty) {
     for (int64_t c = 4 * x; c < a.cols; c += 4 * tx) {
-      float4v u = load_four(a.g, b * a.g.stride + r * a.g.ld + c, c, a.cols, a.vec);
+      float4v u = load_four(a.g, b * a.g.stride + r * a.g.ld + c, c, a.cols);
       if (a.mom) {
         const int64_t off = b * a.mom_stride + r * a.mom_ld + c;
-        float4v m = load_four<float>(a.mom, off, c, a.cols, a.vec);
+        float4v m = load_four<float>(a.mom, off, c, a.cols);
 #pragma unroll
         for (int e = 0; e < 4; ++e) m[e] = fmaf(a.mu, m[e], u[e]);
-        if (a.vec && c + 3 < a.cols) {
-          *(float4v*)(a.mom + off) = m;
+        if (c + 3 < a.cols) {
+          *(Near<float, 4>*)(a.mom + off) = Near<float, 4>{{m[0], m[1], m[2], m[3]}};
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -366,22 +359,17 @@ __device__ __forceinline__ half8 transpose8(half8 c0, half8 c1, int x, int lane)
   return half8{p[0], p[1], p[2], p[3], q[0], q[1], q[2], q[3]};
 }
 
-template <typename T>
-struct alignas(16) Eight {
-  T v[8];
-};
-
 // Eight results of one row of the caller's matrix, columns c .. c + 7 of n.
 template <typename T>
 __device__ __forceinline__ void store_eight(const ProdArgs& a, int64_t off, int64_t c, int64_t n, const float (&o)[8]) {
   T* p = (T*)a.dst.p + off;
-  if (a.vec && c + 7 < n) {
-    Eight<T> w;
-    if (a.update) w = *(const Eight<T>*)p;
+  if (c + 7 < n) {
+    Near<T, 8> w;
+    if (a.update) w = *(const Near<T, 8>*)p;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       w.v[e] = from_f32<T>(a.update ? fmaf(a.keep, to_f32(w.v[e]), -a.rate * o[e]) : o[e]);
-    *(Eight<T>*)p = w;
+    *(Near<T, 8>*)p = w;
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
@@ -469,6 +457,38 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
   }
   const int wm = wave / (BT / WN) * WM, wn = wave % (BT / WN) * WN;
   float4v acc[MI][NJ] = {};
+
+  // What the epilogue reads: of small tiles asked for now, before the products, else when it is needed.
+  constexpr bool EARLY = BT == 64;
+  constexpr int CI = MI / 2, CJ = NJ;  // eight rows of a column each
+  half8 inh[EARLY ? CI : 1][EARLY ? CJ : 1], inl[EARLY ? CI : 1][EARLY ? CJ : 1];
+  float dcol[EARLY ? CJ : 1];
+  float4v drow[EARLY ? CI : 1][2];
+  auto row_at = [&](int i) { return (int64_t)ti * BT + wm + 16 * i + lane / 16 * 8; };
+  auto column_at = [&](int j) { return (int64_t)tj * BT + wn + j / 2 * 32 + j % 2 * 4 + lane % 16 / 4 * 8 + lane % 4; };
+  auto ask = [&](int i, int j, half8& h, half8& l, float& dc, float4v (&dr)[2]) {  // i even
+    const int64_t r = row_at(i), c = column_at(j);
+    l = half8{};
+    if (EPI == POLY) {
+      const int64_t at = b * a.ostride + panel_at(c, r, a.Mp);
+      h = *(const half8*)(a.ah + at);
+      if (SPLIT) l = *(const half8*)(a.al + at);
+      dc = a.dA[b * a.Mp + c];
+      dr[0] = *(const float4v*)(a.dA + b * a.Mp + r);
+      dr[1] = *(const float4v*)(a.dA + b * a.Mp + r + 4);
+    } else if (EPI == STEP || EPI == LAST) {
+      const int64_t at = b * a.Mp * a.Np + panel_at(c, r, a.Mp);
+      h = *(const half8*)(a.xh + at);
+      l = *(const half8*)(a.xl + at);
+      dc = a.dB[b * a.Mp + c];
+    }
+  };
+  if constexpr (EARLY && (EPI == POLY || EPI == STEP || EPI == LAST)) {
+#pragma unroll
+    for (int i = 0; i < CI; ++i)
+#pragma unroll
+      for (int j = 0; j < CJ; ++j) ask(2 * i, j, inh[i][j], inl[i][j], dcol[j], drow[i]);
+  }
 
   // stages [first, first + stages), an even number of them
   int first = 0, stages = (int)(a.ldk / kBK);
@@ -646,13 +666,12 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
   for (int i = 0; i < MI; i += 2) {
 #pragma unroll
     for (int j = 0; j < NJ; j += 2) {
-      const int64_t r = (int64_t)ti * BT + wm + 16 * i + lane / 16 * 8;
-      const int64_t cq = (int64_t)tj * BT + wn + 16 * j + lane % 16 / 4 * 8;
-      const int64_t rq = r + lane % 4;
+      const int64_t r = row_at(i), rq = r + lane % 4;
+      const int64_t cq = column_at(j) - lane % 4;
       float v[2][8];  // [column][row]
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        const int64_t c = cq + 4 * y + lane % 4;
+        const int64_t c = column_at(j + y);
         float d[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) d[e] = acc[i + e / 4][j + y][e % 4];
@@ -665,33 +684,44 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
               v[y][e] = 0.0f;
             }
           }
-        } else if (EPI == POLY || EPI == BOTH) {
-          const int64_t at = b * a.ostride + panel_at(c, r, a.Mp);
-          half8 oh = {}, ol = {};
-          if (EPI == POLY) oh = *(const half8*)(a.ah + at);
-          if (EPI == POLY && SPLIT) ol = *(const half8*)(a.al + at);
-          const float* dA = EPI == BOTH ? diagonal : a.dA + b * a.Mp;
-          const float dc = dA[c];
+          continue;
+        }
+        half8 h = {}, l = {};
+        float dc = 0.0f;
+        float4v dr[2] = {};
+        if constexpr (EPI != GRAM && EPI != BOTH) {
+          if constexpr (EARLY) {
+            h = inh[i / 2][j + y];
+            l = inl[i / 2][j + y];
+            dc = dcol[j + y];
+            dr[0] = drow[i / 2][0];
+            dr[1] = drow[i / 2][1];
+          } else {
+            ask(i, j + y, h, l, dc, dr);
+          }
+        }
+        if (EPI == POLY || EPI == BOTH) {
+          if (EPI == BOTH) {
+            dc = diagonal[EPI == BOTH ? c : 0];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dr[e / 4][e % 4] = diagonal[EPI == BOTH ? r + e : 0];
+          }
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float dr = dA[r + e];
             const float o = EPI == BOTH ? whole[EPI == BOTH ? i + e / 4 : 0][EPI == BOTH ? j + y : 0][e % 4]
-                                        : (float)oh[e] + (float)ol[e];
+                                        : (float)h[e] + (float)l[e];
             // (D + O)^2 = D^2 + D O + O D + O O
-            v[y][e] = fmaf(a.c, fmaf(dr + dc, o, d[e] * kInvScale), a.b * o);
+            v[y][e] = fmaf(a.c, fmaf(dr[e / 4][e % 4] + dc, o, d[e] * kInvScale), a.b * o);
             if (r + e == c) {
               a.dB[b * a.Mp + c] = fmaf(a.c, fmaf(dc, dc, d[e] * kInvScale * kInvScale), a.b * dc);
               v[y][e] = 0.0f;
             }
           }
         } else {  // rows are the long side, columns the short one
-          const int64_t at = b * a.Mp * a.Np + panel_at(c, r, a.Mp);
-          const half8 xh = *(const half8*)(a.xh + at), xl = *(const half8*)(a.xl + at);
-          const float q = a.dB[b * a.Mp + c];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float h = (float)xh[e], x = h + (float)xl[e];
-            v[y][e] = fmaf(a.a, x, fmaf(q, SPLIT || EPI == LAST ? x : h, d[e] * kInvScale));
+            const float hi = (float)h[e], x = hi + (float)l[e];
+            v[y][e] = fmaf(a.a, x, fmaf(dc, SPLIT || EPI == LAST ? x : hi, d[e] * kInvScale));
           }
         }
       }
@@ -886,20 +916,7 @@ hipError_t launch_prod(const Plan& p, const ProdArgs& a, int64_t tiles, hipStrea
   return p.split ? launch_prod<EPI, true>(p, a, tiles, s) : launch_prod<EPI, false>(p, a, tiles, s);
 }
 
-bool by_fours(const View& v, int64_t batch) {
-  return (uintptr_t)v.p % (4 * type_bytes(v.type)) == 0 && v.ld % 4 == 0 && (batch == 1 || v.stride % 4 == 0);
-}
-
-// Whether eight adjacent elements, at every eighth column, are aligned for 16-byte accesses.
-bool by_eights(const View& v, int64_t batch) {
-  const int64_t unit = 16 / (int64_t)type_bytes(v.type);
-  return (uintptr_t)v.p % 16 == 0 && v.ld % unit == 0 && (batch == 1 || v.stride % unit == 0);
-}
-
 hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_params& o, void* ws, hipStream_t s) {
-  pa.vec = by_fours(pa.g, p.batch) &&
-           (!pa.mom || by_fours(View{pa.mom, pa.mom_ld, pa.mom_stride, NF_TYPE_F32}, p.batch));
-  last.vec = by_eights(last.dst, p.batch);
   unsigned char* w = static_cast<unsigned char*>(ws);
   auto half = [&](size_t at) { return reinterpret_cast<_Float16*>(w + at); };
   pa.rows = p.rows;

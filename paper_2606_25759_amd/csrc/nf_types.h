@@ -37,6 +37,13 @@ __device__ __forceinline__ Bf16 from_f32<Bf16>(float x) {
   return __builtin_bit_cast(Bf16, (__bf16)x);
 }
 
+// N adjacent elements at any element's address: the card reads and writes
+// whole registers across alignment.
+template <typename T, int N>
+struct __attribute__((packed)) Near {
+  T v[N];
+};
+
 // Calls f with a null pointer of the type's element.
 template <typename F>
 inline void with_type(int32_t t, F f) {
