@@ -8,8 +8,8 @@
 //   k_prod     one product P Q^T on the matrix cores with an epilogue:
 //                GRAM  A = X X^T
 //                POLY  B = b A + c A A
-//                BOTH  GRAM and POLY where A is one tile (a short side of at
-//                      most 64): a launch less a step
+//                BOTH  A and the product of a few steps' polynomials of it,
+//                      where A is one tile (a short side of at most 64)
 //                STEP  X = a X + B X
 //                LAST  the same, into the caller's matrix or weights
 //
@@ -37,6 +37,7 @@
 //   - B's diagonal multiplies the same rounded X as the rest of B does,
 //     except in the last step, after which nothing is amplified any more.
 #include <math.h>
+#include <string.h>
 
 #include <type_traits>
 
@@ -58,6 +59,7 @@ constexpr int kStages = 4;                // LDS stages of k_prod
 constexpr int kNormThreads = 256;
 constexpr int kNormElems = 4096;          // elements of a norm partial, at least
 constexpr int kMaxParts = 1024;           // of a matrix
+constexpr int kBlock = 3;                 // steps that BOTH takes at once, at most
 
 enum { GRAM, POLY, STEP, LAST, BOTH };
 
@@ -92,6 +94,8 @@ struct ProdArgs {
   int64_t pstride, qstride;           // a matrix of the batch
   int32_t tm, tn;                     // tiles
   float a, b, c;
+  int32_t steps;                      // BOTH: at most kBlock of them
+  float coef[kBlock][3];
   _Float16 *oh, *ol;                  // GRAM: A, POLY: B; STEP: X^T
   int64_t ostride;
   const _Float16 *ah, *al;            // POLY: A
@@ -622,42 +626,126 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
     }
   }
 
-  // BOTH: A times the scale in FP32, its diagonal apart; its FP16 matrix stays in LDS, panel by panel, for A A
-  float4v whole[EPI == BOTH ? MI : 1][EPI == BOTH ? NJ : 1];
-  __shared__ float diagonal[EPI == BOTH ? BT : 1];
+  // BOTH: the steps of A = X X^T in LDS.  With q(A) = a + b A + c A A a step is X <- q(A) X, so A <- q(A) A q(A), and
+  // after some steps X <- P X with P the product of the q(A): all are polynomials of the first A, symmetric and
+  // commuting.  P is formed here, and X read and written once for all of them.  A place in LDS holds a matrix as
+  // operands (two panels, both halves, zero diagonal, times the scale) and its diagonal in FP32; of what a product
+  // gives, the lower triangle is kept and mirrored (left unsymmetric, the rounding grows from step to step).
+  __shared__ float diagonal[EPI == BOTH ? 4 : 1][EPI == BOTH ? BT : 1];
   if constexpr (EPI == BOTH) {
-    static_assert(BT / kBK <= kStages, "a panel takes the place of a stage");
-    __syncthreads();  // the stages are read
+    static_assert(BT == 64 && SPLIT && kStages == 4, "a matrix takes the place of a stage");
+    enum { kA, kZ, kP, kR };
+    auto place = [&](int m, int half, int c, int r) {  // rows r .. r + 7 of column c
+      return &lds[m][2 * half + r / kBK][c * kBK + ((r % kBK / 8) ^ swizzle(c)) * 8];
+    };
+    auto put = [&](int m) {  // acc, which holds the matrix times the scale
 #pragma unroll
-    for (int i = 0; i < MI; i += 2) {
+      for (int j = 0; j < NJ; j += 2) {
+        const int r = (int)row_at(0), cq = (int)column_at(j) - lane % 4;
+        half8 h[2], l[2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const int c = (int)column_at(j + y);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            float v = acc[e / 4][j + y][e % 4];
+            if (r + e == c) {
+              diagonal[m][c] = v;
+              v = 0.0f;
+            }
+            h[y][e] = (_Float16)v;
+            l[y][e] = (_Float16)(v - (float)h[y][e]);
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const half8 th = transpose8(h[0], h[1], x, lane), tl = transpose8(l[0], l[1], x, lane);
+          const int c = cq + 4 * x + lane % 4;  // of this lane, and, where r = cq, the row that th is of
+          if (r > cq) {
+            *(half8*)place(m, 0, c, r) = h[x];
+            *(half8*)place(m, 1, c, r) = l[x];
+            *(half8*)place(m, 0, r + 4 * x + lane % 4, cq) = th;
+            *(half8*)place(m, 1, r + 4 * x + lane % 4, cq) = tl;
+          } else if (r == cq) {
+            half8 sh, sl;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              sh[e] = r + e >= c ? h[x][e] : th[e];
+              sl[e] = r + e >= c ? l[x][e] : tl[e];
+            }
+            *(half8*)place(m, 0, c, r) = sh;
+            *(half8*)place(m, 1, c, r) = sl;
+          }
+        }
+      }
+    };
+    // acc = alpha Y + beta Z Y:  (D + O)(D' + O') = D D' + D O' + O D' + O O'
+    auto combine = [&](int z, int y, float alpha, float beta) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[0][j] = acc[1][j] = float4v{};
+#pragma unroll
+      for (int s = 0; s < BT / kBK; ++s) {
+        read_from(lds[z][s], lds[y][s], lds[z][2 + s], lds[y][2 + s], f0);
+        multiply(f0);
+      }
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        const int r = wm + 16 * i + lane / 16 * 8;
-        const int c = wn + j / 2 * 32 + lane % 16 / 4 * 8 + j % 2 * 4 + lane % 4;
-        half8 h, l;
+        const int r = (int)row_at(0), c = (int)column_at(j);
+        const half8 zh = *(const half8*)place(z, 0, c, r), zl = *(const half8*)place(z, 1, c, r);
+        const half8 yh = *(const half8*)place(y, 0, c, r), yl = *(const half8*)place(y, 1, c, r);
+        const float dy = diagonal[y][c];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          float v = acc[i + e / 4][j][e % 4] * kInvScale;
-          if (r + e == c) {
-            diagonal[c] = v * kInvScale;
-            v = 0.0f;
-          }
-          whole[i + e / 4][j][e % 4] = v;
-          h[e] = (_Float16)v;
-          l[e] = (_Float16)(v - (float)h[e]);
+          const float dz = diagonal[z][r + e];
+          const float oz = (float)zh[e] + (float)zl[e], oy = (float)yh[e] + (float)yl[e];
+          float v = fmaf(dz, oy, fmaf(oz, dy, acc[e / 4][j][e % 4]));
+          if (r + e == c) v = fmaf(dz, dy, v);
+          acc[e / 4][j][e % 4] = fmaf(beta * kInvScale, v, alpha * (r + e == c ? dy : oy));
         }
-        const int at = c * kBK + ((r % kBK / 8) ^ swizzle(c)) * 8;
-        *(half8*)(lds[r / kBK][0] + at) = h;
-        if constexpr (SPLIT) *(half8*)(lds[r / kBK][2] + at) = l;
-        acc[i][j] = acc[i + 1][j] = float4v{};
       }
-    }
-    __syncthreads();
+    };
 #pragma unroll
-    for (int s = 0; s < BT / kBK; ++s) {
-      read_from(lds[s][0], lds[s][0], SPLIT ? lds[s][2 % OPS] : nullptr, SPLIT ? lds[s][2 % OPS] : nullptr, f0);
-      multiply(f0);
+    for (int i = 0; i < MI * NJ; ++i) acc[i / NJ][i % NJ] *= kInvScale;
+    __syncthreads();  // the stages are read
+    put(kA);
+    __syncthreads();
+    for (int k = 0; k < a.steps; ++k) {
+      combine(kA, kA, a.coef[k][1], a.coef[k][2]);  // Z = b A + c A A, q(A) = a + Z
+      put(kZ);
+      if (k == 0) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (row_at(0) + e == column_at(j)) acc[e / 4][j][e % 4] += a.coef[0][0] * kScale;
+        put(kP);
+      }
+      __syncthreads();
+      if (k) {
+        combine(kZ, kP, a.coef[k][0], 1.0f);
+        __syncthreads();  // P is read
+        put(kP);
+      }
+      if (k + 1 < a.steps) {
+        combine(kZ, kA, a.coef[k][0], 1.0f);
+        put(kR);
+        __syncthreads();
+        combine(kZ, kR, a.coef[k][0], 1.0f);
+        put(kA);  // (read by the product before the barrier, not by this one)
+      }
+      __syncthreads();
     }
+    // P's columns, to go where B goes
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int r = (int)row_at(0), c = (int)column_at(j);
+      const half8 h = *(const half8*)place(kP, 0, c, r), l = *(const half8*)place(kP, 1, c, r);
+      const int64_t at = b * a.ostride + panel_at(c, r, a.Mp);
+      *(half8*)(a.oh + at) = h;
+      *(half8*)(a.ol + at) = l;
+      if (r <= c && c < r + 8) a.dB[b * a.Mp + c] = diagonal[kP][c] * kInvScale;
+    }
+    return;
   }
 
   // Two pairs of fragments at a time: rows r .. r + 7 of columns c and c + 4; transposed, rows rq and rq + 4 of
@@ -689,7 +777,7 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
         half8 h = {}, l = {};
         float dc = 0.0f;
         float4v dr[2] = {};
-        if constexpr (EPI != GRAM && EPI != BOTH) {
+        if constexpr (EPI != GRAM) {
           if constexpr (EARLY) {
             h = inh[i / 2][j + y];
             l = inl[i / 2][j + y];
@@ -700,16 +788,10 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
             ask(i, j + y, h, l, dc, dr);
           }
         }
-        if (EPI == POLY || EPI == BOTH) {
-          if (EPI == BOTH) {
-            dc = diagonal[EPI == BOTH ? c : 0];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) dr[e / 4][e % 4] = diagonal[EPI == BOTH ? r + e : 0];
-          }
+        if (EPI == POLY) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float o = EPI == BOTH ? whole[EPI == BOTH ? i + e / 4 : 0][EPI == BOTH ? j + y : 0][e % 4]
-                                        : (float)h[e] + (float)l[e];
+            const float o = (float)h[e] + (float)l[e];
             // (D + O)^2 = D^2 + D O + O D + O O
             v[y][e] = fmaf(a.c, fmaf(dr[e / 4][e % 4] + dc, o, d[e] * kInvScale), a.b * o);
             if (r + e == c) {
@@ -916,7 +998,28 @@ hipError_t launch_prod(const Plan& p, const ProdArgs& a, int64_t tiles, hipStrea
   return p.split ? launch_prod<EPI, true>(p, a, tiles, s) : launch_prod<EPI, false>(p, a, tiles, s);
 }
 
-hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_params& o, void* ws, hipStream_t s) {
+// Steps from the k-th on that BOTH takes at once.  What grows a small singular value grows the rounding of A, P and
+// P X as well: as far as P stays within 48 (three steps of 3.4445, and FP16's range).  The error is then up to 6e-6
+// (4e-6 step by step), which only a result in FP32 from split products shows: that one goes step by step.
+int block_of(const nf_orthogonal_params& o, int k, bool coarse) {
+  double growth = 1.0;
+  int n = 0;
+  for (; n < kBlock && k + n < o.steps; ++n) {
+    const float* c = o.coef[k + n];
+    double most = 0.0;
+    for (int i = 0; i <= 24; ++i) {  // |q| over the squares of singular values up to 1.2
+      const double x = i * 0.06;
+      most = fmax(most, fabs(c[0] + x * (c[1] + x * c[2])));
+    }
+    growth *= fmax(most, 1.0);
+    if (n > 0 && (!coarse || growth > 48.0)) break;
+  }
+  return n;
+}
+
+// coarse: the result need not be closer than about 1e-5.
+hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_params& o, bool coarse, void* ws,
+               hipStream_t s) {
   unsigned char* w = static_cast<unsigned char*>(ws);
   auto half = [&](size_t at) { return reinterpret_cast<_Float16*>(w + at); };
   pa.rows = p.rows;
@@ -943,7 +1046,7 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
   if ((e = hipGetLastError()) != hipSuccess) return e;
 
   const int64_t tm = p.Mp / p.tile, tn = p.Np / p.tile;
-  for (int k = 0; k < o.steps; ++k) {
+  for (int k = 0, turn = 0, taken = 1; k < o.steps; k += taken, ++turn) {
     ProdArgs g = last;
     g.a = o.coef[k][0];
     g.b = o.coef[k][1];
@@ -971,9 +1074,13 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
     x.ol = p.split ? half(p.al) : nullptr;
     x.ostride = p.Mp * p.Mp;
     if (p.m <= 64) {
+      taken = block_of(o, k, coarse);
+      x.steps = taken;
+      memcpy(x.coef, o.coef[k], sizeof(float) * 3 * taken);
       x.oh = half(p.bh);
-      x.ol = p.split ? half(p.bl) : nullptr;
+      x.ol = half(p.bl);
       if ((e = launch_prod<BOTH>(p, x, 1, s)) != hipSuccess) return e;
+      g.a = 0.0f;  // P holds it
     } else {
       if ((e = launch_prod<GRAM>(p, x, below_diagonal(x.tm), s)) != hipSuccess) return e;
       x.ph = x.qh = x.ah = half(p.ah);  // B = b A + c A A
@@ -986,7 +1093,7 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
       if ((e = launch_prod<POLY>(p, x, below_diagonal(x.tm), s)) != hipSuccess) return e;
     }
 
-    const int from = k & 1;  // X^T <- X^T B: rows of the long side
+    const int from = turn & 1;  // X^T <- X^T B: rows of the long side
     x = g;
     x.ph = half(p.th[from]);
     x.pl = p.split ? half(p.tl[from]) : nullptr;
@@ -1000,7 +1107,7 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
     x.oh = half(p.th[from ^ 1]);
     x.ol = p.split ? half(p.tl[from ^ 1]) : nullptr;
     x.ostride = p.Mp * p.Np;
-    e = k + 1 < o.steps ? launch_prod<STEP>(p, x, tn * tm, s) : launch_prod<LAST>(p, x, tn * tm, s);
+    e = k + taken < o.steps ? launch_prod<STEP>(p, x, tn * tm, s) : launch_prod<LAST>(p, x, tn * tm, s);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -1087,7 +1194,8 @@ nf_status nf_orthogonalize(const void* src, int32_t src_type, int64_t src_ld, in
   pa.g = View{const_cast<void*>(src), src_ld, src_stride, src_type};
   ProdArgs last = {};
   last.dst = View{dst, dst_ld, dst_stride, dst_type};
-  return finish(run(p, pa, last, *params, ws, static_cast<hipStream_t>(stream)));
+  const bool coarse = params->products == NF_PRODUCTS_SINGLE || dst_type != NF_TYPE_F32;
+  return finish(run(p, pa, last, *params, coarse, ws, static_cast<hipStream_t>(stream)));
 }
 
 nf_status nf_orthogonal_update(const void* grad, int32_t grad_type, int64_t grad_ld, int64_t grad_stride,
@@ -1127,7 +1235,7 @@ nf_status nf_orthogonal_update(const void* grad, int32_t grad_type, int64_t grad
   last.update = 1;
   last.keep = 1.0f - step->lr * step->weight_decay;
   last.rate = step->lr * step->scale;
-  return finish(run(p, pa, last, *params, ws, static_cast<hipStream_t>(stream)));
+  return finish(run(p, pa, last, *params, true, ws, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"
