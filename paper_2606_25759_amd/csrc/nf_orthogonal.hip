@@ -8,6 +8,7 @@
 //   k_prod     one product P Q^T on the matrix cores with an epilogue:
 //                GRAM  A = X X^T
 //                POLY  B = b A + c A A
+//                MULT  alpha Y + Z Y of symmetric matrices that commute
 //                BOTH  A and the product of a few steps' polynomials of it,
 //                      where A is one tile (a short side of at most 64)
 //                STEP  X = a X + B X
@@ -61,7 +62,7 @@ constexpr int kNormElems = 4096;          // elements of a norm partial, at leas
 constexpr int kMaxParts = 1024;           // of a matrix
 constexpr int kBlock = 3;                 // steps that BOTH takes at once, at most
 
-enum { GRAM, POLY, STEP, LAST, BOTH };
+enum { GRAM, POLY, STEP, LAST, BOTH, MULT };
 
 // One matrix of the caller's, seen as rows x cols.
 struct View {
@@ -98,9 +99,11 @@ struct ProdArgs {
   float coef[kBlock][3];
   _Float16 *oh, *ol;                  // GRAM: A, POLY: B; STEP: X^T
   int64_t ostride;
-  const _Float16 *ah, *al;            // POLY: A
-  float* dA;                          // diagonals, [batch][Mp]
-  float* dB;
+  const _Float16 *ah, *al;            // POLY: A; MULT: Y (Z is P)
+  float* dA;                          // diagonals, [batch][Mp]: of A or Y
+  float* dB;                          // of B, of what MULT gives, of P where STEP takes that
+  const float* dZ;                    // MULT: of Z
+  float* dP;                          // POLY: if not nullptr, that of a + B
   _Float16 *xh, *xl;                  // STEP, LAST: X [Mp x Np]
   int64_t Mp, Np;
   View dst;                           // LAST
@@ -429,7 +432,7 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
   constexpr int OPS = SPLIT ? 4 : 2;         // tiles of a stage: P, Q (, their low halves)
   constexpr int LOADS = OPS * BT / 16 / NW;  // of a wavefront a stage
   constexpr int MI = WM / 16, NJ = WN / 16;
-  constexpr bool SYM = EPI == GRAM || EPI == POLY || EPI == BOTH;
+  constexpr bool SYM = EPI == GRAM || EPI == POLY || EPI == BOTH || EPI == MULT;
   __shared__ __align__(16) _Float16 lds[kStages][OPS][BT * kBK];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   // blocks go round the eight XCDs: each XCD takes a contiguous share of the tiles, matrix by matrix
@@ -468,18 +471,25 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
   half8 inh[EARLY ? CI : 1][EARLY ? CJ : 1], inl[EARLY ? CI : 1][EARLY ? CJ : 1];
   float dcol[EARLY ? CJ : 1];
   float4v drow[EARLY ? CI : 1][2];
+  half8 inzh[EARLY && EPI == MULT ? CI : 1][EARLY && EPI == MULT ? CJ : 1];
+  half8 inzl[EARLY && EPI == MULT ? CI : 1][EARLY && EPI == MULT ? CJ : 1];
   auto row_at = [&](int i) { return (int64_t)ti * BT + wm + 16 * i + lane / 16 * 8; };
   auto column_at = [&](int j) { return (int64_t)tj * BT + wn + j / 2 * 32 + j % 2 * 4 + lane % 16 / 4 * 8 + lane % 4; };
-  auto ask = [&](int i, int j, half8& h, half8& l, float& dc, float4v (&dr)[2]) {  // i even
+  auto ask = [&](int i, int j, half8& h, half8& l, float& dc, float4v (&dr)[2], half8& zh, half8& zl) {  // i even
     const int64_t r = row_at(i), c = column_at(j);
     l = half8{};
-    if (EPI == POLY) {
+    if (EPI == POLY || EPI == MULT) {
       const int64_t at = b * a.ostride + panel_at(c, r, a.Mp);
       h = *(const half8*)(a.ah + at);
       if (SPLIT) l = *(const half8*)(a.al + at);
       dc = a.dA[b * a.Mp + c];
-      dr[0] = *(const float4v*)(a.dA + b * a.Mp + r);
-      dr[1] = *(const float4v*)(a.dA + b * a.Mp + r + 4);
+      const float* rows = EPI == MULT ? a.dZ : a.dA;
+      dr[0] = *(const float4v*)(rows + b * a.Mp + r);
+      dr[1] = *(const float4v*)(rows + b * a.Mp + r + 4);
+      if (EPI == MULT) {
+        zh = *(const half8*)(a.ph + at);
+        zl = *(const half8*)(a.pl + at);
+      }
     } else if (EPI == STEP || EPI == LAST) {
       const int64_t at = b * a.Mp * a.Np + panel_at(c, r, a.Mp);
       h = *(const half8*)(a.xh + at);
@@ -487,11 +497,13 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
       dc = a.dB[b * a.Mp + c];
     }
   };
-  if constexpr (EARLY && (EPI == POLY || EPI == STEP || EPI == LAST)) {
+  if constexpr (EARLY && (EPI == POLY || EPI == STEP || EPI == LAST || EPI == MULT)) {
 #pragma unroll
     for (int i = 0; i < CI; ++i)
 #pragma unroll
-      for (int j = 0; j < CJ; ++j) ask(2 * i, j, inh[i][j], inl[i][j], dcol[j], drow[i]);
+      for (int j = 0; j < CJ; ++j)
+        ask(2 * i, j, inh[i][j], inl[i][j], dcol[j], drow[i], inzh[EPI == MULT ? i : 0][EPI == MULT ? j : 0],
+            inzl[EPI == MULT ? i : 0][EPI == MULT ? j : 0]);
   }
 
   // stages [first, first + stages), an even number of them
@@ -774,19 +786,21 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
           }
           continue;
         }
-        half8 h = {}, l = {};
+        half8 h = {}, l = {}, zh = {}, zl = {};
         float dc = 0.0f;
         float4v dr[2] = {};
-        if constexpr (EPI != GRAM) {
-          if constexpr (EARLY) {
-            h = inh[i / 2][j + y];
-            l = inl[i / 2][j + y];
-            dc = dcol[j + y];
-            dr[0] = drow[i / 2][0];
-            dr[1] = drow[i / 2][1];
-          } else {
-            ask(i, j + y, h, l, dc, dr);
+        if constexpr (EARLY) {
+          h = inh[i / 2][j + y];
+          l = inl[i / 2][j + y];
+          dc = dcol[j + y];
+          dr[0] = drow[i / 2][0];
+          dr[1] = drow[i / 2][1];
+          if (EPI == MULT) {
+            zh = inzh[EPI == MULT ? i / 2 : 0][EPI == MULT ? j + y : 0];
+            zl = inzl[EPI == MULT ? i / 2 : 0][EPI == MULT ? j + y : 0];
           }
+        } else {
+          ask(i, j + y, h, l, dc, dr, zh, zl);
         }
         if (EPI == POLY) {
 #pragma unroll
@@ -795,7 +809,19 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
             // (D + O)^2 = D^2 + D O + O D + O O
             v[y][e] = fmaf(a.c, fmaf(dr[e / 4][e % 4] + dc, o, d[e] * kInvScale), a.b * o);
             if (r + e == c) {
-              a.dB[b * a.Mp + c] = fmaf(a.c, fmaf(dc, dc, d[e] * kInvScale * kInvScale), a.b * dc);
+              const float on = fmaf(a.c, fmaf(dc, dc, d[e] * kInvScale * kInvScale), a.b * dc);
+              a.dB[b * a.Mp + c] = on;
+              if (a.dP) a.dP[b * a.Mp + c] = a.a + on;
+              v[y][e] = 0.0f;
+            }
+          }
+        } else if (EPI == MULT) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float o = (float)h[e] + (float)l[e], z = (float)zh[e] + (float)zl[e], dz = dr[e / 4][e % 4];
+            v[y][e] = fmaf(dz, o, fmaf(z, dc, d[e] * kInvScale)) + a.a * o;
+            if (r + e == c) {
+              a.dB[b * a.Mp + c] = fmaf(dz, dc, d[e] * kInvScale * kInvScale) + a.a * dc;
               v[y][e] = 0.0f;
             }
           }
@@ -819,23 +845,39 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
           h[y][e] = (_Float16)v[y][e];
           l[y][e] = (_Float16)(v[y][e] - (float)h[y][e]);
         }
-        const int64_t c = cq + 4 * y + lane % 4;
-        if (SYM) {
-          const int64_t at = b * a.ostride + panel_at(c, r, a.Mp);
-          *(half8*)(a.oh + at) = h[y];
-          if (SPLIT) *(half8*)(a.ol + at) = l[y];
-        } else {
-          const int64_t at = b * a.Mp * a.Np + panel_at(c, r, a.Mp);
+        if (!SYM) {
+          const int64_t at = b * a.Mp * a.Np + panel_at(cq + 4 * y + lane % 4, r, a.Mp);
           *(half8*)(a.xh + at) = h[y];
           *(half8*)(a.xl + at) = l[y];
         }
       }
-      if (SYM && ti == tj) continue;  // the block on the diagonal has both halves
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const int64_t to = b * a.ostride + panel_at(rq + 4 * x, cq, SYM ? a.Mp : a.Np);
-        *(half8*)(a.oh + to) = transpose8(h[0], h[1], x, lane);
-        if (SPLIT) *(half8*)(a.ol + to) = transpose8(l[0], l[1], x, lane);
+        const half8 th = transpose8(h[0], h[1], x, lane), tl = SPLIT ? transpose8(l[0], l[1], x, lane) : half8{};
+        if (!SYM) {
+          const int64_t to = b * a.ostride + panel_at(rq + 4 * x, cq, a.Np);
+          *(half8*)(a.oh + to) = th;
+          if (SPLIT) *(half8*)(a.ol + to) = tl;
+          continue;
+        }
+        // of a symmetric matrix what is below the diagonal, and its mirror image
+        const int64_t c = cq + 4 * x + lane % 4;
+        const int64_t at = b * a.ostride + panel_at(c, r, a.Mp), to = b * a.ostride + panel_at(rq + 4 * x, cq, a.Mp);
+        if (r > cq) {
+          *(half8*)(a.oh + at) = h[x];
+          *(half8*)(a.oh + to) = th;
+          if (SPLIT) *(half8*)(a.ol + at) = l[x];
+          if (SPLIT) *(half8*)(a.ol + to) = tl;
+        } else if (r == cq) {  // th is of row c
+          half8 sh, sl;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            sh[e] = r + e >= c ? h[x][e] : th[e];
+            sl[e] = r + e >= c ? l[x][e] : tl[e];
+          }
+          *(half8*)(a.oh + at) = sh;
+          if (SPLIT) *(half8*)(a.ol + at) = sl;
+        }
       }
     }
   }
@@ -848,10 +890,12 @@ struct Plan {
   int tall, nparts, lg_tx;
   int tile, gram_tile, poly_tile;  // of STEP and LAST, GRAM and BOTH, POLY
   bool split;
+  bool gram_space;  // a few steps at a time by their Gram matrix (m > 64: by MULT)
   int shares;      // of a GRAM tile's k
   int64_t tiles;   // GRAM's, if it has shares
   size_t gpart, arrived;
   size_t part, dA, dB, xh, xl, th[2], tl[2], ah, al, bh, bl, total;
+  size_t sq[10], sqd[6];  // gram_space: R, two Z, two P, high and low; their diagonals and that of the first P
 };
 
 constexpr int64_t kCUs = 256;
@@ -886,11 +930,14 @@ int shares_of(int64_t tiles, int64_t stages, int tile) {
 int64_t below_diagonal(int64_t tm) { return tm * (tm + 1) / 2; }
 
 // The tiles of each product: the cheapest for a STEP, whose tile the sides are padded to, then for the others the
-// cheapest of those that divide it.
-void choose_tiles(Plan* p) {
+// cheapest of those that divide it.  Returns the microseconds of a GRAM and a STEP, and of a product of m x m.
+struct Cost {
+  double x, square;
+};
+Cost choose_tiles(Plan* p) {
   const int most = p->split ? 128 : 256;
   p->tile = p->gram_tile = p->poly_tile = 64;
-  if (p->m <= 64) return;  // A is one tile
+  if (p->m <= 64) return Cost{};  // A is one tile
   auto padded = [](int64_t x, int t) { return ceil_div(x, t) * t; };
   double best = 0.0;
   for (int t = 64; t <= most; t *= 2) {
@@ -910,10 +957,27 @@ void choose_tiles(Plan* p) {
     if (t == 64 || gram < best_gram) best_gram = gram, p->gram_tile = t;
     if (t == 64 || poly < best_poly) best_poly = poly, p->poly_tile = t;
   }
+  // a launch takes 4 us at least; what a STEP reads and writes of X, 5 TB/s, is not hidden behind its products
+  const double moved = (p->split ? 16.0 : 10.0) * (double)p->batch * (double)M * (double)N / 5e6;
+  return Cost{8.0 + best_gram + best + moved, 4.0 + best_poly};
+}
+
+// Steps at a time by the Gram matrix, where that is sooner: of five steps (three and two), X is read and written for
+// two, and there are fourteen products of m x m in place of five, all of split operands.
+void choose_form(Plan* p, bool coarse) {
+  Plan q = *p;
+  q.split = true;
+  const Cost by_step = choose_tiles(p);
+  if (p->m <= 64 || !coarse) return;
+  const Cost by_gram = choose_tiles(&q);
+  if (2.0 * by_gram.x + 14.0 * by_gram.square < 5.0 * (by_step.x + by_step.square)) {
+    *p = q;
+    p->gram_space = true;
+  }
 }
 
 // Sizes are checked by the caller.
-Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split) {
+Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split, bool coarse) {
   Plan p = {};
   p.rows = rows;
   p.cols = cols;
@@ -924,7 +988,7 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split) {
   // a short side of few rows has few roundings to average out (3.4e-3 measured at 1 x 7), and costs launches,
   // not products: always in pairs
   p.split = split || p.m <= 64;
-  choose_tiles(&p);
+  choose_form(&p, coarse);
   p.Mp = ceil_div(p.m, p.tile) * p.tile;
   p.Np = ceil_div(p.n, p.tile) * p.tile;
   p.nparts = (int)(ceil_div(rows * cols, kNormElems) < kMaxParts ? ceil_div(rows * cols, kNormElems) : kMaxParts);
@@ -946,6 +1010,10 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split) {
   const bool one = p.m <= 64;  // A never leaves its block
   if (!one) p.ah = take(a);
   p.bh = take(a);
+  if (p.gram_space) {
+    for (size_t& o : p.sq) o = take(a);
+    for (size_t& o : p.sqd) o = take((size_t)(4 * batch * p.Mp));
+  }
   if (p.split) {
     p.tl[0] = take(x);
     p.tl[1] = take(x);
@@ -966,7 +1034,7 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split) {
 template <int EPI, bool SPLIT>
 hipError_t launch_prod(const Plan& p, const ProdArgs& a, int64_t tiles, hipStream_t s) {
   const unsigned grid = (unsigned)(tiles * p.batch);
-  const int tile = EPI == GRAM || EPI == BOTH ? p.gram_tile : EPI == POLY ? p.poly_tile : p.tile;
+  const int tile = EPI == GRAM || EPI == BOTH ? p.gram_tile : EPI == POLY || EPI == MULT ? p.poly_tile : p.tile;
   if constexpr (EPI == BOTH) {
     if (p.shares > 1)
       k_prod<64, 32, 32, true, EPI, true><<<grid * p.shares, 256, 0, s>>>(a);
@@ -994,25 +1062,32 @@ hipError_t launch_prod(const Plan& p, const ProdArgs& a, int64_t tiles, hipStrea
 
 template <int EPI>
 hipError_t launch_prod(const Plan& p, const ProdArgs& a, int64_t tiles, hipStream_t s) {
-  if constexpr (EPI == BOTH) return launch_prod<EPI, true>(p, a, tiles, s);
-  return p.split ? launch_prod<EPI, true>(p, a, tiles, s) : launch_prod<EPI, false>(p, a, tiles, s);
+  if constexpr (EPI == BOTH || EPI == MULT)
+    return launch_prod<EPI, true>(p, a, tiles, s);
+  else
+    return p.split ? launch_prod<EPI, true>(p, a, tiles, s) : launch_prod<EPI, false>(p, a, tiles, s);
 }
 
-// Steps from the k-th on that BOTH takes at once.  What grows a small singular value grows the rounding of A, P and
-// P X as well: as far as P stays within 48 (three steps of 3.4445, and FP16's range).  The error is then up to 6e-6
-// (4e-6 step by step), which only a result in FP32 from split products shows: that one goes step by step.
+// Steps from the k-th on that are taken at once by the Gram matrix.  What grows a small singular value grows the
+// rounding of A, P and P X as well: as far as P, whose norm is at most the product of the largest |q|, stays within 48
+// (three steps of 3.4445; FP16's range ends at 64).  The error is then up to 6e-6 (4e-6 step by step), which only a
+// result in FP32 from split products shows: that one goes step by step.
 int block_of(const nf_orthogonal_params& o, int k, bool coarse) {
-  double growth = 1.0;
+  double top = 1.0, growth = 1.0;  // of the singular values: X is scaled to at most 1
   int n = 0;
-  for (; n < kBlock && k + n < o.steps; ++n) {
-    const float* c = o.coef[k + n];
-    double most = 0.0;
-    for (int i = 0; i <= 24; ++i) {  // |q| over the squares of singular values up to 1.2
-      const double x = i * 0.06;
-      most = fmax(most, fabs(c[0] + x * (c[1] + x * c[2])));
+  for (int i = 0; i < k + kBlock && i < o.steps; ++i) {
+    const float* c = o.coef[i];
+    double most = 0.0, next = 0.0;
+    for (int j = 0; j <= 64; ++j) {
+      const double sv = top * j / 64, q = fabs(c[0] + sv * sv * (c[1] + sv * sv * c[2]));
+      most = fmax(most, q);
+      next = fmax(next, sv * q);
     }
+    top = next;
+    if (i < k) continue;
     growth *= fmax(most, 1.0);
-    if (n > 0 && (!coarse || growth > 48.0)) break;
+    if (n > 0 && (!coarse || !(growth <= 48.0))) break;
+    ++n;
   }
   return n;
 }
@@ -1064,6 +1139,7 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
     g.xh = half(p.xh);
     g.xl = half(p.xl);
 
+    _Float16 *bh = half(p.bh), *bl = p.split ? half(p.bl) : nullptr;  // what STEP multiplies X by
     ProdArgs x = g;  // A = X X^T
     x.ph = x.qh = half(p.xh);
     x.pl = x.ql = half(p.xl);
@@ -1081,6 +1157,67 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
       x.ol = half(p.bl);
       if ((e = launch_prod<BOTH>(p, x, 1, s)) != hipSuccess) return e;
       g.a = 0.0f;  // P holds it
+    } else if (p.gram_space) {
+      taken = block_of(o, k, coarse);
+      if ((e = launch_prod<GRAM>(p, x, below_diagonal(x.tm), s)) != hipSuccess) return e;
+      // A <- q(A) A q(A) by R = q(A) A, and P, the product of the q(A) = a + Z so far
+      struct Square {
+        _Float16 *h, *l;
+        float* d;
+      };
+      auto square = [&](int i, int d) {
+        return Square{half(p.sq[2 * i]), half(p.sq[2 * i + 1]), reinterpret_cast<float*>(w + p.sqd[d])};
+      };
+      const Square A = {half(p.ah), half(p.al), g.dA}, R = square(0, 0), Z[2] = {square(1, 1), square(2, 2)},
+                   Q[2] = {square(3, 3), square(4, 4)};
+      ProdArgs y = x;
+      y.ldk = p.Mp;
+      y.pstride = y.qstride = p.Mp * p.Mp;
+      y.tm = y.tn = (int32_t)(p.Mp / p.poly_tile);
+      const int64_t tiles = below_diagonal(y.tm);
+      auto multiply = [&](const Square& z, const Square& with, const Square& to, float alpha) {
+        y.ph = z.h;
+        y.pl = z.l;
+        y.dZ = z.d;
+        y.qh = y.ah = with.h;
+        y.ql = y.al = with.l;
+        y.dA = with.d;
+        y.oh = to.h;
+        y.ol = to.l;
+        y.dB = to.d;
+        y.a = alpha;
+        return launch_prod<MULT>(p, y, tiles, s);
+      };
+      Square P = {};
+      for (int i = 0; i < taken; ++i) {
+        const float* c = o.coef[k + i];
+        const Square& z = Z[i & 1];
+        y.ph = y.qh = y.ah = A.h;  // Z = b A + c A A
+        y.pl = y.ql = y.al = A.l;
+        y.dA = A.d;
+        y.a = c[0];
+        y.b = c[1];
+        y.c = c[2];
+        y.oh = z.h;
+        y.ol = z.l;
+        y.dB = z.d;
+        y.dP = i == 0 ? reinterpret_cast<float*>(w + p.sqd[5]) : nullptr;
+        if ((e = launch_prod<POLY>(p, y, tiles, s)) != hipSuccess) return e;
+        if (i == 0) {
+          P = Square{z.h, z.l, y.dP};  // differs from Z in its diagonal only
+        } else {
+          if ((e = multiply(z, P, Q[i & 1], c[0])) != hipSuccess) return e;
+          P = Q[i & 1];
+        }
+        if (i + 1 < taken) {
+          if ((e = multiply(z, A, R, c[0])) != hipSuccess) return e;
+          if ((e = multiply(z, R, A, c[0])) != hipSuccess) return e;
+        }
+      }
+      bh = P.h;
+      bl = P.l;
+      g.dB = P.d;
+      g.a = 0.0f;  // P holds it
     } else {
       if ((e = launch_prod<GRAM>(p, x, below_diagonal(x.tm), s)) != hipSuccess) return e;
       x.ph = x.qh = x.ah = half(p.ah);  // B = b A + c A A
@@ -1097,8 +1234,8 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
     x = g;
     x.ph = half(p.th[from]);
     x.pl = p.split ? half(p.tl[from]) : nullptr;
-    x.qh = half(p.bh);
-    x.ql = p.split ? half(p.bl) : nullptr;
+    x.qh = bh;
+    x.ql = bl;
     x.ldk = p.Mp;
     x.pstride = p.Mp * p.Np;
     x.qstride = p.Mp * p.Mp;
@@ -1170,7 +1307,11 @@ extern "C" {
 size_t nf_orthogonal_workspace_bytes(int64_t rows, int64_t cols, int64_t batch, const nf_orthogonal_params* params) {
   if (nf::check_params(params) || nf::check_sizes(rows, cols, batch) || nf::too_large(rows, cols, batch)) return 0;
   if (rows == 0 || cols == 0 || batch == 0) return 0;
-  return nf::plan_of(rows, cols, batch, params->products == NF_PRODUCTS_SPLIT).total;
+  // (a caller's results may be of any type: the larger of the two forms)
+  const bool split = params->products == NF_PRODUCTS_SPLIT;
+  const size_t fine = nf::plan_of(rows, cols, batch, split, false).total;
+  const size_t coarse = nf::plan_of(rows, cols, batch, split, true).total;
+  return fine > coarse ? fine : coarse;
 }
 
 nf_status nf_orthogonalize(const void* src, int32_t src_type, int64_t src_ld, int64_t src_stride, void* dst,
@@ -1188,13 +1329,13 @@ nf_status nf_orthogonalize(const void* src, int32_t src_type, int64_t src_ld, in
   st = check_view(dst, dst_type, dst_ld, dst_stride, rows, cols, batch, "dst is NULL",
                   "dst_ld < cols or dst_stride too small", "dst not aligned to its elements");
   if (st != NF_OK) return st;
-  const Plan p = plan_of(rows, cols, batch, params->products == NF_PRODUCTS_SPLIT);
-  if ((st = check_ws(ws, ws_bytes, p.total)) != NF_OK) return st;
+  const bool coarse = params->products == NF_PRODUCTS_SINGLE || dst_type != NF_TYPE_F32;
+  const Plan p = plan_of(rows, cols, batch, params->products == NF_PRODUCTS_SPLIT, coarse);
+  if ((st = check_ws(ws, ws_bytes, nf_orthogonal_workspace_bytes(rows, cols, batch, params))) != NF_OK) return st;
   PrepArgs pa = {};
   pa.g = View{const_cast<void*>(src), src_ld, src_stride, src_type};
   ProdArgs last = {};
   last.dst = View{dst, dst_ld, dst_stride, dst_type};
-  const bool coarse = params->products == NF_PRODUCTS_SINGLE || dst_type != NF_TYPE_F32;
   return finish(run(p, pa, last, *params, coarse, ws, static_cast<hipStream_t>(stream)));
 }
 
@@ -1221,8 +1362,8 @@ nf_status nf_orthogonal_update(const void* grad, int32_t grad_type, int64_t grad
   st = check_view(weight, weight_type, weight_ld, weight_stride, rows, cols, batch, "weight is NULL",
                   "weight_ld < cols or weight_stride too small", "weight not aligned to its elements");
   if (st != NF_OK) return st;
-  const Plan p = plan_of(rows, cols, batch, params->products == NF_PRODUCTS_SPLIT);
-  if ((st = check_ws(ws, ws_bytes, p.total)) != NF_OK) return st;
+  const Plan p = plan_of(rows, cols, batch, params->products == NF_PRODUCTS_SPLIT, true);
+  if ((st = check_ws(ws, ws_bytes, nf_orthogonal_workspace_bytes(rows, cols, batch, params))) != NF_OK) return st;
   PrepArgs pa = {};
   pa.g = View{const_cast<void*>(grad), grad_ld, grad_stride, grad_type};
   pa.mom = momentum;

@@ -152,6 +152,34 @@ def test_steps_and_coefficients(steps, coef, products):
     assert far(dst, exact(u.cpu().numpy(), steps, triples, eps=np.float32(0.01))) <= BOUND[products]["gauss"]
 
 
+@pytest.mark.parametrize("dst", ["bf16", "f32"])
+@pytest.mark.parametrize("products", BOTH)
+@pytest.mark.parametrize("kind", ["gauss", "decay"])
+@pytest.mark.parametrize("batch,m,n", [(12, 100, 4000), (3, 6001, 150), (1, 64, 20_000), (30, 30, 2000), (2, 300, 5000)])
+def test_long_sides(batch, m, n, kind, products, dst):
+    """Where several steps are taken at once by the Gram matrix, and a tile's k by several blocks."""
+    u = torch.from_numpy(make(kind, m, n, m + n, batch)).float().to(DEV)
+    d = torch.empty(u.shape, dtype=TYPES[dst], device=DEV)
+    how = nf.orthogonal(products=products)
+    nf.nf_orthogonalize(u, d, how, workspace(u, how))
+    for k in range(0, batch, 5):
+        assert far(d[k], exact(u[k].cpu().numpy())) <= BOUND[products][kind] + UNIT[dst]
+
+
+@pytest.mark.parametrize("coef", [COEF, (1.5, -0.5, 0.0), (2.0, -1.5, 0.5), (3.0, -3.2, 1.2)])
+@pytest.mark.parametrize("steps", [1, 2, 4, 7, 12])
+@pytest.mark.parametrize("batch,m,n", [(12, 100, 4000), (2, 40, 900)])
+def test_long_sides_steps(batch, m, n, steps, coef):
+    u = torch.from_numpy(make("gauss", m, n, 3, batch)).float().to(DEV)
+    d = torch.empty(u.shape, dtype=torch.bfloat16, device=DEV)
+    triples = [coef] * (steps - 1) + [(1.875, -1.25, 0.375)]
+    how = nf.orthogonal(steps=steps, coef=triples)
+    nf.nf_orthogonalize(u, d, how, workspace(u, how))
+    for k in (0, batch - 1):
+        want = exact(u[k].cpu().numpy(), steps, triples)
+        assert far(d[k], want) <= BOUND[nf.NF_PRODUCTS_SINGLE]["gauss"] + UNIT["bf16"]
+
+
 def test_in_place_other_stream_and_repeatable():
     u = torch.from_numpy(make("decay", 200, 150, 1, 2)).float().to(DEV)
     how = nf.orthogonal()
