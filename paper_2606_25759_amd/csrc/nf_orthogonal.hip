@@ -434,7 +434,8 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
   constexpr int MI = WM / 16, NJ = WN / 16;
   constexpr bool SYM = EPI == GRAM || EPI == POLY || EPI == BOTH || EPI == MULT;
   __shared__ __align__(16) _Float16 lds[kStages][OPS][BT * kBK];
-  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  int lane = threadIdx.x % 64;
   // blocks go round the eight XCDs: each XCD takes a contiguous share of the tiles, matrix by matrix
   int id;
   {
@@ -590,6 +591,7 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
   }
   step(none, none, stages - 2, f0, f1);
   multiply(f1);
+  asm volatile("" : "+v"(lane));  // what the epilogue derives from it is not worth registers during the products
 
   if constexpr (SHARED) {
     // Each share's sums go to memory; the block that is last to arrive adds them up, in the order of the shares.
@@ -1035,28 +1037,31 @@ template <int EPI, bool SPLIT>
 hipError_t launch_prod(const Plan& p, const ProdArgs& a, int64_t tiles, hipStream_t s) {
   const unsigned grid = (unsigned)(tiles * p.batch);
   const int tile = EPI == GRAM || EPI == BOTH ? p.gram_tile : EPI == POLY || EPI == MULT ? p.poly_tile : p.tile;
-  if constexpr (EPI == BOTH) {
-    if (p.shares > 1)
-      k_prod<64, 32, 32, true, EPI, true><<<grid * p.shares, 256, 0, s>>>(a);
-    else
-      k_prod<64, 32, 32, true, EPI><<<grid, 256, 0, s>>>(a);
-  } else if (EPI == GRAM && p.shares > 1) {
-    if (tile == 64)
-      k_prod<64, 32, 32, SPLIT, EPI, EPI == GRAM><<<grid * p.shares, 256, 0, s>>>(a);
-    else if (SPLIT)
-      k_prod<128, 64, 32, true, EPI, EPI == GRAM><<<grid * p.shares, 512, 0, s>>>(a);
-    else
-      k_prod<128, 64, 64, false, EPI, EPI == GRAM><<<grid * p.shares, 256, 0, s>>>(a);
-  } else {
-    if (tile == 64)
-      k_prod<64, 32, 32, SPLIT, EPI><<<grid, 256, 0, s>>>(a);
-    else if (SPLIT)
-      k_prod<128, 64, 32, true, EPI><<<grid, 512, 0, s>>>(a);
-    else if (tile == 128)
-      k_prod<128, 64, 64, false, EPI><<<grid, 256, 0, s>>>(a);
-    else
-      k_prod<256, 128, 64, false, EPI><<<grid, 512, 0, s>>>(a);
+  auto go = [&](auto shared, unsigned blocks) {
+    constexpr bool S = decltype(shared)::value;
+    if constexpr (EPI == BOTH) {
+      k_prod<64, 32, 32, true, EPI, S><<<blocks, 256, 0, s>>>(a);
+    } else if constexpr (SPLIT) {
+      if (tile == 64)
+        k_prod<64, 32, 32, true, EPI, S><<<blocks, 256, 0, s>>>(a);
+      else
+        k_prod<128, 64, 32, true, EPI, S><<<blocks, 512, 0, s>>>(a);
+    } else {
+      if (tile == 64)
+        k_prod<64, 32, 32, false, EPI, S><<<blocks, 256, 0, s>>>(a);
+      else if (tile == 128)
+        k_prod<128, 64, 64, false, EPI, S><<<blocks, 256, 0, s>>>(a);
+      else if constexpr (!S)
+        k_prod<256, 128, 64, false, EPI><<<blocks, 512, 0, s>>>(a);
+    }
+  };
+  if constexpr (EPI == GRAM || EPI == BOTH) {
+    if (p.shares > 1) {
+      go(std::true_type{}, grid * p.shares);
+      return hipGetLastError();
+    }
   }
+  go(std::false_type{}, grid);
   return hipGetLastError();
 }
 
