@@ -847,12 +847,20 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
           h[y][e] = (_Float16)v[y][e];
           l[y][e] = (_Float16)(v[y][e] - (float)h[y][e]);
         }
+        const int64_t c = cq + 4 * y + lane % 4;
         if (!SYM) {
-          const int64_t at = b * a.Mp * a.Np + panel_at(cq + 4 * y + lane % 4, r, a.Mp);
+          const int64_t at = b * a.Mp * a.Np + panel_at(c, r, a.Mp);
           *(half8*)(a.xh + at) = h[y];
           *(half8*)(a.xl + at) = l[y];
+        } else if (!SPLIT || ti != tj) {
+          const int64_t at = b * a.ostride + panel_at(c, r, a.Mp);
+          *(half8*)(a.oh + at) = h[y];
+          if (SPLIT) *(half8*)(a.ol + at) = l[y];
         }
       }
+      // Of a symmetric matrix a tile below the diagonal has its mirror image elsewhere.  A tile on it has both halves:
+      // 11 bits do not show that they differ; of 22, what is below the diagonal is kept and mirrored.
+      if (SYM && !SPLIT && ti == tj) continue;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const half8 th = transpose8(h[0], h[1], x, lane), tl = SPLIT ? transpose8(l[0], l[1], x, lane) : half8{};
@@ -862,23 +870,25 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
           if (SPLIT) *(half8*)(a.ol + to) = tl;
           continue;
         }
-        // of a symmetric matrix what is below the diagonal, and its mirror image
         const int64_t c = cq + 4 * x + lane % 4;
         const int64_t at = b * a.ostride + panel_at(c, r, a.Mp), to = b * a.ostride + panel_at(rq + 4 * x, cq, a.Mp);
-        if (r > cq) {
-          *(half8*)(a.oh + at) = h[x];
+        if (ti != tj) {
           *(half8*)(a.oh + to) = th;
-          if (SPLIT) *(half8*)(a.ol + at) = l[x];
           if (SPLIT) *(half8*)(a.ol + to) = tl;
-        } else if (r == cq) {  // th is of row c
-          half8 sh, sl;
+        } else if (SPLIT && r >= cq) {
+          half8 sh = h[x], sl = l[x];
+          if (r == cq) {  // th is of row c
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            sh[e] = r + e >= c ? h[x][e] : th[e];
-            sl[e] = r + e >= c ? l[x][e] : tl[e];
+            for (int e = 0; e < 8; ++e) {
+              if (r + e < c) sh[e] = th[e];
+              if (r + e < c) sl[e] = tl[e];
+            }
+          } else {
+            *(half8*)(a.oh + to) = th;
+            *(half8*)(a.ol + to) = tl;
           }
           *(half8*)(a.oh + at) = sh;
-          if (SPLIT) *(half8*)(a.ol + at) = sl;
+          *(half8*)(a.ol + at) = sl;
         }
       }
     }
