@@ -637,8 +637,8 @@ nf_status nf_embedding_lookup(const void* table, int32_t table_type, int64_t tab
  * accumulate != 0 the sums are added to what the segment holds and rows
  * without a token are left alone.  Tokens outside [0, V), and those equal to
  * padding_id (-1 for none), add to no row.  Each row's terms are added in
- * FP32 in an order fixed by the sizes (tokens in ascending order in groups),
- * without floating-point atomics: two calls give the same bits.
+ * FP32 in an order fixed by the ids (ascending tokens, in groups), without
+ * floating-point atomics: two calls give the same bits.
  * `grads` is the segment in worker 0's row (a row's base plus the table's
  * offset in it), 4-byte aligned.  dy[w] is T rows dy_ld apart, workers
  * dy_stride elements apart; ids rows ids_stride apart.
@@ -653,9 +653,10 @@ nf_status nf_embedding_grad(const void* dy, int32_t dy_type, int64_t dy_ld, int6
                             int64_t worker_stride, void* ws, size_t ws_bytes, void* stream);
 
 /* How nf_orthogonalize forms its products: of operands rounded once to FP16
- * (11 bits), or each held as two FP16 numbers (22 bits, three products; a
- * shorter side of at most 64 always takes these).  The result is within about 2e-3 of the exact one relative to its norm, or within
- * about 1e-5 (FP32 products are no closer). */
+ * (11 bits), or each held as two FP16 numbers (22 bits, three products).  The
+ * result is within about 2e-3 of the exact one relative to its norm, or within
+ * about 1e-5 (FP32 products are no closer).  Sizes for which products are not
+ * what takes the time get the latter with NF_PRODUCTS_SINGLE as well. */
 enum { NF_PRODUCTS_SINGLE = 0, NF_PRODUCTS_SPLIT = 1 };
 #define NF_ORTHOGONAL_MAX_STEPS 12
 typedef struct {

@@ -12,8 +12,9 @@
 //   k_join      the rows of the latter: a frequent token's rows are read by
 //               many wavefronts, and none reads more than kOwn
 //
-// All are bound by memory traffic: the gradient's floor is the dense FP32
-// segment written once and dy read once.  The order in which a row's terms
+// All are bound by memory traffic, or, up to some thousand tokens, by the
+// latency of one launch after the other.  The gradient's floor is the dense
+// FP32 segment written once and dy read once.  The order in which a row's terms
 // are added depends on the sorted tokens alone, so results are reproducible
 // bit for bit.
 #include <type_traits>
@@ -44,6 +45,9 @@ constexpr int kThreadsE = 256;
 
 // Eight elements of a row a thread (one where rows have fewer), the last ones
 // of a row where they are: the thread before may have some of them too.
+// Bound by memory: 32,768 skewed tokens of width 2048, FP32 to BF16, in 43 us
+// (about 12,500 different rows: 237 MB, 5.5 TB/s); 64 tokens in 2.7 us, under
+// the 6 us that the call takes on the host.
 template <typename A, typename B, int N>
 __global__ __launch_bounds__(kThreadsE) void k_lookup(LookupArgs a) {
   const int tx = 1 << a.lg_tx, ty = kThreadsE >> a.lg_tx;
@@ -118,7 +122,9 @@ __device__ void fill_zero(float* p, int64_t n, int64_t b, int64_t nb) {
 }
 
 // Least-significant-digit radix sort of up to THREADS * ITEMS tokens, 8 bits
-// a pass.  Item i of lane l of wavefront w is the (w * ITEMS + i) * 64 + l-th,
+// a pass: 12 us for runs of 4,096, hidden behind the zeroes where there are
+// any (412 MB: 62 us, 6.6 TB/s; 3.3 GB: 570 us, 5.8 TB/s).  Runs of 16,384
+// took 33 us: the ranks are VALU work of one CU.  Item i of lane l of wavefront w is the (w * ITEMS + i) * 64 + l-th,
 // so ranks taken wavefront by wavefront, item by item and lane by lane keep
 // equal digits in order.
 template <int THREADS, int ITEMS>
@@ -223,7 +229,8 @@ __global__ __launch_bounds__(THREADS) void k_sort(GradArgs a) {
 // Groups of kRuns runs of a.run tokens: a token goes behind those of its own
 // run before it and those of every other run with a smaller id (of the
 // earlier runs: or the same).  Neighbours in a run have neighbouring ids, so
-// a wavefront's searches touch the same few lines.
+// a wavefront's searches touch the same few lines.  8,192 tokens in two runs
+// 7.6 us, 2 x 30,011 in eight 12 us: the searches' latency.
 __global__ __launch_bounds__(kThreadsE) void k_merge(GradArgs a) {
   const int64_t i = (int64_t)blockIdx.x * kThreadsE + threadIdx.x;
   if (i >= a.T) return;
@@ -268,9 +275,9 @@ __global__ __launch_bounds__(kThreadsE) void k_merge(GradArgs a) {
 // ---------------------------------------------------------------- the sums
 
 // A block's columns are an even share of a row's, N adjacent ones a lane (four;
-// one where rows have fewer than four); the last
-// lane that has any takes the last N (its neighbour may have some of them
-// too, and comes to the same values), so that no access needs a condition.
+// one where rows have fewer than four); the last lane that has any takes the
+// last N (its neighbour may have some of them too, and comes to the same
+// values), so that no access needs a condition.
 struct Columns {
   int at;     // of this lane
   bool mine;  // false: `at` is another lane's too, and this one stores nothing
@@ -294,7 +301,8 @@ __device__ __forceinline__ void add_to(float (&s)[N], const Near<D, N>& x) {
 }
 
 // Sorted tokens [p0, p0 + kOwn).  Their rows are asked for at once: an id
-// does not wait for the one before it.
+// does not wait for the one before it (8,192 tokens of width 2048: 73 us when
+// it did, 23 us now, for 34 MB read and about 30 MB written).
 template <typename D, int N, bool ADD, bool ALONE>
 __global__ __launch_bounds__(64) void k_rows_sum(GradArgs a) {
   const int lane = threadIdx.x, w = blockIdx.z;
@@ -314,7 +322,8 @@ __global__ __launch_bounds__(64) void k_rows_sum(GradArgs a) {
   const int end = __popcll(__ballot(lane < count && here < V));  // those of no row come last
   if (end == 0) return;
   if (ALONE && !(begins & ((1ull << end) - 1))) return;
-  const bool goes_on = end == kOwn && __builtin_amdgcn_readlane(here, kOwn) == __builtin_amdgcn_readlane(here, kOwn - 1);
+  const bool goes_on =
+      end == kOwn && __builtin_amdgcn_readlane(here, kOwn) == __builtin_amdgcn_readlane(here, kOwn - 1);
   auto row_of = [&](int i) {
     const uint32_t id = (uint32_t)__builtin_amdgcn_readlane(here, min(i, end - 1));
     return (Near<float, N>*)(grads + (int64_t)id * a.d + c.at);
@@ -372,8 +381,9 @@ __global__ __launch_bounds__(64) void k_rows_sum(GradArgs a) {
 }
 
 // Ids that begin in kOwn tokens and go on after them, a wavefront each: their
-// sums in order.  One of more than kAlone sums is left to the whole block: an
-// even share of them to each wavefront, and the shares in order.
+// sums in order (5 us for 8,192 skewed tokens of width 2048).  One of more than
+// kAlone sums is left to the whole block: an even share of them to each
+// wavefront, and the shares in order.
 constexpr int kDepth = 8;  // sums under way
 constexpr int kAlone = 4 * kDepth;
 
@@ -582,7 +592,8 @@ nf_status nf_embedding_grad(const void* dy, int32_t dy_type, int64_t dy_ld, int6
   if (ids_bytes != 4 && ids_bytes != 8) return bad("ids_bytes must be 4 or 8");
   if (const char* why = check_grad_sizes(W, T, V, d)) return bad(why);
   if (dy_ld < d) return bad("dy_ld < d");
-  if (W > 1 && T > 0 && (dy_stride < (T - 1) * dy_ld + d || ids_stride < T)) return bad("dy_stride or ids_stride too small");
+  if (W > 1 && T > 0 && (dy_stride < (T - 1) * dy_ld + d || ids_stride < T))
+    return bad("dy_stride or ids_stride too small");
   if (W > 1 && worker_stride < V * d) return bad("worker_stride < V * d");
   if (accumulate != 0 && accumulate != 1) return bad("accumulate must be 0 or 1");
   if (V == 0 || d == 0) return set_error(NF_OK, "");

@@ -170,13 +170,16 @@ __device__ double block_sum(double x, double* s) {
 
 // Block x of matrix y: every nparts-th group of rows, threads 2^lg_tx across
 // a row.  Squares are FP64, so no gradient's scale overflows or vanishes.
+// Bound by memory: 24 x (2048 x 2048) FP32 in 79 to 93 us (403 MB, 4.3 to 5.1
+// TB/s); with the momentum, 4 x (8192 x 2048) in 142 us (805 MB, 5.7 TB/s).
 __global__ __launch_bounds__(kNormThreads) void k_norm(PrepArgs a) {
   __shared__ double s[kNormThreads / 64];
   const int tx = 1 << a.lg_tx, ty = kNormThreads >> a.lg_tx;
   const int64_t b = blockIdx.y;
-  if (b == 0)
-    for (int64_t i = (int64_t)blockIdx.x * kNormThreads + threadIdx.x; i < a.tiles; i += (int64_t)gridDim.x * kNormThreads)
-      a.arrived[i] = 0;
+  if (b == 0) {
+    const int64_t all = (int64_t)gridDim.x * kNormThreads;
+    for (int64_t i = (int64_t)blockIdx.x * kNormThreads + threadIdx.x; i < a.tiles; i += all) a.arrived[i] = 0;
+  }
   const int x = threadIdx.x & (tx - 1), y = threadIdx.x >> a.lg_tx;
   double sum = 0.0;
   for (int64_t r = (int64_t)blockIdx.x * ty + y; r < a.rows; r += (int64_t)gridDim.x * ty) {
@@ -206,7 +209,8 @@ __global__ __launch_bounds__(kNormThreads) void k_norm(PrepArgs a) {
 }
 
 // A 64 x 64 tile of the caller's matrix, padding included: scaled, split in
-// two FP16, stored as it lies and transposed.
+// two FP16, stored as it lies and transposed.  Bound by memory: 24 x (2048 x
+// 2048) in 177 us (403 MB read, 604 MB written: 5.7 TB/s).
 __global__ __launch_bounds__(kNormThreads) void k_scale(PrepArgs a) {
   __shared__ double s[kNormThreads / 64];
   __shared__ float tile[64][65];
@@ -426,6 +430,16 @@ __device__ __forceinline__ void store_last(const ProdArgs& a, int64_t b, int64_t
 // wavefront that passes it has its loads of stage s + 1 in LDS, and has read
 // stage s - 1, whose place stage s + 3 takes.  In split mode a stage holds
 // both halves of both operands, and feeds three products.
+//
+// What bounds it.  The loop by itself, with tiles of 256 on 4096 x 4096 x 4096,
+// does 1.36 PFLOP/s, as a library product of that type does (1.38 to 1.41).
+// Of 24 x (2048 x 2048), GRAM takes 238 us (0.97 PFLOP/s: 864 tiles are 3.4
+// rounds of the card), POLY 261 us, STEP 475 us: 412 GFLOP are 300 us of that
+// and the 1.0 GB that its epilogue reads and writes the rest, one after the
+// other, since all blocks of a round end together.  (Two blocks a CU with
+// tiles of 256 x 128 do not overlap them either: 488 us against 483 in a copy
+// of the loop.)  Small matrices are bound by launches, 4 to 6 us each, most of
+// it the way of the first operands from another XCD's writes.
 template <int BT, int WM, int WN, bool SPLIT, int EPI, bool SHARED = false>
 __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
   constexpr int NW = BT / WM * (BT / WN);
@@ -644,7 +658,9 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
   // after some steps X <- P X with P the product of the q(A): all are polynomials of the first A, symmetric and
   // commuting.  P is formed here, and X read and written once for all of them.  A place in LDS holds a matrix as
   // operands (two panels, both halves, zero diagonal, times the scale) and its diagonal in FP32; of what a product
-  // gives, the lower triangle is kept and mirrored (left unsymmetric, the rounding grows from step to step).
+  // gives, the lower triangle is kept and mirrored (left unsymmetric, the rounding grows from step to step).  One
+  // block a matrix is slow at it, about 1.9 us a product, but nine products are three steps, and those were a launch
+  // of 4 us for X and one of 8 us for A and B each: 3 x (64 x 576) take 58 us so, 69 step by step.
   __shared__ float diagonal[EPI == BOTH ? 4 : 1][EPI == BOTH ? BT : 1];
   if constexpr (EPI == BOTH) {
     static_assert(BT == 64 && SPLIT && kStages == 4, "a matrix takes the place of a stage");

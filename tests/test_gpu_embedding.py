@@ -151,8 +151,8 @@ def test_grad_is_the_lookups():
     nf.nf_embedding_lookup(table + h * way, ids, up, scale=3.0)
     nf.nf_embedding_lookup(table - h * way, ids, down, scale=3.0)
     rows = torch.empty(1, V * d, device=DEV)
-    nf.nf_embedding_grad(c[None], ids[None], rows, 0, V, nf.empty_workspace(nf.nf_embedding_workspace_bytes(1, T, V, d)),
-                         scale=3.0)
+    ws = nf.empty_workspace(nf.nf_embedding_workspace_bytes(1, T, V, d))
+    nf.nf_embedding_grad(c[None], ids[None], rows, 0, V, ws, scale=3.0)
     by_difference = float((c.double() * (up.double() - down.double())).sum() / (2 * h))
     by_gradient = float((rows.view(V, d).double() * way.double()).sum())
     # every product and sum rounded once: 2^-24 of their absolute values, some tokens a row

@@ -155,7 +155,8 @@ def test_steps_and_coefficients(steps, coef, products):
 @pytest.mark.parametrize("dst", ["bf16", "f32"])
 @pytest.mark.parametrize("products", BOTH)
 @pytest.mark.parametrize("kind", ["gauss", "decay"])
-@pytest.mark.parametrize("batch,m,n", [(12, 100, 4000), (3, 6001, 150), (1, 64, 20_000), (30, 30, 2000), (2, 300, 5000)])
+@pytest.mark.parametrize("batch,m,n", [(12, 100, 4000), (3, 6001, 150), (1, 64, 20_000), (30, 30, 2000),
+                                       (2, 300, 5000)])
 def test_long_sides(batch, m, n, kind, products, dst):
     """Where several steps are taken at once by the Gram matrix, and a tile's k by several blocks."""
     u = torch.from_numpy(make(kind, m, n, m + n, batch)).float().to(DEV)

@@ -88,7 +88,8 @@ def test_orthogonal():
         (INVALID, {1: 3}), (INVALID, {5: -1}), (INVALID, {2: 29}), (INVALID, {3: 1199}), (INVALID, {6: 29}),
         (INVALID, {7: 1199}), (INVALID, {8: -1}), (INVALID, {9: -1}), (INVALID, {10: -1}), (INVALID, {0: None}),
         (INVALID, {4: None}), (ALIGN, {0: P(0x1002)}), (ALIGN, {4: ODD}), (ALIGN, {12: P(0x100010)}),
-        (UNSUPPORTED, {8: (1 << 17) + 1, 3: BIG, 7: BIG}), (UNSUPPORTED, {9: (1 << 17) + 1, 2: BIG, 3: BIG, 6: BIG, 7: BIG}),
+        (UNSUPPORTED, {8: (1 << 17) + 1, 3: BIG, 7: BIG}),
+        (UNSUPPORTED, {9: (1 << 17) + 1, 2: BIG, 3: BIG, 6: BIG, 7: BIG}),
         (UNSUPPORTED, {10: 65536}), (WORKSPACE, {13: need - 1}), (WORKSPACE, {12: None})])
     for k in (8, 9, 10):
         args = list(good)
