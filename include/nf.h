@@ -621,7 +621,7 @@ enum { NF_TYPE_F32 = 0, NF_TYPE_BF16 = 1, NF_TYPE_F16 = 2 };
  * The product is taken in FP32.  table is V rows of d elements, table_ld
  * apart; out is T rows, out_ld apart; both of any NF_TYPE_*, aligned to
  * their elements.  ids: int32 (ids_bytes = 4) or int64 (8).  T = 0 or d = 0
- * launches nothing.  NF_ERR_INVALID_ARG: V, T, d < 0, d > 2^24, T > 2^31 - 1,
+ * launches nothing.  NF_ERR_INVALID_ARG: V, T, d < 0, d > 2^23, T > 2^31 - 1,
  * table_ld or out_ld < d, unknown types.
  */
 nf_status nf_embedding_lookup(const void* table, int32_t table_type, int64_t table_ld, int64_t V, int64_t d,
@@ -643,7 +643,7 @@ nf_status nf_embedding_lookup(const void* table, int32_t table_type, int64_t tab
  * offset in it), 4-byte aligned.  dy[w] is T rows dy_ld apart, workers
  * dy_stride elements apart; ids rows ids_stride apart.
  * NF_ERR_INVALID_ARG: W outside [1, 255]; V < 0 or > 2^31 - 1; T < 0 or
- * > 2^24; d < 0 or > 2^24; dy_ld < d; dy_stride < (T - 1) * dy_ld + d or
+ * > 2^24; d < 0 or > 2^23; dy_ld < d; dy_stride < (T - 1) * dy_ld + d or
  * ids_stride < T with W > 1; worker_stride < V * d with W > 1.
  */
 size_t nf_embedding_workspace_bytes(int32_t W, int64_t T, int64_t V, int64_t d);
@@ -683,8 +683,8 @@ typedef struct {
  * rows src_ld (dst_ld) and matrices src_stride (dst_stride) elements apart,
  * of any NF_TYPE_*, aligned to their elements; dst may be src.
  * NF_ERR_INVALID_ARG: sizes < 0, ld < cols, a stride < (rows-1)*ld + cols with
- * batch > 1, bad parameters.  NF_ERR_UNSUPPORTED: a side > 2^17 or more than
- * 2^30 tiles of work.  rows, cols or batch = 0 launches nothing.
+ * batch > 1, bad parameters.  NF_ERR_UNSUPPORTED: a side > 2^17, batch >
+ * 65535 or more than 2^23 pieces of 64 x 64.  rows, cols or batch = 0 launches nothing.
  */
 size_t nf_orthogonal_workspace_bytes(int64_t rows, int64_t cols, int64_t batch,
                                      const nf_orthogonal_params* params_host);

@@ -632,12 +632,16 @@ def _type(t, name):
     return code
 
 
+_ID_BYTES = {} if torch is None else {torch.int32: 4, torch.int64: 8}
+
+
 def _ids(t, name="ids"):
-    if t.dtype not in (torch.int32, torch.int64):
+    size = _ID_BYTES.get(t.dtype)
+    if size is None:
         raise ValueError(f"{name} must be int32 or int64, got {t.dtype}")
-    if t.numel() > 1 and t.stride(-1) != 1:
+    if t.dim() == 0 or (t.stride(-1) != 1 and t.numel() > 1):
         raise ValueError(f"{name} must have unit stride in the last dimension")
-    return _dev_ptr(t, None, name), t.element_size()
+    return _dev_ptr(t, None, name), size
 
 
 def _rows_of(t, name):
@@ -668,10 +672,12 @@ def nf_embedding_lookup(table, ids, out, scale=1.0, stream=None):
     tp, tld = _rows_of(table, "table")
     op, old = _rows_of(out, "out")
     ip, ibytes = _ids(ids)
-    if ids.dim() != 1 or tuple(out.shape) != (ids.shape[0], table.shape[1]):
-        raise ValueError(f"out must be [{ids.numel()}, {table.shape[1]}] and ids one-dimensional")
-    _check(load().nf_embedding_lookup(tp, _type(table, "table"), tld, table.shape[0], table.shape[1], ip, ibytes,
-                                      ids.shape[0], float(scale), op, _type(out, "out"), old, _stream(stream)))
+    V, d = table.shape
+    T = ids.numel()
+    if ids.dim() != 1 or out.shape != (T, d):
+        raise ValueError(f"out must be [{T}, {d}] and ids one-dimensional")
+    _check(load().nf_embedding_lookup(tp, _type(table, "table"), tld, V, d, ip, ibytes, T, scale, op,
+                                      _type(out, "out"), old, _stream(stream)))
 
 
 def nf_embedding_workspace_bytes(W, T, V, d):
@@ -685,16 +691,16 @@ def nf_embedding_grad(dy, ids, grads, offset, V, ws, scale=1.0, padding_id=-1, a
     g, stride, W = _rows(grads)
     if dy.dim() != 3 or (dy.shape[2] > 1 and dy.stride(2) != 1):
         raise ValueError("dy must be [W, T, d] with unit stride in the last dimension")
-    T, d = dy.shape[1:]
+    workers, T, d = dy.shape
     ip, ibytes = _ids(ids)
-    if dy.shape[0] != W or tuple(ids.shape) != (W, T):
+    if workers != W or ids.shape != (W, T):
         raise ValueError(f"dy must be [{W}, T, d] and ids [{W}, T], got {tuple(dy.shape)} and {tuple(ids.shape)}")
     if offset < 0 or V < 0 or offset + V * d > grads.shape[1]:
         raise ValueError(f"the table's segment [{offset}, {offset + V * d}) exceeds the rows of {grads.shape[1]}")
     ld = dy.stride(1) if T > 1 else max(d, 1)
     _check(load().nf_embedding_grad(_dev_ptr(dy, None, "dy"), _type(dy, "dy"), ld,
                                     dy.stride(0) if W > 1 else T * ld, ip, ibytes, ids.stride(0) if W > 1 else T,
-                                    W, T, V, d, float(scale), int(padding_id), int(bool(accumulate)),
+                                    W, T, V, d, scale, padding_id, 1 if accumulate else 0,
                                     g + 4 * offset, stride, _dev_ptr(ws, torch.uint8, "ws"), ws.numel(),
                                     _stream(stream)))
 

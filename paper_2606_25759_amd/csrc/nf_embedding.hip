@@ -52,24 +52,24 @@ template <typename A, typename B, int N>
 __global__ __launch_bounds__(kThreadsE) void k_lookup(LookupArgs a) {
   const int tx = 1 << a.lg_tx, ty = kThreadsE >> a.lg_tx;
   const int x = threadIdx.x & (tx - 1);
-  const int64_t t = (int64_t)blockIdx.x * ty + (threadIdx.x >> a.lg_tx);
-  if (t >= a.T) return;
-  const int64_t id = id_at(a.ids, a.ids64, t);
-  const bool in = id >= 0 && id < a.V;
-  const A* row = (const A*)a.table + (in ? id : 0) * a.table_ld;
-  B* out = (B*)a.out + t * a.out_ld;
-  for (int j = x * N; j < a.d; j += tx * N) {
-    const int at = min(j, a.d - N);
-    Near<B, N> o;
-    if (in) {
-      const Near<A, N> p = *(const Near<A, N>*)(row + at);
+  for (int64_t t = (int64_t)blockIdx.x * ty + (threadIdx.x >> a.lg_tx); t < a.T; t += (int64_t)gridDim.x * ty) {
+    const int64_t id = id_at(a.ids, a.ids64, t);
+    const bool in = id >= 0 && id < a.V;
+    const A* row = (const A*)a.table + (in ? id : 0) * a.table_ld;
+    B* out = (B*)a.out + t * a.out_ld;
+    for (int j = x * N; j < a.d; j += tx * N) {
+      const int at = min(j, a.d - N);
+      Near<B, N> o;
+      if (in) {
+        const Near<A, N> p = *(const Near<A, N>*)(row + at);
 #pragma unroll
-      for (int e = 0; e < N; ++e) o.v[e] = from_f32<B>(to_f32(p.v[e]) * a.scale);
-    } else {
+        for (int e = 0; e < N; ++e) o.v[e] = from_f32<B>(to_f32(p.v[e]) * a.scale);
+      } else {
 #pragma unroll
-      for (int e = 0; e < N; ++e) o.v[e] = from_f32<B>(0.0f);
+        for (int e = 0; e < N; ++e) o.v[e] = from_f32<B>(0.0f);
+      }
+      *(Near<B, N>*)(out + at) = o;
     }
-    *(Near<B, N>*)(out + at) = o;
   }
 }
 
@@ -274,19 +274,20 @@ __global__ __launch_bounds__(kThreadsE) void k_merge(GradArgs a) {
 
 // ---------------------------------------------------------------- the sums
 
-// A block's columns are an even share of a row's, N adjacent ones a lane (four;
-// one where rows have fewer than four); the last lane that has any takes the
-// last N (its neighbour may have some of them too, and comes to the same
-// values), so that no access needs a condition.
+// A block's columns are an even share of a row's groups of N (four; one where
+// rows have fewer), a group a lane.  The row's last group is its last N
+// columns, some of which its neighbour in the same wavefront may have too, and
+// comes to the same values: no access needs a condition.  (A share has 32
+// groups at least where there are several, so the neighbour is in it.)
 struct Columns {
   int at;     // of this lane
   bool mine;  // false: `at` is another lane's too, and this one stores nothing
 };
 template <int N>
 __device__ __forceinline__ Columns columns_of(int d, int lane) {
-  const int width = ((d + gridDim.y - 1) / gridDim.y + N - 1) / N * N;
-  const int end = min((int)(blockIdx.y + 1) * width, d), c = blockIdx.y * width + N * lane;
-  return {max(min(c, end - N), 0), c < end};
+  const int64_t groups = (d + N - 1) / N;
+  const int begin = (int)(groups * blockIdx.y / gridDim.y), end = (int)(groups * (blockIdx.y + 1) / gridDim.y);
+  return {min(min(begin + lane, end - 1) * N, d - N), begin + lane < end};
 }
 
 template <typename D, int N>
@@ -501,13 +502,13 @@ nf_status finish(hipError_t e) {
   return set_error(NF_OK, "");
 }
 
-constexpr int64_t kMaxD = 1 << 24, kMaxT = 1 << 24, kMaxInt = 0x7fffffff;
+constexpr int64_t kMaxD = 1 << 23, kMaxT = 1 << 24, kMaxInt = 0x7fffffff;
 
 const char* check_grad_sizes(int32_t W, int64_t T, int64_t V, int64_t d) {
   if (W < 1 || W > 255) return "W outside [1, 255]";
   if (T < 0 || T > kMaxT) return "T outside [0, 2^24]";
   if (V < 0 || V > kMaxInt) return "V outside [0, 2^31)";
-  if (d < 0 || d > kMaxD) return "d outside [0, 2^24]";
+  if (d < 0 || d > kMaxD) return "d outside [0, 2^23]";
   return nullptr;
 }
 
@@ -563,7 +564,8 @@ nf_status nf_embedding_lookup(const void* table, int32_t table_type, int64_t tab
   LookupArgs a = {table, ids, out, table_ld, out_ld, V, T, (int32_t)d, ids_bytes == 8, scale, 0};
   const int each = d < 8 ? 1 : 8;
   while (a.lg_tx < 8 && (each << a.lg_tx) < d) ++a.lg_tx;
-  const unsigned blocks = (unsigned)ceil_div(T, kThreadsE >> a.lg_tx);
+  const int64_t most = 1 << 22, want = ceil_div(T, kThreadsE >> a.lg_tx);  // a launch has under 2^32 threads
+  const unsigned blocks = (unsigned)(want < most ? want : most);
   hipStream_t s = static_cast<hipStream_t>(stream);
   with_type(table_type, [&](auto* tp) {
     with_type(out_type, [&](auto* op) {

@@ -115,6 +115,13 @@ def test_grad_one_id(T):
         check_grad(1, T, 9, 260, "f16", ids=ids, seed=first)
 
 
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("d", [255, 257, 511, 513, 1023, 16_385, 25_345, 50_945])
+def test_grad_wide_rows(d, accumulate):
+    """Rows of many blocks' columns, of which the last may have a single one more than whole blocks do."""
+    check_grad(2, 300, 3, d, lead=1, accumulate=accumulate, seed=d)
+
+
 @pytest.mark.parametrize("kind", [torch.int32, torch.int64])
 def test_grad_padding_and_outside(kind):
     g = torch.Generator().manual_seed(2)
