@@ -18,6 +18,11 @@
 // flops: A and A A are symmetric, so tiles on and below the diagonal are
 // computed and mirrored.
 //
+// Long sides take a few steps at once.  With q(A) = a + b A + c A A a step is
+// X <- q(A) X, and A <- q(A) A q(A): after some steps X <- P X with P, the
+// product of the q(A), from m x m matrices alone (MULT, BOTH), so that X is
+// read and written once for all of them.
+//
 // Operands lie in panels of 32 k: element (row, k) of a matrix of R rows is
 // at ((k / 32) R + row) 32 + k % 32.  A stage's BT rows are then one
 // contiguous piece of memory, whole cache lines, whatever the tile.
@@ -138,6 +143,9 @@ __device__ __forceinline__ float4v load_four(const View& g, int64_t off, int64_t
   if (g.type == NF_TYPE_BF16) return load_four<Bf16>(g.p, off, c, n);
   return load_four<_Float16>(g.p, off, c, n);
 }
+
+// The number that a pair of halves holds (as a product and sum: one instruction that takes both as FP16).
+__device__ __forceinline__ float pair(_Float16 h, _Float16 l) { return fmaf((float)h, 1.0f, (float)l); }
 
 // Where (row, k) of a matrix of R rows lies.
 __device__ __forceinline__ int64_t panel_at(int64_t row, int64_t k, int64_t R) {
@@ -302,13 +310,11 @@ __device__ __forceinline__ void load_tile(const _Float16* src, _Float16* lds, in
   }
 }
 
-template <int N>
-__device__ __forceinline__ void wait_loads() {  // until at most N of this wavefront's are under way
-  if (N == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  if (N == 2) asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
-  if (N == 4) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
-  if (N == 8) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
-  static_assert(N == 0 || N == 2 || N == 4 || N == 8, "");
+// Until at most N of this wavefront's loads into LDS, and R of its reads of LDS, are under way.
+template <int N, int R>
+__device__ __forceinline__ void wait_for() {
+  static_assert(N >= 0 && N < 64 && R >= 0 && R < 16, "the counters' ranges");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(%1)" ::"n"(N), "n"(R) : "memory");
 }
 
 __device__ __forceinline__ void block_barrier() {
@@ -570,10 +576,13 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
       products(f.p[1], f.q[0]);
     }
   };
-  // Stage s: at most `flying` loads stay under way (those of stage s + 2).  Without branches, so that the compiler
-  // knows which reads are outstanding and waits for those of this stage only.
+  // Stage s: at most `flying` loads stay under way (those of stage s + 2), and of the reads only this stage's own: the
+  // products of stage s - 1, and with them the wait for its fragments, may be scheduled past the barrier, but its place
+  // is given away behind it.  Without branches, so that the compiler knows which reads are outstanding and waits for
+  // those of this stage only.
+  constexpr int READS = OPS / 2 * (MI + NJ);
   auto step = [&](auto flying, auto loads, int s, Frags& now, Frags& next) {
-    wait_loads<decltype(flying)::value>();
+    wait_for<decltype(flying)::value, READS>();
     block_barrier();
     if (decltype(loads)::value) load(s + 3);
     read(s + 1, next);
@@ -588,9 +597,9 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
   load(1);  // stages is even: sides are multiples of 64
   if (stages > 2) {
     load(2);
-    wait_loads<2 * LOADS>();
+    wait_for<2 * LOADS, 0>();
   } else {
-    wait_loads<LOADS>();
+    wait_for<LOADS, 0>();
   }
   block_barrier();
   read(0, f0);
@@ -657,60 +666,50 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
   // BOTH: the steps of A = X X^T in LDS.  With q(A) = a + b A + c A A a step is X <- q(A) X, so A <- q(A) A q(A), and
   // after some steps X <- P X with P the product of the q(A): all are polynomials of the first A, symmetric and
   // commuting.  P is formed here, and X read and written once for all of them.  A place in LDS holds a matrix as
-  // operands (two panels, both halves, zero diagonal, times the scale) and its diagonal in FP32; of what a product
-  // gives, the lower triangle is kept and mirrored (left unsymmetric, the rounding grows from step to step).  One
-  // block a matrix is slow at it, about 1.9 us a product, but nine products are three steps, and those were a launch
-  // of 4 us for X and one of 8 us for A and B each: 3 x (64 x 576) take 58 us so, 69 step by step.
-  __shared__ float diagonal[EPI == BOTH ? 4 : 1][EPI == BOTH ? BT : 1];
+  // operands (two panels, both halves, times the scale); of what a product gives, the lower triangle is kept and
+  // mirrored (left unsymmetric, the rounding grows from step to step).  One block a matrix is slow at it, but nine
+  // products are three steps, and those were a launch of 4 us for X and one of 8 us for A and B each: 3 x (64 x 576)
+  // took 69 us step by step.
   if constexpr (EPI == BOTH) {
     static_assert(BT == 64 && SPLIT && kStages == 4, "a matrix takes the place of a stage");
     enum { kA, kZ, kP, kR };
-    auto place = [&](int m, int half, int c, int r) {  // rows r .. r + 7 of column c
-      return &lds[m][2 * half + r / kBK][c * kBK + ((r % kBK / 8) ^ swizzle(c)) * 8];
+    const int r = (int)row_at(0), cq = (int)column_at(0) - lane % 4;  // rows r .. r + 7 of columns cq .. cq + 7
+    auto place = [&](int m, int half, int c, int row) {               // rows row .. row + 7 of column c
+      return (half8*)&lds[m][2 * half + row / kBK][c * kBK + ((row % kBK / 8) ^ swizzle(c)) * 8];
     };
     auto put = [&](int m) {  // acc, which holds the matrix times the scale
+      half8 h[2], l[2];
 #pragma unroll
-      for (int j = 0; j < NJ; j += 2) {
-        const int r = (int)row_at(0), cq = (int)column_at(j) - lane % 4;
-        half8 h[2], l[2];
+      for (int y = 0; y < 2; ++y) {
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const int c = (int)column_at(j + y);
+        for (int e = 0; e < 8; ++e) {
+          const float v = acc[e / 4][y][e % 4];
+          h[y][e] = (_Float16)v;
+          l[y][e] = (_Float16)(v - (float)h[y][e]);
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const half8 th = transpose8(h[0], h[1], x, lane), tl = transpose8(l[0], l[1], x, lane);
+        const int c = cq + 4 * x + lane % 4;  // of this lane, and, where r = cq, the row that th is of
+        if (r > cq) {
+          *place(m, 0, c, r) = h[x];
+          *place(m, 1, c, r) = l[x];
+          *place(m, 0, r + 4 * x + lane % 4, cq) = th;
+          *place(m, 1, r + 4 * x + lane % 4, cq) = tl;
+        } else if (r == cq) {
+          half8 sh, sl;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            float v = acc[e / 4][j + y][e % 4];
-            if (r + e == c) {
-              diagonal[m][c] = v;
-              v = 0.0f;
-            }
-            h[y][e] = (_Float16)v;
-            l[y][e] = (_Float16)(v - (float)h[y][e]);
+            sh[e] = r + e >= c ? h[x][e] : th[e];
+            sl[e] = r + e >= c ? l[x][e] : tl[e];
           }
-        }
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const half8 th = transpose8(h[0], h[1], x, lane), tl = transpose8(l[0], l[1], x, lane);
-          const int c = cq + 4 * x + lane % 4;  // of this lane, and, where r = cq, the row that th is of
-          if (r > cq) {
-            *(half8*)place(m, 0, c, r) = h[x];
-            *(half8*)place(m, 1, c, r) = l[x];
-            *(half8*)place(m, 0, r + 4 * x + lane % 4, cq) = th;
-            *(half8*)place(m, 1, r + 4 * x + lane % 4, cq) = tl;
-          } else if (r == cq) {
-            half8 sh, sl;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              sh[e] = r + e >= c ? h[x][e] : th[e];
-              sl[e] = r + e >= c ? l[x][e] : tl[e];
-            }
-            *(half8*)place(m, 0, c, r) = sh;
-            *(half8*)place(m, 1, c, r) = sl;
-          }
+          *place(m, 0, c, r) = sh;
+          *place(m, 1, c, r) = sl;
         }
       }
     };
-    // acc = alpha Y + beta Z Y:  (D + O)(D' + O') = D D' + D O' + O D' + O O'
-    auto combine = [&](int z, int y, float alpha, float beta) {
+    auto combine = [&](int z, int y, float alpha, float beta) {  // acc = alpha Y + beta Z Y
 #pragma unroll
       for (int j = 0; j < NJ; ++j) acc[0][j] = acc[1][j] = float4v{};
 #pragma unroll
@@ -720,18 +719,10 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
       }
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        const int r = (int)row_at(0), c = (int)column_at(j);
-        const half8 zh = *(const half8*)place(z, 0, c, r), zl = *(const half8*)place(z, 1, c, r);
-        const half8 yh = *(const half8*)place(y, 0, c, r), yl = *(const half8*)place(y, 1, c, r);
-        const float dy = diagonal[y][c];
+        const half8 yh = *place(y, 0, cq + 4 * j + lane % 4, r), yl = *place(y, 1, cq + 4 * j + lane % 4, r);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float dz = diagonal[z][r + e];
-          const float oz = (float)zh[e] + (float)zl[e], oy = (float)yh[e] + (float)yl[e];
-          float v = fmaf(dz, oy, fmaf(oz, dy, acc[e / 4][j][e % 4]));
-          if (r + e == c) v = fmaf(dz, dy, v);
-          acc[e / 4][j][e % 4] = fmaf(beta * kInvScale, v, alpha * (r + e == c ? dy : oy));
-        }
+        for (int e = 0; e < 8; ++e)
+          acc[e / 4][j][e % 4] = fmaf(beta * kInvScale, acc[e / 4][j][e % 4], alpha * pair(yh[e], yl[e]));
       }
     };
 #pragma unroll
@@ -747,7 +738,7 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if (row_at(0) + e == column_at(j)) acc[e / 4][j][e % 4] += a.coef[0][0] * kScale;
+            if (r + e == cq + 4 * j + lane % 4) acc[e / 4][j][e % 4] += a.coef[0][0] * kScale;
         put(kP);
       }
       __syncthreads();
@@ -765,15 +756,21 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
       }
       __syncthreads();
     }
-    // P's columns, to go where B goes
+    // P goes where B goes, its diagonal apart
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const int r = (int)row_at(0), c = (int)column_at(j);
-      const half8 h = *(const half8*)place(kP, 0, c, r), l = *(const half8*)place(kP, 1, c, r);
+      const int c = cq + 4 * j + lane % 4;
+      half8 h = *place(kP, 0, c, r), l = *place(kP, 1, c, r);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (r + e == c) {
+          a.dB[b * a.Mp + c] = pair(h[e], l[e]) * kInvScale;
+          h[e] = l[e] = (_Float16)0.0f;
+        }
+      }
       const int64_t at = b * a.ostride + panel_at(c, r, a.Mp);
       *(half8*)(a.oh + at) = h;
       *(half8*)(a.ol + at) = l;
-      if (r <= c && c < r + 8) a.dB[b * a.Mp + c] = diagonal[kP][c] * kInvScale;
     }
     return;
   }
@@ -823,7 +820,7 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
         if (EPI == POLY) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float o = (float)h[e] + (float)l[e];
+            const float o = pair(h[e], l[e]);
             // (D + O)^2 = D^2 + D O + O D + O O
             v[y][e] = fmaf(a.c, fmaf(dr[e / 4][e % 4] + dc, o, d[e] * kInvScale), a.b * o);
             if (r + e == c) {
@@ -836,7 +833,7 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
         } else if (EPI == MULT) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float o = (float)h[e] + (float)l[e], z = (float)zh[e] + (float)zl[e], dz = dr[e / 4][e % 4];
+            const float o = pair(h[e], l[e]), z = pair(zh[e], zl[e]), dz = dr[e / 4][e % 4];
             v[y][e] = fmaf(dz, o, fmaf(z, dc, d[e] * kInvScale)) + a.a * o;
             if (r + e == c) {
               a.dB[b * a.Mp + c] = fmaf(dz, dc, d[e] * kInvScale * kInvScale) + a.a * dc;
@@ -846,7 +843,7 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
         } else {  // rows are the long side, columns the short one
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float hi = (float)h[e], x = hi + (float)l[e];
+            const float hi = (float)h[e], x = pair(h[e], l[e]);
             v[y][e] = fmaf(a.a, x, fmaf(dc, SPLIT || EPI == LAST ? x : hi, d[e] * kInvScale));
           }
         }
@@ -1306,7 +1303,8 @@ const char* check_sizes(int64_t rows, int64_t cols, int64_t batch) {
 
 bool too_large(int64_t rows, int64_t cols, int64_t batch) {
   if (rows > kMaxSide || cols > kMaxSide || batch > 65535) return true;
-  return ceil_div(rows, 64) * ceil_div(cols, 64) > (1ll << 30) / (batch > 0 ? batch : 1);
+  // a launch has under 2^32 threads
+  return ceil_div(rows, 64) * ceil_div(cols, 64) > (1ll << 23) / (batch > 0 ? batch : 1);
 }
 
 nf_status check_view(const void* p, int32_t type, int64_t ld, int64_t stride, int64_t rows, int64_t cols, int64_t batch,
