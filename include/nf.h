@@ -674,9 +674,9 @@ typedef struct {
  * with X X^T on the shorter side (X^T X and X (...) where rows > cols: the
  * same matrix).  The norm is an FP64 sum.  A matrix with a NaN or an
  * infinity gives NaN everywhere; other matrices of the batch are unaffected.
- * Coefficients must keep the squares of the singular values of X, and the
- * norm of b A + c A A, below 60, as any that converge do: products beyond the
- * range of FP16 give NaN.  Steps may be taken together, as X <- P X with P the
+ * Coefficients must keep |a|, the squares of the singular values of X, and the
+ * norm of b A + c A A, with a or without it, below 60, as any that converge
+ * do: products beyond the range of FP16 give NaN.  Steps may be taken together, as X <- P X with P the
  * product of their a + b A + c A A, where that is sooner and not less exact
  * than is said above.
  * src and dst: `batch` matrices of rows x cols, elements of a row adjacent,
