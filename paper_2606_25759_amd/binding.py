@@ -639,7 +639,7 @@ def _ids(t, name="ids"):
     size = _ID_BYTES.get(t.dtype)
     if size is None:
         raise ValueError(f"{name} must be int32 or int64, got {t.dtype}")
-    if t.dim() == 0 or (t.stride(-1) != 1 and t.numel() > 1):
+    if t.dim() == 0 or (t.shape[-1] > 1 and t.stride(-1) != 1):
         raise ValueError(f"{name} must have unit stride in the last dimension")
     return _dev_ptr(t, None, name), size
 

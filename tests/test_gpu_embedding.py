@@ -202,3 +202,17 @@ def test_segment_past_32_bits(accumulate):
     assert bool((seg[1_048_576] == 3 + base).all()) and bool((seg[1_048_575] == base).all())
     assert bool((seg[V - 2] == base).all()) and bool((rows[0, lead + V * d:] == 2.0).all())
     assert bool((rows[0, :lead] == 2.0).all())
+
+
+def test_grad_one_token_each():
+    """A dimension of one element has any stride: [W, 1] as the transpose of [1, W]."""
+    W, V, d = 3, 7, 20
+    ids = torch.tensor([[4, 0, 4]], device=DEV).t()
+    assert ids.stride(-1) != 1
+    dy = torch.randn(W, 1, d, device=DEV)
+    rows = torch.full((W, V * d), float("nan"), device=DEV)
+    nf.nf_embedding_grad(dy, ids, rows, 0, V, nf.empty_workspace(nf.nf_embedding_workspace_bytes(W, 1, V, d)))
+    want = torch.zeros(W, V, d, device=DEV)
+    for w, i in enumerate((4, 0, 4)):
+        want[w, i] = dy[w, 0]
+    assert torch.equal(rows.view(W, V, d), want)
