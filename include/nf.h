@@ -693,6 +693,25 @@ nf_status nf_orthogonalize(const void* src, int32_t src_type, int64_t src_ld, in
                            int64_t batch, const nf_orthogonal_params* params_host, void* ws, size_t ws_bytes,
                            void* stream);
 
+/*
+ * Profiling query (no paper counterpart): the product kernels that
+ * nf_orthogonalize runs for these sizes into a result of dst_type;
+ * nf_orthogonal_update runs those of a 16-bit dst_type whatever its weights'
+ * type.  All zeros where nothing is launched.  Errors as for
+ * nf_orthogonalize.  Pure host function.
+ */
+typedef struct {
+  int32_t split;      /* products of 22-bit operands                           */
+  int32_t step_tile;  /* side of the tiles of X's products: 64, 128 or 256     */
+  int32_t gram_tile;  /* of A = X X^T                                          */
+  int32_t poly_tile;  /* of b A + c A A, and of what else is m x m             */
+  int32_t shares;     /* blocks that share a tile of A                         */
+  int32_t rounds;     /* products with X: one a step, or one for a few steps   */
+  int32_t squares;    /* launches of products of m x m                         */
+} nf_orthogonal_path_info;
+nf_status nf_orthogonal_path(int64_t rows, int64_t cols, int64_t batch, const nf_orthogonal_params* params_host,
+                             int32_t dst_type, nf_orthogonal_path_info* info_host);
+
 /* The step around it. */
 typedef struct {
   float lr;            /* finite                                               */

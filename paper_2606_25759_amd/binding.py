@@ -41,7 +41,7 @@ EXPORTS = ["nf_abi_version", "nf_last_error", "nf_mask_from_segments", "nf_works
            "nf_sliced_layout_sizes", "nf_sliced_layout", "nf_compact_signs", "nf_slice_workspace_bytes",
            "nf_slice_scales", "nf_compact_signcount_reduce",
            "nf_embedding_lookup", "nf_embedding_workspace_bytes", "nf_embedding_grad",
-           "nf_orthogonal_workspace_bytes", "nf_orthogonalize", "nf_orthogonal_update"]
+           "nf_orthogonal_workspace_bytes", "nf_orthogonal_path", "nf_orthogonalize", "nf_orthogonal_update"]
 NF_TYPE_F32, NF_TYPE_BF16, NF_TYPE_F16 = 0, 1, 2
 NF_PRODUCTS_SINGLE, NF_PRODUCTS_SPLIT = 0, 1
 NF_ORTHOGONAL_MAX_STEPS = 12
@@ -96,6 +96,11 @@ class nf_endpoint_model(ctypes.Structure):
 class nf_orthogonal_params(ctypes.Structure):
     _fields_ = [("products", ctypes.c_int32), ("steps", ctypes.c_int32), ("eps", ctypes.c_float),
                 ("coef", ctypes.c_float * 3 * NF_ORTHOGONAL_MAX_STEPS)]
+
+
+class nf_orthogonal_path_info(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("split", "step_tile", "gram_tile", "poly_tile", "shares", "rounds",
+                                              "squares")]
 
 
 class nf_matrix_step(ctypes.Structure):
@@ -186,6 +191,7 @@ def load(path=None):
         "nf_embedding_grad": (ctypes.c_int, [_P, _I32, _I64, _I64, _P, _I32, _I64, _I32, _I64, _I64, _I64,
                                              ctypes.c_float, _I64, _I32, _P, _I64, _P, _SZ, _P]),
         "nf_orthogonal_workspace_bytes": (_SZ, [_I64, _I64, _I64, _P]),
+        "nf_orthogonal_path": (ctypes.c_int, [_I64, _I64, _I64, _P, _I32, _P]),
         "nf_orthogonalize": (ctypes.c_int, [_P, _I32, _I64, _I64, _P, _I32, _I64, _I64, _I64, _I64, _I64, _P, _P,
                                             _SZ, _P]),
         "nf_orthogonal_update": (ctypes.c_int, [_P, _I32, _I64, _I64, _P, _I64, _I64, _P, _I32, _I64, _I64, _I64,
@@ -723,6 +729,13 @@ def matrix_step(lr, momentum=0.95, nesterov=True, weight_decay=0.0, scale=1.0):
 
 def nf_orthogonal_workspace_bytes(rows, cols, batch, params):
     return int(load().nf_orthogonal_workspace_bytes(rows, cols, batch, ctypes.byref(params)))
+
+
+def nf_orthogonal_path(rows, cols, batch, params, dst_type=NF_TYPE_BF16):
+    """The product kernels that a call of these sizes runs (profiling)."""
+    info = nf_orthogonal_path_info()
+    _check(load().nf_orthogonal_path(rows, cols, batch, ctypes.byref(params), dst_type, ctypes.byref(info)))
+    return info
 
 
 def nf_orthogonalize(src, dst, params, ws, stream=None):

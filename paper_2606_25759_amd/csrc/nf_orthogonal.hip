@@ -1343,6 +1343,30 @@ size_t nf_orthogonal_workspace_bytes(int64_t rows, int64_t cols, int64_t batch, 
   return fine > coarse ? fine : coarse;
 }
 
+nf_status nf_orthogonal_path(int64_t rows, int64_t cols, int64_t batch, const nf_orthogonal_params* params,
+                             int32_t dst_type, nf_orthogonal_path_info* info) {
+  using namespace nf;
+  if (!info) return bad("info is NULL");
+  *info = nf_orthogonal_path_info{};
+  if (const char* w = check_params(params)) return bad(w);
+  if (const char* w = check_sizes(rows, cols, batch)) return bad(w);
+  if (!known_type(dst_type)) return bad("unknown element type");
+  if (too_large(rows, cols, batch)) return set_error(NF_ERR_UNSUPPORTED, "matrices too large");
+  if (rows == 0 || cols == 0 || batch == 0) return set_error(NF_OK, "");
+  const bool coarse = params->products == NF_PRODUCTS_SINGLE || dst_type != NF_TYPE_F32;
+  const Plan p = plan_of(rows, cols, batch, params->products == NF_PRODUCTS_SPLIT, coarse);
+  info->split = p.split;
+  info->step_tile = p.tile;
+  info->gram_tile = p.gram_tile;
+  info->poly_tile = p.poly_tile;
+  info->shares = p.shares;
+  for (int k = 0, taken = 1; k < params->steps; k += taken, ++info->rounds) {
+    if (p.m <= 64 || p.gram_space) taken = block_of(*params, k, coarse);
+    if (p.m > 64) info->squares += p.gram_space ? 4 * taken - 3 : 1;
+  }
+  return set_error(NF_OK, "");
+}
+
 nf_status nf_orthogonalize(const void* src, int32_t src_type, int64_t src_ld, int64_t src_stride, void* dst,
                            int32_t dst_type, int64_t dst_ld, int64_t dst_stride, int64_t rows, int64_t cols,
                            int64_t batch, const nf_orthogonal_params* params, void* ws, size_t ws_bytes,
