@@ -655,7 +655,8 @@ nf_status nf_embedding_grad(const void* dy, int32_t dy_type, int64_t dy_ld, int6
 /* How nf_orthogonalize forms its products: of operands rounded once to FP16
  * (11 bits), or each held as two FP16 numbers (22 bits, three products).  The
  * result is within about 2e-3 of the exact one relative to its norm, or within
- * about 1e-5 (FP32 products are no closer).  Sizes for which products are not
+ * about 1e-5 (FP32 products are no closer), however small ||G|| is against eps,
+ * down to the smallest numbers of the result's type.  Sizes for which products are not
  * what takes the time get the latter with NF_PRODUCTS_SINGLE as well. */
 enum { NF_PRODUCTS_SINGLE = 0, NF_PRODUCTS_SPLIT = 1 };
 #define NF_ORTHOGONAL_MAX_STEPS 12

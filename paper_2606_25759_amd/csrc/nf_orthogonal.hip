@@ -42,6 +42,9 @@
 //     the rounding of its large diagonal would be the largest error left.
 //   - B's diagonal multiplies the same rounded X as the rest of B does,
 //     except in the last step, after which nothing is amplified any more.
+// FP16 pairs keep 22 bits of what is well above their spacing of 2^-24.  Where
+// ||G|| is far below eps, X is far below one, and held times another power of
+// two a matrix and step (Steps); for all others that power is one.
 #include <math.h>
 #include <string.h>
 
@@ -76,6 +79,13 @@ struct View {
   int32_t type;
 };
 
+// A matrix's steps.  With X held times 2^e before a step and times 2^f after it, the same step has the coefficients
+// a 2^(f - e), b 2^(f - 3 e) and c 2^(f - 5 e).
+struct Steps {
+  float coef[NF_ORTHOGONAL_MAX_STEPS][3];
+  int32_t shift;  // the result is held times 2^shift
+};
+
 struct PrepArgs {
   View g;              // gradient or source
   float* mom;          // nullptr: U = g
@@ -89,6 +99,9 @@ struct PrepArgs {
   int32_t nparts;
   int32_t lg_tx;       // k_norm: log2 of the threads across a row, four elements each
   float eps;
+  int32_t steps;
+  float coef[NF_ORTHOGONAL_MAX_STEPS][3];
+  Steps* table;        // [batch]
   _Float16 *xh, *xl, *th, *tl;  // tl: split only
   int32_t* arrived;    // to be zeroed
   int64_t tiles;
@@ -99,9 +112,10 @@ struct ProdArgs {
   int64_t ldk;                        // k of both
   int64_t pstride, qstride;           // a matrix of the batch
   int32_t tm, tn;                     // tiles
-  float a, b, c;
+  const Steps* table;                 // [batch]
+  int32_t k;                          // the step, or the first of them
   int32_t steps;                      // BOTH: at most kBlock of them
-  float coef[kBlock][3];
+  int32_t whole;                      // STEP, LAST: Q is all that X is multiplied by (else a X is added)
   _Float16 *oh, *ol;                  // GRAM: A, POLY: B; STEP: X^T
   int64_t ostride;
   const _Float16 *ah, *al;            // POLY: A; MULT: Y (Z is P)
@@ -120,6 +134,30 @@ struct ProdArgs {
   uint64_t* part;                     // their sums, [tile][share][BT x BT], two FP32 a word
   int32_t* arrived;                   // [tile], zero between launches
 };
+
+// The power of two that X of a norm of at most u is held times: to [1/2, 1), and never down.
+__device__ __forceinline__ int shift_of(double u) {
+  int e = 0;
+  if (u > 0.0 && u < 0.5) frexp(u, &e);
+  return -e;
+}
+
+// The steps of a matrix that begins with the norm u.  No singular value grows by more than |a| + |b| u^2 + |c| u^4, and
+// neither does the norm.
+__device__ void steps_of(const PrepArgs& a, double u, Steps* to) {
+  int e = shift_of(u);
+  for (int k = 0; k < a.steps; ++k) {
+    const float* c = a.coef[k];
+    const double uu = u * u;
+    u = fmin(u * (fabs((double)c[0]) + uu * (fabs((double)c[1]) + uu * fabs((double)c[2]))), 0x1p100);
+    const int f = shift_of(u);
+    to->coef[k][0] = ldexpf(c[0], f - e);
+    to->coef[k][1] = ldexpf(c[1], f - 3 * e);
+    to->coef[k][2] = ldexpf(c[2], f - 5 * e);
+    e = f;
+  }
+  to->shift = e;
+}
 
 // Elements c .. c + 3 of n of a row, the first at p + off; zeros past the row's end.
 template <typename T>
@@ -225,8 +263,10 @@ __global__ __launch_bounds__(kNormThreads) void k_scale(PrepArgs a) {
   const int64_t b = blockIdx.z;
   double part = 0.0;
   for (int i = threadIdx.x; i < a.nparts; i += kNormThreads) part += a.part[b * a.nparts + i];
-  const double norm = sqrt(block_sum(part, s)) + (double)a.eps;
-  const double inv = norm > 0.0 || norm != norm ? (double)kScale / norm : 0.0;
+  const double size_of_u = sqrt(block_sum(part, s)), norm = size_of_u + (double)a.eps;
+  const double u = size_of_u / norm;  // of X
+  const double inv = norm > 0.0 || norm != norm ? ldexp((double)kScale, shift_of(u)) / norm : 0.0;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) steps_of(a, u, a.table + b);
   const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
   const int x = threadIdx.x % 16 * 4, y = threadIdx.x / 16;
   const int64_t size = a.Mp * a.Np;
@@ -398,7 +438,7 @@ __device__ __forceinline__ void store_eight(const ProdArgs& a, int64_t off, int6
 // cq + 4 y + lane % 4, times the scale.  Eight adjacent elements of a row of it are rows here, or, where it is tall,
 // columns.
 __device__ __forceinline__ void store_last(const ProdArgs& a, int64_t b, int64_t r, int64_t rq, int64_t cq, int lane,
-                                           float (&v)[2][8]) {
+                                           float scale, float (&v)[2][8]) {
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     float o[8];
@@ -408,11 +448,11 @@ __device__ __forceinline__ void store_last(const ProdArgs& a, int64_t b, int64_t
         float w[4] = {v[y][4 * x], v[y][4 * x + 1], v[y][4 * x + 2], v[y][4 * x + 3]};
         transpose4(w, lane);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[4 * y + e] = w[e] * kInvScale;
+        for (int e = 0; e < 4; ++e) o[4 * y + e] = w[e] * scale;
       }
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = v[x][e] * kInvScale;
+      for (int e = 0; e < 8; ++e) o[e] = v[x][e] * scale;
     }
     const int64_t row = a.tall ? rq + 4 * x : cq + 4 * x + lane % 4, col = a.tall ? cq : r;
     const int64_t rows = a.tall ? a.n : a.m, cols = a.tall ? a.m : a.n;
@@ -485,6 +525,17 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
   }
   const int wm = wave / (BT / WN) * WM, wn = wave % (BT / WN) * WN;
   float4v acc[MI][NJ] = {};
+
+  // The matrix's coefficients, asked for before the products.
+  constexpr int TAKEN = EPI == GRAM ? 0 : EPI == BOTH ? kBlock : 1;
+  float coef[TAKEN ? TAKEN : 1][3] = {};
+#pragma unroll
+  for (int q = 0; q < TAKEN; ++q)
+#pragma unroll
+    for (int e = 0; e < 3; ++e) coef[q][e] = a.table[b].coef[min(a.k + q, NF_ORTHOGONAL_MAX_STEPS - 1)][e];
+  const float ca = EPI == STEP || EPI == LAST ? (a.whole ? 0.0f : coef[0][0]) : coef[0][0];
+  const float cb = coef[0][1], cc = coef[0][2];
+  const float scale = EPI == LAST ? ldexpf(kInvScale, -a.table[b].shift) : 0.0f;
 
   // What the epilogue reads: of small tiles asked for now, before the products, else when it is needed.
   constexpr bool EARLY = BT == 64;
@@ -731,27 +782,30 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
     put(kA);
     __syncthreads();
     for (int k = 0; k < a.steps; ++k) {
-      combine(kA, kA, a.coef[k][1], a.coef[k][2]);  // Z = b A + c A A, q(A) = a + Z
+      const float qa = k == 0 ? coef[0][0] : k == 1 ? coef[1][0] : coef[2][0];
+      const float qb = k == 0 ? coef[0][1] : k == 1 ? coef[1][1] : coef[2][1];
+      const float qc = k == 0 ? coef[0][2] : k == 1 ? coef[1][2] : coef[2][2];
+      combine(kA, kA, qb, qc);  // Z = b A + c A A, q(A) = a + Z
       put(kZ);
       if (k == 0) {
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if (r + e == cq + 4 * j + lane % 4) acc[e / 4][j][e % 4] += a.coef[0][0] * kScale;
+            if (r + e == cq + 4 * j + lane % 4) acc[e / 4][j][e % 4] += qa * kScale;
         put(kP);
       }
       __syncthreads();
       if (k) {
-        combine(kZ, kP, a.coef[k][0], 1.0f);
+        combine(kZ, kP, qa, 1.0f);
         __syncthreads();  // P is read
         put(kP);
       }
       if (k + 1 < a.steps) {
-        combine(kZ, kA, a.coef[k][0], 1.0f);
+        combine(kZ, kA, qa, 1.0f);
         put(kR);
         __syncthreads();
-        combine(kZ, kR, a.coef[k][0], 1.0f);
+        combine(kZ, kR, qa, 1.0f);
         put(kA);  // (read by the product before the barrier, not by this one)
       }
       __syncthreads();
@@ -822,11 +876,11 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
           for (int e = 0; e < 8; ++e) {
             const float o = pair(h[e], l[e]);
             // (D + O)^2 = D^2 + D O + O D + O O
-            v[y][e] = fmaf(a.c, fmaf(dr[e / 4][e % 4] + dc, o, d[e] * kInvScale), a.b * o);
+            v[y][e] = fmaf(cc, fmaf(dr[e / 4][e % 4] + dc, o, d[e] * kInvScale), cb * o);
             if (r + e == c) {
-              const float on = fmaf(a.c, fmaf(dc, dc, d[e] * kInvScale * kInvScale), a.b * dc);
+              const float on = fmaf(cc, fmaf(dc, dc, d[e] * kInvScale * kInvScale), cb * dc);
               a.dB[b * a.Mp + c] = on;
-              if (a.dP) a.dP[b * a.Mp + c] = a.a + on;
+              if (a.dP) a.dP[b * a.Mp + c] = ca + on;
               v[y][e] = 0.0f;
             }
           }
@@ -834,9 +888,9 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const float o = pair(h[e], l[e]), z = pair(zh[e], zl[e]), dz = dr[e / 4][e % 4];
-            v[y][e] = fmaf(dz, o, fmaf(z, dc, d[e] * kInvScale)) + a.a * o;
+            v[y][e] = fmaf(dz, o, fmaf(z, dc, d[e] * kInvScale)) + ca * o;
             if (r + e == c) {
-              a.dB[b * a.Mp + c] = fmaf(dz, dc, d[e] * kInvScale * kInvScale) + a.a * dc;
+              a.dB[b * a.Mp + c] = fmaf(dz, dc, d[e] * kInvScale * kInvScale) + ca * dc;
               v[y][e] = 0.0f;
             }
           }
@@ -844,12 +898,12 @@ __global__ __launch_bounds__(BT / WM * (BT / WN) * 64) void k_prod(ProdArgs a) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const float hi = (float)h[e], x = pair(h[e], l[e]);
-            v[y][e] = fmaf(a.a, x, fmaf(dc, SPLIT || EPI == LAST ? x : hi, d[e] * kInvScale));
+            v[y][e] = fmaf(ca, x, fmaf(dc, SPLIT || EPI == LAST ? x : hi, d[e] * kInvScale));
           }
         }
       }
       if (EPI == LAST) {
-        store_last(a, b, r, rq, cq, lane, v);
+        store_last(a, b, r, rq, cq, lane, scale, v);
         continue;
       }
       half8 h[2], l[2];
@@ -919,7 +973,7 @@ struct Plan {
   int shares;      // of a GRAM tile's k
   int64_t tiles;   // GRAM's, if it has shares
   size_t gpart, arrived;
-  size_t part, dA, dB, xh, xl, th[2], tl[2], ah, al, bh, bl, total;
+  size_t part, table, dA, dB, xh, xl, th[2], tl[2], ah, al, bh, bl, total;
   size_t sq[10], sqd[6];  // gram_space: R, two Z, two P, high and low; their diagonals and that of the first P
 };
 
@@ -1026,6 +1080,7 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split, bool coarse)
   };
   const size_t x = (size_t)(2 * batch * p.Mp * p.Np), a = (size_t)(2 * batch * p.Mp * p.Mp);
   p.part = take((size_t)(8 * batch * p.nparts));
+  p.table = take(sizeof(Steps) * (size_t)batch);
   p.dA = take((size_t)(4 * batch * p.Mp));
   p.dB = take((size_t)(4 * batch * p.Mp));
   p.xh = take(x);
@@ -1134,6 +1189,9 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
   pa.nparts = p.nparts;
   pa.lg_tx = p.lg_tx;
   pa.eps = o.eps;
+  pa.steps = o.steps;
+  memcpy(pa.coef, o.coef, sizeof(pa.coef));
+  pa.table = reinterpret_cast<Steps*>(w + p.table);
   pa.xh = half(p.xh);
   pa.xl = half(p.xl);
   pa.th = half(p.th[0]);
@@ -1151,9 +1209,8 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
   const int64_t tm = p.Mp / p.tile, tn = p.Np / p.tile;
   for (int k = 0, turn = 0, taken = 1; k < o.steps; k += taken, ++turn) {
     ProdArgs g = last;
-    g.a = o.coef[k][0];
-    g.b = o.coef[k][1];
-    g.c = o.coef[k][2];
+    g.table = pa.table;
+    g.k = k;
     g.dA = reinterpret_cast<float*>(w + p.dA);
     g.dB = reinterpret_cast<float*>(w + p.dB);
     g.Mp = p.Mp;
@@ -1180,11 +1237,10 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
     if (p.m <= 64) {
       taken = block_of(o, k, coarse);
       x.steps = taken;
-      memcpy(x.coef, o.coef[k], sizeof(float) * 3 * taken);
       x.oh = half(p.bh);
       x.ol = half(p.bl);
       if ((e = launch_prod<BOTH>(p, x, 1, s)) != hipSuccess) return e;
-      g.a = 0.0f;  // P holds it
+      g.whole = 1;
     } else if (p.gram_space) {
       taken = block_of(o, k, coarse);
       if ((e = launch_prod<GRAM>(p, x, below_diagonal(x.tm), s)) != hipSuccess) return e;
@@ -1203,7 +1259,7 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
       y.pstride = y.qstride = p.Mp * p.Mp;
       y.tm = y.tn = (int32_t)(p.Mp / p.poly_tile);
       const int64_t tiles = below_diagonal(y.tm);
-      auto multiply = [&](const Square& z, const Square& with, const Square& to, float alpha) {
+      auto multiply = [&](const Square& z, const Square& with, const Square& to) {
         y.ph = z.h;
         y.pl = z.l;
         y.dZ = z.d;
@@ -1213,19 +1269,15 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
         y.oh = to.h;
         y.ol = to.l;
         y.dB = to.d;
-        y.a = alpha;
         return launch_prod<MULT>(p, y, tiles, s);
       };
       Square P = {};
       for (int i = 0; i < taken; ++i) {
-        const float* c = o.coef[k + i];
+        y.k = k + i;
         const Square& z = Z[i & 1];
         y.ph = y.qh = y.ah = A.h;  // Z = b A + c A A
         y.pl = y.ql = y.al = A.l;
         y.dA = A.d;
-        y.a = c[0];
-        y.b = c[1];
-        y.c = c[2];
         y.oh = z.h;
         y.ol = z.l;
         y.dB = z.d;
@@ -1234,18 +1286,18 @@ hipError_t run(const Plan& p, PrepArgs pa, ProdArgs last, const nf_orthogonal_pa
         if (i == 0) {
           P = Square{z.h, z.l, y.dP};  // differs from Z in its diagonal only
         } else {
-          if ((e = multiply(z, P, Q[i & 1], c[0])) != hipSuccess) return e;
+          if ((e = multiply(z, P, Q[i & 1])) != hipSuccess) return e;
           P = Q[i & 1];
         }
         if (i + 1 < taken) {
-          if ((e = multiply(z, A, R, c[0])) != hipSuccess) return e;
-          if ((e = multiply(z, R, A, c[0])) != hipSuccess) return e;
+          if ((e = multiply(z, A, R)) != hipSuccess) return e;
+          if ((e = multiply(z, R, A)) != hipSuccess) return e;
         }
       }
       bh = P.h;
       bl = P.l;
       g.dB = P.d;
-      g.a = 0.0f;  // P holds it
+      g.whole = 1;
     } else {
       if ((e = launch_prod<GRAM>(p, x, below_diagonal(x.tm), s)) != hipSuccess) return e;
       x.ph = x.qh = x.ah = half(p.ah);  // B = b A + c A A
