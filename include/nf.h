@@ -653,11 +653,18 @@ nf_status nf_embedding_grad(const void* dy, int32_t dy_type, int64_t dy_ld, int6
                             int64_t worker_stride, void* ws, size_t ws_bytes, void* stream);
 
 /* How nf_orthogonalize forms its products: of operands rounded once to FP16
- * (11 bits), or each held as two FP16 numbers (22 bits, three products).  The
- * result is within about 2e-3 of the exact one relative to its norm, or within
- * about 1e-5 (FP32 products are no closer), however small ||G|| is against eps,
- * down to the smallest numbers of the result's type.  Sizes for which products are not
- * what takes the time get the latter with NF_PRODUCTS_SINGLE as well. */
+ * (11 bits), or each held as two FP16 numbers (22 bits, three products).  Sizes
+ * for which products are not what takes the time get the latter with
+ * NF_PRODUCTS_SINGLE as well.  How far the result is from the exact one,
+ * relative to its norm:
+ *   SINGLE  about 2e-3 up to seven steps and 3.5e-3 at twelve with the
+ *           binding's default coefficients, whose singular values go on
+ *           moving; 5e-4 with ones that converge, (2, -1.5, 0.5) for all steps
+ *   SPLIT   as far as FP32 products: about 1e-5 at five steps and 3e-5 at
+ *           twelve, more the farther the large singular values are above the
+ *           others (2e-4 at five steps where one is above noise of 1e-4)
+ * however small ||G|| is against eps, down to the smallest numbers of the
+ * result's type. */
 enum { NF_PRODUCTS_SINGLE = 0, NF_PRODUCTS_SPLIT = 1 };
 #define NF_ORTHOGONAL_MAX_STEPS 12
 typedef struct {

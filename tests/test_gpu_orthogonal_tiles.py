@@ -86,6 +86,29 @@ def test_steps(steps, batch, m, n, products, dst_type):
         assert off(d[k], definition(u[k], triples)) <= BOUND[products] + UNIT[d.dtype], k
 
 
+# An emulation in NumPy of the roundings of 11-bit operands (Gaussian matrices of 128 x 300, 512 x 512 and 200 x 900)
+# is off by at most 1.9e-3 after seven steps of the default coefficients, 3.4e-3 after twelve, and 5.1e-4 after twelve
+# of coefficients that converge: half as much again is allowed.  22 bits: what nf.h says, and as much again.
+@pytest.mark.parametrize("gauss", [False, True])
+@pytest.mark.parametrize("coef,steps,bound", [
+    (COEF, 7, {SINGLE: 2.9e-3, SPLIT: 6e-5}), (COEF, 8, {SINGLE: 5.1e-3, SPLIT: 6e-5}),
+    (COEF, 12, {SINGLE: 5.1e-3, SPLIT: 6e-5}), ((2.0, -1.5, 0.5), 12, {SINGLE: 7.7e-4, SPLIT: 6e-5}),
+    ((1.5, -0.5, 0.0), 11, {SINGLE: 7.7e-4, SPLIT: 6e-5})])
+@pytest.mark.parametrize("batch,m,n", [(2, 190, 130), (1, 512, 512), (30, 449, 385), (16, 769, 769)])
+def test_many_steps(batch, m, n, coef, steps, bound, gauss):
+    """Steps one by one, the rounding of every one of them in the result."""
+    u = decaying(batch, m, n, 0, m + n + steps)
+    if gauss:
+        u.copy_(torch.randn(u.shape, generator=torch.Generator(device=DEV).manual_seed(steps), device=DEV))
+    d = torch.empty(batch, m, n, device=DEV)
+    for products in (SINGLE, SPLIT):
+        how = nf.orthogonal(products=products, steps=steps, coef=coef)
+        assert nf.nf_orthogonal_path(m, n, batch, how, nf.NF_TYPE_F32).rounds == steps
+        nf.nf_orthogonalize(u, d, how, workspace(u, how))
+        for k in (0, batch - 1):
+            assert off(d[k], definition(u[k], [coef] * steps)) <= bound[products], (products, k)
+
+
 @pytest.mark.parametrize("batch,m,n", [(30, 449, 385), (16, 769, 769), (8, 500, 4000), (8, 4000, 500)])
 def test_nan_stays_in_its_matrix(batch, m, n):
     u = decaying(batch, m, n, 0, 1)
