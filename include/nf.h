@@ -693,6 +693,7 @@ typedef struct {
  * NF_ERR_INVALID_ARG: sizes < 0, ld < cols, a stride < (rows-1)*ld + cols with
  * batch > 1, bad parameters.  NF_ERR_UNSUPPORTED: a side > 2^17, batch >
  * 65535 or more than 2^23 pieces of 64 x 64.  rows, cols or batch = 0 launches nothing.
+ * A workspace serves any steps, coefficients and types with its params' products.
  */
 size_t nf_orthogonal_workspace_bytes(int64_t rows, int64_t cols, int64_t batch,
                                      const nf_orthogonal_params* params_host);

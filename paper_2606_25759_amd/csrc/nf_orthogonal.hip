@@ -1041,22 +1041,63 @@ Cost choose_tiles(Plan* p) {
   return Cost{8.0 + best_gram + best + moved, 4.0 + best_poly};
 }
 
+// Steps from the k-th on that are taken at once by the Gram matrix.  What grows a small singular value grows the
+// rounding of A, P and P X as well: as far as P, whose norm is at most the product of the largest |q|, stays within 48
+// (three steps of 3.4445; FP16's range ends at 64).  The error is then up to 6e-6 (4e-6 step by step), which only a
+// result in FP32 from split products shows: that one goes step by step.
+int block_of(const nf_orthogonal_params& o, int k, bool coarse) {
+  double top = 1.0, growth = 1.0;  // of the singular values: X is scaled to at most 1
+  int n = 0;
+  for (int i = 0; i < k + kBlock && i < o.steps; ++i) {
+    const float* c = o.coef[i];
+    double most = 0.0, next = 0.0;
+    for (int j = 0; j <= 64; ++j) {
+      const double sv = top * j / 64, q = fabs(c[0] + sv * sv * (c[1] + sv * sv * c[2]));
+      most = fmax(most, q);
+      next = fmax(next, sv * q);
+    }
+    top = next;
+    if (i < k) continue;
+    growth *= fmax(most, 1.0);
+    if (n > 0 && (!coarse || !(growth <= 48.0))) break;
+    ++n;
+  }
+  return n;
+}
+
+// What o's steps come to, taken at once as far as block_of goes: products with X, and products of m x m.
+struct Schedule {
+  int rounds, squares;
+};
+Schedule schedule_of(const nf_orthogonal_params& o, bool coarse) {
+  Schedule s = {};
+  for (int k = 0, taken; k < o.steps; k += taken, ++s.rounds) {
+    taken = block_of(o, k, coarse);
+    s.squares += 4 * taken - 3;
+  }
+  return s;
+}
+
 // Steps at a time by the Gram matrix, where that is sooner: of five steps (three and two), X is read and written for
-// two, and there are fourteen products of m x m in place of five, all of split operands.
-void choose_form(Plan* p, bool coarse) {
+// two, and there are fourteen products of m x m in place of five, all of split operands.  Both five such steps and
+// the call's own have to be sooner: a workspace has room for what five take (o = nullptr), and so serves any steps.
+void choose_form(Plan* p, bool coarse, const nf_orthogonal_params* o) {
   Plan q = *p;
   q.split = true;
   const Cost by_step = choose_tiles(p);
   if (p->m <= 64 || !coarse) return;
   const Cost by_gram = choose_tiles(&q);
-  if (2.0 * by_gram.x + 14.0 * by_gram.square < 5.0 * (by_step.x + by_step.square)) {
+  auto sooner = [&](int steps, Schedule s) {
+    return s.rounds * by_gram.x + s.squares * by_gram.square < steps * (by_step.x + by_step.square);
+  };
+  if (sooner(5, Schedule{2, 14}) && (!o || sooner(o->steps, schedule_of(*o, coarse)))) {
     *p = q;
     p->gram_space = true;
   }
 }
 
-// Sizes are checked by the caller.
-Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split, bool coarse) {
+// Sizes are checked by the caller.  o: the steps, or nullptr for the room that a workspace has.
+Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split, bool coarse, const nf_orthogonal_params* o) {
   Plan p = {};
   p.rows = rows;
   p.cols = cols;
@@ -1067,7 +1108,7 @@ Plan plan_of(int64_t rows, int64_t cols, int64_t batch, bool split, bool coarse)
   // a short side of few rows has few roundings to average out (3.4e-3 measured at 1 x 7), and costs launches,
   // not products: always in pairs
   p.split = split || p.m <= 64;
-  choose_form(&p, coarse);
+  choose_form(&p, coarse, o);
   p.Mp = ceil_div(p.m, p.tile) * p.tile;
   p.Np = ceil_div(p.n, p.tile) * p.tile;
   p.nparts = (int)(ceil_div(rows * cols, kNormElems) < kMaxParts ? ceil_div(rows * cols, kNormElems) : kMaxParts);
@@ -1149,30 +1190,6 @@ hipError_t launch_prod(const Plan& p, const ProdArgs& a, int64_t tiles, hipStrea
     return launch_prod<EPI, true>(p, a, tiles, s);
   else
     return p.split ? launch_prod<EPI, true>(p, a, tiles, s) : launch_prod<EPI, false>(p, a, tiles, s);
-}
-
-// Steps from the k-th on that are taken at once by the Gram matrix.  What grows a small singular value grows the
-// rounding of A, P and P X as well: as far as P, whose norm is at most the product of the largest |q|, stays within 48
-// (three steps of 3.4445; FP16's range ends at 64).  The error is then up to 6e-6 (4e-6 step by step), which only a
-// result in FP32 from split products shows: that one goes step by step.
-int block_of(const nf_orthogonal_params& o, int k, bool coarse) {
-  double top = 1.0, growth = 1.0;  // of the singular values: X is scaled to at most 1
-  int n = 0;
-  for (int i = 0; i < k + kBlock && i < o.steps; ++i) {
-    const float* c = o.coef[i];
-    double most = 0.0, next = 0.0;
-    for (int j = 0; j <= 64; ++j) {
-      const double sv = top * j / 64, q = fabs(c[0] + sv * sv * (c[1] + sv * sv * c[2]));
-      most = fmax(most, q);
-      next = fmax(next, sv * q);
-    }
-    top = next;
-    if (i < k) continue;
-    growth *= fmax(most, 1.0);
-    if (n > 0 && (!coarse || !(growth <= 48.0))) break;
-    ++n;
-  }
-  return n;
 }
 
 // coarse: the result need not be closer than about 1e-5.
@@ -1388,10 +1405,10 @@ extern "C" {
 size_t nf_orthogonal_workspace_bytes(int64_t rows, int64_t cols, int64_t batch, const nf_orthogonal_params* params) {
   if (nf::check_params(params) || nf::check_sizes(rows, cols, batch) || nf::too_large(rows, cols, batch)) return 0;
   if (rows == 0 || cols == 0 || batch == 0) return 0;
-  // (a caller's results may be of any type: the larger of the two forms)
+  // (a caller's results may be of any type, and its steps any: the larger of the two forms)
   const bool split = params->products == NF_PRODUCTS_SPLIT;
-  const size_t fine = nf::plan_of(rows, cols, batch, split, false).total;
-  const size_t coarse = nf::plan_of(rows, cols, batch, split, true).total;
+  const size_t fine = nf::plan_of(rows, cols, batch, split, false, nullptr).total;
+  const size_t coarse = nf::plan_of(rows, cols, batch, split, true, nullptr).total;
   return fine > coarse ? fine : coarse;
 }
 
@@ -1406,16 +1423,16 @@ nf_status nf_orthogonal_path(int64_t rows, int64_t cols, int64_t batch, const nf
   if (too_large(rows, cols, batch)) return set_error(NF_ERR_UNSUPPORTED, "matrices too large");
   if (rows == 0 || cols == 0 || batch == 0) return set_error(NF_OK, "");
   const bool coarse = params->products == NF_PRODUCTS_SINGLE || dst_type != NF_TYPE_F32;
-  const Plan p = plan_of(rows, cols, batch, params->products == NF_PRODUCTS_SPLIT, coarse);
+  const Plan p = plan_of(rows, cols, batch, params->products == NF_PRODUCTS_SPLIT, coarse, params);
   info->split = p.split;
   info->step_tile = p.tile;
   info->gram_tile = p.gram_tile;
   info->poly_tile = p.poly_tile;
   info->shares = p.shares;
-  for (int k = 0, taken = 1; k < params->steps; k += taken, ++info->rounds) {
-    if (p.m <= 64 || p.gram_space) taken = block_of(*params, k, coarse);
-    if (p.m > 64) info->squares += p.gram_space ? 4 * taken - 3 : 1;
-  }
+  const bool one = p.m <= 64;
+  const Schedule s = one || p.gram_space ? schedule_of(*params, coarse) : Schedule{params->steps, params->steps};
+  info->rounds = s.rounds;
+  info->squares = one ? 0 : s.squares;
   return set_error(NF_OK, "");
 }
 
@@ -1435,7 +1452,7 @@ nf_status nf_orthogonalize(const void* src, int32_t src_type, int64_t src_ld, in
                   "dst_ld < cols or dst_stride too small", "dst not aligned to its elements");
   if (st != NF_OK) return st;
   const bool coarse = params->products == NF_PRODUCTS_SINGLE || dst_type != NF_TYPE_F32;
-  const Plan p = plan_of(rows, cols, batch, params->products == NF_PRODUCTS_SPLIT, coarse);
+  const Plan p = plan_of(rows, cols, batch, params->products == NF_PRODUCTS_SPLIT, coarse, params);
   if ((st = check_ws(ws, ws_bytes, nf_orthogonal_workspace_bytes(rows, cols, batch, params))) != NF_OK) return st;
   PrepArgs pa = {};
   pa.g = View{const_cast<void*>(src), src_ld, src_stride, src_type};
@@ -1467,7 +1484,7 @@ nf_status nf_orthogonal_update(const void* grad, int32_t grad_type, int64_t grad
   st = check_view(weight, weight_type, weight_ld, weight_stride, rows, cols, batch, "weight is NULL",
                   "weight_ld < cols or weight_stride too small", "weight not aligned to its elements");
   if (st != NF_OK) return st;
-  const Plan p = plan_of(rows, cols, batch, params->products == NF_PRODUCTS_SPLIT, true);
+  const Plan p = plan_of(rows, cols, batch, params->products == NF_PRODUCTS_SPLIT, true, params);
   if ((st = check_ws(ws, ws_bytes, nf_orthogonal_workspace_bytes(rows, cols, batch, params))) != NF_OK) return st;
   PrepArgs pa = {};
   pa.g = View{const_cast<void*>(grad), grad_ld, grad_stride, grad_type};

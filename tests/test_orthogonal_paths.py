@@ -38,6 +38,26 @@ def test_path():
         assert path(*empty, SINGLE, BF16) == [0] * 7
 
 
+def test_the_schedule_decides_the_form():
+    """Steps are taken at once only where the call's own steps gain by it; room for it is there whatever they are."""
+    long_sides = [(40, 257, 449, SPLIT), (20, 769, 65, SPLIT), (12, 100, 4000, SINGLE), (3, 6001, 150, SINGLE),
+                  (25, 3456, 143, SINGLE), (8, 768, 16_384, SINGLE), (4, 1024, 32_768, SINGLE)]
+    steep = (7.5, -10.0, 3.6)  # two such steps grow by more than may be taken at once
+    for batch, m, n, products in long_sides:
+        def path(how):
+            i = nf.nf_orthogonal_path(m, n, batch, how)
+            return i.split, i.rounds, i.squares
+
+        one_by_one = int(products == SPLIT)
+        assert path(nf.orthogonal(products=products)) == (1, 2, 14)
+        assert path(nf.orthogonal(products=products, steps=1)) == (one_by_one, 1, 1)
+        assert path(nf.orthogonal(products=products, steps=4, coef=steep)) == (one_by_one, 4, 4)
+        need = {nf.nf_orthogonal_workspace_bytes(m, n, batch, how)
+                for how in (nf.orthogonal(products=products, steps=s, coef=c)
+                            for s in range(1, 13) for c in (steep, (2.0, -1.5, 0.5), (3.4445, -4.7750, 2.0315)))}
+        assert len(need) == 1
+
+
 def test_refusals():
     fn, how, info = nf.load().nf_orthogonal_path, nf.orthogonal(), nf.nf_orthogonal_path_info()
     good = [40, 30, 2, ctypes.byref(how), 1, ctypes.byref(info)]
