@@ -594,7 +594,7 @@ nf_status nf_embedding_grad(const void* dy, int32_t dy_type, int64_t dy_ld, int6
   if (ids_bytes != 4 && ids_bytes != 8) return bad("ids_bytes must be 4 or 8");
   if (const char* why = check_grad_sizes(W, T, V, d)) return bad(why);
   if (dy_ld < d) return bad("dy_ld < d");
-  if (W > 1 && T > 0 && (dy_stride < (T - 1) * dy_ld + d || ids_stride < T))
+  if (W > 1 && T > 0 && (overlaps(dy_stride, T, dy_ld, d) || ids_stride < T))
     return bad("dy_stride or ids_stride too small");
   if (W > 1 && worker_stride < V * d) return bad("worker_stride < V * d");
   if (accumulate != 0 && accumulate != 1) return bad("accumulate must be 0 or 1");

@@ -1379,7 +1379,7 @@ bool too_large(int64_t rows, int64_t cols, int64_t batch) {
 nf_status check_view(const void* p, int32_t type, int64_t ld, int64_t stride, int64_t rows, int64_t cols, int64_t batch,
                      const char* null, const char* shape, const char* align) {
   if (!known_type(type)) return bad("unknown element type");
-  if (ld < cols || (batch > 1 && stride < (rows - 1) * ld + cols)) return bad(shape);
+  if (ld < cols || (batch > 1 && overlaps(stride, rows, ld, cols))) return bad(shape);
   if (!p) return bad(null);
   if ((uintptr_t)p % type_bytes(type)) return set_error(NF_ERR_ALIGNMENT, align);
   return NF_OK;

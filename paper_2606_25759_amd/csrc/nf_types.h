@@ -14,6 +14,10 @@ struct Bf16 {
 };
 
 inline bool known_type(int32_t t) { return t == NF_TYPE_F32 || t == NF_TYPE_BF16 || t == NF_TYPE_F16; }
+// Whether `stride` is less than what rows x cols elements take, rows `ld` apart (a product that may pass 64 bits).
+inline bool overlaps(int64_t stride, int64_t rows, int64_t ld, int64_t cols) {
+  return (__int128)stride < (__int128)(rows - 1) * ld + cols;
+}
 inline size_t type_bytes(int32_t t) { return t == NF_TYPE_F32 ? 4 : 2; }
 
 __device__ __forceinline__ float to_f32(float x) { return x; }
