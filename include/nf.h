@@ -684,15 +684,17 @@ typedef struct {
  * infinity gives NaN everywhere; other matrices of the batch are unaffected.
  * Coefficients must keep |a|, the squares of the singular values of X, and the
  * norm of b A + c A A, with a or without it, below 60, as any that converge
- * do: products beyond the range of FP16 give NaN.  Steps may be taken together, as X <- P X with P the
- * product of their a + b A + c A A, where that is sooner and not less exact
- * than is said above.
+ * do: products beyond the range of FP16 give NaN.  Steps may be taken
+ * together, as X <- P X with P the product of their a + b A + c A A, where that
+ * is sooner and not less exact than is said above; into FP32 from
+ * NF_PRODUCTS_SPLIT they go one by one (4e-6 where that is 6e-6).
  * src and dst: `batch` matrices of rows x cols, elements of a row adjacent,
  * rows src_ld (dst_ld) and matrices src_stride (dst_stride) elements apart,
  * of any NF_TYPE_*, aligned to their elements; dst may be src.
  * NF_ERR_INVALID_ARG: sizes < 0, ld < cols, a stride < (rows-1)*ld + cols with
  * batch > 1, bad parameters.  NF_ERR_UNSUPPORTED: a side > 2^17, batch >
- * 65535 or more than 2^23 pieces of 64 x 64.  rows, cols or batch = 0 launches nothing.
+ * 65535 or more than 2^23 pieces of 64 x 64.  rows, cols or batch = 0
+ * launches nothing.
  * A workspace serves any steps, coefficients and types with its params' products.
  */
 size_t nf_orthogonal_workspace_bytes(int64_t rows, int64_t cols, int64_t batch,
@@ -736,7 +738,8 @@ typedef struct {
  *   M = mu M + g;   U = g + mu M if nesterov, else M
  *   w = (1 - lr weight_decay) w - lr scale orthogonalised(U)
  * M is FP32, grad and weight any NF_TYPE_*; w is formed in FP32 and rounded
- * once.  Layouts, requirements and errors as for nf_orthogonalize.
+ * once.  Layouts, requirements and errors as for nf_orthogonalize; steps may be
+ * taken together whatever the weights' type.
  */
 nf_status nf_orthogonal_update(const void* grad, int32_t grad_type, int64_t grad_ld, int64_t grad_stride,
                                float* momentum, int64_t momentum_ld, int64_t momentum_stride, void* weight,

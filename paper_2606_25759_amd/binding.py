@@ -712,8 +712,10 @@ def nf_embedding_grad(dy, ids, grads, offset, V, ws, scale=1.0, padding_id=-1, a
 
 
 def orthogonal(products=NF_PRODUCTS_SINGLE, steps=5, coef=(3.4445, -4.7750, 2.0315), eps=1e-7):
-    """Parameters of nf_orthogonalize.  coef: (a, b, c) for every step, or a
-    sequence of `steps` such triples."""
+    """Parameters of nf_orthogonalize.  products: NF_PRODUCTS_SINGLE whatever
+    the result's type; FP32 results that should be as exact as FP32 products
+    ask for NF_PRODUCTS_SPLIT.  coef: (a, b, c) for every step, or a sequence
+    of `steps` such triples."""
     p = nf_orthogonal_params(products, steps, eps)
     rows = [coef] * steps if np.ndim(coef) == 1 else list(coef)
     if len(rows) != steps:

@@ -479,8 +479,8 @@ __device__ __forceinline__ void store_last(const ProdArgs& a, int64_t b, int64_t
 //
 // What bounds it.  The loop by itself, with tiles of 256 on 4096 x 4096 x 4096,
 // does 1.36 PFLOP/s, as a library product of that type does (1.38 to 1.41).
-// Of 24 x (2048 x 2048), GRAM takes 238 us (0.97 PFLOP/s: 864 tiles are 3.4
-// rounds of the card), POLY 261 us, STEP 475 us: 412 GFLOP are 300 us of that
+// Of 24 x (2048 x 2048), GRAM takes 243 us (0.95 PFLOP/s: 864 tiles are 3.4
+// rounds of the card), POLY 266 us, STEP 481 us: 412 GFLOP are 300 us of that
 // and the 1.0 GB that its epilogue reads and writes the rest, one after the
 // other, since all blocks of a round end together.  (Two blocks a CU with
 // tiles of 256 x 128 do not overlap them either: 488 us against 483 in a copy
@@ -980,11 +980,12 @@ struct Plan {
 constexpr int64_t kCUs = 256;
 
 // Microseconds that a launch's tiles take for one stage of 32 k, by how they fill the card: one block a CU with tiles
-// of 256 (one of 128 in split mode), two of 128 (64 in split mode), four of 64.  From the time of whole calls of
-// 1 to 24 matrices of 512 to 4,096 with each tile forced; a full card does 1.25 PFLOP/s of products with tiles of
-// 256, 0.98 with 128 and 0.87 with 64 (in split mode 1.3 with 128 and 1.1 with 64), but smaller tiles fill it sooner:
-// one matrix of 1000 x 1601 takes 194 us with tiles of 64, 273 with 128 and 536 with 256; four of 2048 x 2048 take
-// 1,209, 1,030 and 933 us.
+// of 256 (one of 128 in split mode), two of 128 (64 in split mode), four of 64.  Fitted to the time of whole calls, so
+// a share of their epilogues and last rounds is in them: a full card comes to 1.23 PFLOP/s of products with tiles of
+// 256, 0.90 with 128 and 0.67 with 64 (in split mode 1.30 with 128 and 0.89 with 64).  Smaller tiles fill it sooner:
+// one matrix of 1000 x 1601 takes 184 us with tiles of 64, 279 with 128 and 528 with 256; four of 2048 x 2048 take
+// 1,213, 1,029 and 933 us.  At 19 sizes of 1 to 24 matrices of 512 to 4,096, either products, what the rule takes is
+// within 4% of the best of one tile for all.
 double stage_us(int tile, bool split, int64_t tiles) {
   const int per = (tile == 64 ? 4 : tile == 128 ? 2 : 1) / (split ? 2 : 1);
   // of a card with 1, 2, .. `per` blocks a CU
@@ -996,8 +997,10 @@ double stage_us(int tile, bool split, int64_t tiles) {
 }
 
 // Blocks that share the k of a GRAM tile, as far as the tiles leave the card empty.  A stage takes about 0.25 us and
-// adding up a share 0.35 us, so their sum is least at the square root of 0.7 of the stages.  256 x 2304: 12.7 us with
-// 9 shares, 13.6 with 18, 36 with one; 1000 x 1601 (136 tiles of 64): 17.6 us with 3, 30 with one.
+// adding up a share 0.35 us, so their sum is least at the square root of 0.7 of the stages.  Whole calls: 256 x 2304 in
+// pairs 142 us with the 7 shares that this gives, 170 with one, 196 with 2, 135 at best (12); 3 x (65 x 3000) 137 with
+// 8, 185 with one.  Where it gives two or three there is nothing to gain: 1000 x 1601 takes 183 us with 3 and 180 with
+// one, in pairs 243 and 232, and 5 x (513 x 1100), tiles of 128, 212 and 178.
 int shares_of(int64_t tiles, int64_t stages, int tile) {
   if (tile == 256) return 1;  // built without
   const int64_t free = (tile == 64 ? 2 : 1) * kCUs / (tiles > 0 ? tiles : 1);
@@ -1081,6 +1084,9 @@ Schedule schedule_of(const nf_orthogonal_params& o, bool coarse) {
 // Steps at a time by the Gram matrix, where that is sooner: of five steps (three and two), X is read and written for
 // two, and there are fourteen products of m x m in place of five, all of split operands.  Both five such steps and
 // the call's own have to be sooner: a workspace has room for what five take (o = nullptr), and so serves any steps.
+// 8 x (300 x 16,384) takes 848 us, 1,114 step by step; 40 x (1024 x 2048) would take 4,448 in place of 2,456.
+// At 38 sizes with five steps the rule took the sooner form at 31 and one at most 6% slower at five; 40 x (300 x 2048)
+// (614 us, 487 step by step) and 8 x (1024 x 16,384) (4,193 and 3,705) go the slower way.
 void choose_form(Plan* p, bool coarse, const nf_orthogonal_params* o) {
   Plan q = *p;
   q.split = true;
