@@ -748,6 +748,59 @@ nf_status nf_orthogonal_update(const void* grad, int32_t grad_type, int64_t grad
                                const nf_orthogonal_params* params_host, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * A layer of experts for W workers with T rows of tokens each, in the order
+ * of their experts (no paper counterpart): worker w's expert e has the rows
+ * t in [offsets[w][e], offsets[w][e + 1]).  E matrices of n x k, `matrix`
+ * here, are shared by the workers.
+ *   transposed = 0:  y[w][t] = matrix_e x[w][t]      x has k columns, y has n
+ *   transposed = 1:  y[w][t] = matrix_e^T x[w][t]    x has n columns, y has k
+ *                    (the gradient of the rows, from that of y)
+ * Sums are FP32, of products of the elements as they are, and rounded once to
+ * y's type.  Rows that belong to no expert are left as they are; a row's
+ * infinities and NaN stay in its own row of y.  In a reduction of length zero
+ * rows are zeros.
+ *
+ * offsets: E + 1 int32 (offsets_bytes = 4) or int64 (8) device values a
+ * worker, offsets_stride apart, ascending, within [0, T]; the sizes of groups
+ * are never read on the host.  Values outside [0, T] are taken as the nearer
+ * end and no memory outside the tensors is touched whatever they are, but of
+ * offsets that descend the results are not defined.
+ * x and w of one NF_TYPE_*, y of any, aligned to their elements; rows x_ld
+ * (w_ld, y_ld), workers x_stride (y_stride) and matrices w_stride elements
+ * apart.  y shares no element with x or w.
+ * NF_ERR_INVALID_ARG: W outside [1, 255], T outside [0, 2^24], E outside
+ * [0, 4096], n or k outside [0, 2^20], an ld below the columns, a stride too
+ * small with W > 1 (w_stride with E > 1), y at x or w.  NF_ERR_UNSUPPORTED:
+ * more than 2^22 tiles of 128 x 32 or more.  T, E or the columns of y = 0
+ * launches nothing.
+ */
+nf_status nf_expert_product(const void* x, int32_t type, int64_t x_ld, int64_t x_stride, const void* w, int64_t w_ld,
+                            int64_t w_stride, int32_t transposed, const void* offsets, int32_t offsets_bytes,
+                            int64_t offsets_stride, int32_t W, int64_t T, int32_t E, int64_t n, int64_t k, void* y,
+                            int32_t y_type, int64_t y_ld, int64_t y_stride, void* stream);
+
+/*
+ * Gradient of those matrices for every worker, into its FP32 gradient row:
+ *   grads[w*worker_stride + e*matrix_stride + i*k + j] =
+ *       sum of dy[w][t][i] x[w][t][j] over the rows t of expert e
+ * Experts without a row get zeros.  With accumulate != 0 the sums are added to
+ * what the row holds.  Sums are FP32 in an order fixed by the sizes, without
+ * floating-point atomics: two calls give the same bits.
+ * `grads` is expert 0's matrix in worker 0's row (a row's base plus the
+ * matrices' offset in it), 4-byte aligned; it shares no element with dy or x.
+ * dy (n columns) and x (k columns) of one NF_TYPE_*; offsets, layouts and
+ * errors as for nf_expert_product, and NF_ERR_INVALID_ARG for matrix_stride
+ * < n * k with E > 1 or worker_stride below a worker's matrices with W > 1.
+ * T = 0 writes zeros.  E, n or k = 0 launches nothing.
+ */
+size_t nf_expert_grad_workspace_bytes(int32_t W, int64_t T, int32_t E, int64_t n, int64_t k);
+nf_status nf_expert_grad(const void* dy, int64_t dy_ld, int64_t dy_stride, const void* x, int64_t x_ld,
+                         int64_t x_stride, int32_t type, const void* offsets, int32_t offsets_bytes,
+                         int64_t offsets_stride, int32_t W, int64_t T, int32_t E, int64_t n, int64_t k,
+                         int32_t accumulate, float* grads, int64_t matrix_stride, int64_t worker_stride, void* ws,
+                         size_t ws_bytes, void* stream);
+
+/*
  * Profiling hook (no paper counterpart).  When set on the calling thread,
  * nf_route_bucket and nf_route_buckets record these hipEvent_t handles (each
  * passed as void*) on their stream: before pass 1, after pass 1, after the

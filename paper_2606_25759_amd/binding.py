@@ -41,7 +41,8 @@ EXPORTS = ["nf_abi_version", "nf_last_error", "nf_mask_from_segments", "nf_works
            "nf_sliced_layout_sizes", "nf_sliced_layout", "nf_compact_signs", "nf_slice_workspace_bytes",
            "nf_slice_scales", "nf_compact_signcount_reduce",
            "nf_embedding_lookup", "nf_embedding_workspace_bytes", "nf_embedding_grad",
-           "nf_orthogonal_workspace_bytes", "nf_orthogonal_path", "nf_orthogonalize", "nf_orthogonal_update"]
+           "nf_orthogonal_workspace_bytes", "nf_orthogonal_path", "nf_orthogonalize", "nf_orthogonal_update",
+           "nf_expert_product", "nf_expert_grad_workspace_bytes", "nf_expert_grad"]
 NF_TYPE_F32, NF_TYPE_BF16, NF_TYPE_F16 = 0, 1, 2
 NF_PRODUCTS_SINGLE, NF_PRODUCTS_SPLIT = 0, 1
 NF_ORTHOGONAL_MAX_STEPS = 12
@@ -196,6 +197,11 @@ def load(path=None):
                                             _SZ, _P]),
         "nf_orthogonal_update": (ctypes.c_int, [_P, _I32, _I64, _I64, _P, _I64, _I64, _P, _I32, _I64, _I64, _I64,
                                                 _I64, _I64, _P, _P, _P, _SZ, _P]),
+        "nf_expert_product": (ctypes.c_int, [_P, _I32, _I64, _I64, _P, _I64, _I64, _I32, _P, _I32, _I64, _I32, _I64,
+                                             _I32, _I64, _I64, _P, _I32, _I64, _I64, _P]),
+        "nf_expert_grad_workspace_bytes": (_SZ, [_I32, _I64, _I32, _I64, _I64]),
+        "nf_expert_grad": (ctypes.c_int, [_P, _I64, _I64, _P, _I64, _I64, _I32, _P, _I32, _I64, _I32, _I64, _I32, _I64,
+                                          _I64, _I32, _P, _I64, _I64, _P, _SZ, _P]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -764,6 +770,77 @@ def nf_orthogonal_update(grad, momentum, weight, step, params, ws, stream=None):
                                        grad.shape[0] if grad.dim() == 3 else 1, ctypes.byref(step),
                                        ctypes.byref(params), _dev_ptr(ws, torch.uint8, "ws"), ws.numel(),
                                        _stream(stream)))
+
+
+# ---------------------------------------------------------------- experts
+
+def _here(*tensors):
+    """Refuses tensors of another device than the current one, whose stream the call would run on."""
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"a tensor on {t.device} while the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _worker_rows(t, name):
+    """(pointer, row stride, worker stride, W, T, columns) of a [T, columns] or [W, T, columns] tensor."""
+    p, ld, stride = _matrices(t, None, name)
+    return p, ld, stride, t.shape[0] if t.dim() == 3 else 1, t.shape[-2], t.shape[-1]
+
+
+def _offsets_of(offsets, W, E):
+    p, size = _ids(offsets, "offsets")
+    if tuple(offsets.shape) not in ((W, E + 1),) + (((E + 1,),) if W == 1 else ()):
+        raise ValueError(f"offsets must be [{W}, {E + 1}], got {tuple(offsets.shape)}")
+    return p, size, offsets.stride(0) if offsets.dim() == 2 and W > 1 else E + 1
+
+
+def nf_expert_product(x, w, offsets, y, transposed=False, stream=None):
+    """y[t] = w[e] x[t] for the rows t of expert e, offsets[e] to
+    offsets[e + 1]; transposed: y[t] = w[e]^T x[t].  x, y: [T, columns] or
+    [W, T, columns]; w: [E, n, k]; offsets: [E + 1] or [W, E + 1], int32 or
+    int64, on the device.  Rows of no expert are left as they are."""
+    _here(x, w, offsets, y)
+    if w.dim() != 3:
+        raise ValueError("w must be [E, n, k]")
+    E, n, k = w.shape
+    wp, wld, wst = _matrices(w, None, "w")
+    xp, xld, xst, W, T, cols = _worker_rows(x, "x")
+    yp, yld, yst, yW, yT, ycols = _worker_rows(y, "y")
+    if w.dtype != x.dtype:
+        raise ValueError(f"x and w must have one type, got {x.dtype} and {w.dtype}")
+    if (cols, ycols) != ((n, k) if transposed else (k, n)) or (yW, yT) != (W, T):
+        raise ValueError(f"x {tuple(x.shape)}, w {tuple(w.shape)} and y {tuple(y.shape)} do not belong together")
+    op, obytes, ost = _offsets_of(offsets, W, E)
+    _check(load().nf_expert_product(xp, _type(x, "x"), xld, xst, wp, wld, wst, 1 if transposed else 0, op, obytes, ost,
+                                    W, T, E, n, k, yp, _type(y, "y"), yld, yst, _stream(stream)))
+
+
+def nf_expert_grad_workspace_bytes(W, T, E, n, k):
+    return int(load().nf_expert_grad_workspace_bytes(W, T, E, n, k))
+
+
+def nf_expert_grad(dy, x, offsets, grads, offset, ws, accumulate=False, matrix_stride=None, stream=None):
+    """The matrices' gradient for W workers into their rows of grads, expert
+    e's at element offset + e * matrix_stride (n * k if None).  dy: [W, T, n],
+    x: [W, T, k] (or [T, n] and [T, k] of one worker), offsets: [W, E + 1],
+    grads: [W, stride] float32."""
+    _here(dy, x, offsets, grads, ws)
+    g, stride, rows = _rows(grads)
+    dp, dld, dst, W, T, n = _worker_rows(dy, "dy")
+    xp, xld, xst, xW, xT, k = _worker_rows(x, "x")
+    if dy.dtype != x.dtype:
+        raise ValueError(f"dy and x must have one type, got {dy.dtype} and {x.dtype}")
+    if (xW, xT, rows) != (W, T, W):
+        raise ValueError(f"dy {tuple(dy.shape)}, x {tuple(x.shape)} and {rows} rows of grads do not belong together")
+    E = offsets.shape[-1] - 1 if offsets.dim() else -1
+    op, obytes, ost = _offsets_of(offsets, W, E)
+    each = n * k if matrix_stride is None else matrix_stride
+    end = offset + (E - 1) * each + n * k
+    if offset < 0 or each < 0 or (E > 0 and end > grads.shape[1]):
+        raise ValueError(f"the matrices' segment [{offset}, {end}) exceeds the rows of {grads.shape[1]}")
+    _check(load().nf_expert_grad(dp, dld, dst, xp, xld, xst, _type(dy, "dy"), op, obytes, ost, W, T, E, n, k,
+                                 1 if accumulate else 0, g + 4 * offset, each, stride,
+                                 _dev_ptr(ws, torch.uint8, "ws"), ws.numel(), _stream(stream)))
 
 
 # ------------------------------------------------------- result decoding

@@ -1,0 +1,762 @@
+// nf_expert.hip - products of token rows with their expert's matrix, and the
+// gradient of those matrices, for groups of rows of uneven sizes.
+//
+//   k_expert   D[q][p] = sum over r of Q[q][r] P[p][r] for one tile of one group:
+//                FORWARD   y = W x:     P = W (n x k),    Q = x rows,   r over k
+//                BACKWARD  y = W^T x:   P = W^T (k x n),  Q = x rows,   r over n
+//                GRAD      dW = dy^T x: P = x^T (k x T),  Q = dy^T,     r over tokens
+//   k_join     GRAD with tokens shared between blocks: the shares' sums, in order
+//
+// Group sizes are known on the device only, so the grid is the most that any
+// sizes can need, and each wavefront finds its own tile by a scan over the
+// offsets (a lane for every 1/64 of the experts); blocks past the last tile
+// end at once.  Tiles never span groups: a group's last tile of rows is
+// partly empty, which costs products but no memory traffic.
+//
+// P and Q lie in memory either with r adjacent (as the products take them) or
+// with their own index adjacent (W for BACKWARD, both for GRAD); the latter
+// are transposed on the way from LDS to registers, 16-bit elements by the
+// LDS's own transposing read.
+//
+// FP16 and BF16 operands go to the matrix cores as they are, FP32 operands to
+// its FP32 instruction; sums are FP32 in any case, each result rounded once.
+#include <type_traits>
+
+#include "nf_internal.h"
+#include "nf_tile.h"
+#include "nf_types.h"
+
+namespace nf {
+namespace {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bhalf8 __attribute__((ext_vector_type(8)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
+typedef int16_t short4v __attribute__((ext_vector_type(4)));
+
+enum { FORWARD, BACKWARD, GRAD };
+
+constexpr int kStageBytes = 128;  // of a row in LDS: 64 elements of 16 bits, 32 of FP32
+constexpr int kMaxExperts = 4096;
+
+struct ExpertArgs {
+  const void *p, *q;
+  int64_t p_ld, q_ld;              // elements between rows in memory
+  int64_t p_worker, q_worker;      // between workers
+  int64_t p_expert;                // between experts' matrices (FORWARD, BACKWARD)
+  const void* offsets;             // [E + 1] of each worker
+  int64_t offsets_stride;
+  int64_t T;
+  int32_t offsets64, E;
+  int32_t P, Q, R;                 // lengths: of D's rows; GRAD: of its columns; FORWARD, BACKWARD: of r
+  int32_t tp, tq;                  // tiles of P, and (GRAD) of Q
+  int32_t rows;                    // of a group that a block takes: tile of Q, or (GRAD) tokens of a share
+  void* out;
+  int32_t out_type, accumulate;
+  int64_t out_ld, out_worker, out_expert;
+  float* part;                     // GRAD: sums of shares, [worker][unit][tile][elements]
+  int32_t units;                   // most units of a worker: rounds up what any sizes need
+};
+
+// ------------------------------------------------------------ groups of rows
+
+__device__ __forceinline__ int64_t offset_at(const ExpertArgs& a, int64_t worker, int e) {
+  const int64_t at = worker * a.offsets_stride + e;
+  int64_t v;
+  if (a.offsets64)
+    v = ((const int64_t*)a.offsets)[at];
+  else
+    v = ((const int32_t*)a.offsets)[at];
+  return v < 0 ? 0 : v > a.T ? a.T : v;
+}
+
+struct Group {
+  int32_t e, unit, units;  // expert, which of its units, how many it has
+  int32_t base;            // units of the experts before it
+  int64_t first, rows;     // its rows
+};
+
+// A group's units: a tile of rows each, or a share of its tokens (at least one: its gradient is written in any case).
+template <int MODE>
+__device__ __forceinline__ int units_of(const ExpertArgs& a, int64_t worker, int e, int64_t* first, int64_t* rows) {
+  const int64_t lo = offset_at(a, worker, e), hi = offset_at(a, worker, e + 1);
+  *first = lo;
+  *rows = hi > lo ? hi - lo : 0;
+  const int n = (int)(((uint32_t)*rows + (uint32_t)a.rows - 1) / (uint32_t)a.rows);
+  return MODE == GRAD ? max(n, 1) : n;
+}
+
+// Sums of the lanes up to this one.
+__device__ __forceinline__ int scan(int v, int lane) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int w = __shfl_up(v, o);
+    if (lane >= o) v += w;
+  }
+  return v;
+}
+
+// The group and unit of tile `block` of a worker, `per` tiles a unit; false past the last.  `id` becomes the tile's
+// number in its group.  Blocks go round the eight XCDs: each takes a contiguous share of the tiles.
+template <int MODE>
+__device__ __forceinline__ bool find(const ExpertArgs& a, int64_t worker, int block, int per, Group* g, int* id) {
+  const int lane = threadIdx.x % 64, each = (a.E + 63) / 64;
+  int64_t first, rows;
+  int mine = 0;
+  for (int j = 0; j < each; ++j)
+    if (lane * each + j < a.E) mine += units_of<MODE>(a, worker, lane * each + j, &first, &rows);
+  const int upto = scan(mine, lane);
+  const int total = min(__builtin_amdgcn_readlane(upto, 63), a.units) * per;
+  if (block >= total) return false;
+  {
+    const int x = block & 7, share = total >> 3, more = total & 7;
+    block = x * share + min(x, more) + (block >> 3);
+  }
+  const int u = block / per;
+  const int at = __builtin_ctzll(__ballot(upto > u));
+  int base = __builtin_amdgcn_readlane(upto - mine, at), e = at * each, n = 0;
+  for (;; ++e) {
+    n = units_of<MODE>(a, worker, e, &first, &rows);
+    if (u < base + n || e + 1 >= a.E) break;
+    base += n;
+  }
+  g->e = __builtin_amdgcn_readfirstlane(e);
+  g->units = __builtin_amdgcn_readfirstlane(n);
+  g->base = __builtin_amdgcn_readfirstlane(base);
+  g->unit = u - g->base;
+  g->first = first;
+  g->rows = rows;
+  *id = block - g->base * per;
+  return true;
+}
+
+// ----------------------------------------------------------------- operands
+
+template <typename T>
+constexpr int kPiece = 16 / (int)sizeof(T);  // elements of 16 bytes
+template <typename T>
+constexpr int kStageLen = kStageBytes / (int)sizeof(T);  // r of a stage
+
+// Where BT x kStageLen elements lie in LDS, in pieces of 16 bytes.
+//
+// r adjacent: rows of 128 bytes, and slot j of row `row` holds its piece j ^ s(row).  A fragment is sixteen rows of
+// thirty-two, 8 q + e and, in the odd fragment of a pair, 8 q + 4 + e (q, e in [0, 4)): of the products of a pair a
+// lane then holds eight adjacent p.  A 16-byte read is served sixteen lanes at a time, which touch each of the 64
+// banks once with this s.
+//
+// Own index adjacent: kStageLen rows of BT elements.  A fragment of 16-bit elements is sixteen adjacent columns, of
+// which a transposing read gives each lane four rows of one, from 32 bytes of each of four rows; those go to slots
+// that differ in the eight rows that are read at a time.  FP32 elements are read one by one, 64 bytes of four rows
+// four apart.
+template <typename T, int BT, int NW, bool TURNED>
+struct Tile {
+  static constexpr int kBytes = BT * kStageBytes;
+  static constexpr int kLoads = BT / 8 / NW;  // of a wavefront, 1 KiB each
+  static constexpr int kRow = TURNED ? BT * (int)sizeof(T) : kStageBytes;
+  static constexpr int kRows = 1024 / kRow;  // of one load
+  static_assert(BT % (8 * NW) == 0 && kRow <= 1024, "whole loads");
+
+  static __device__ __forceinline__ int swizzle(int row) {
+    if (!TURNED) {
+      const int q = row >> 3;
+      return ((q >> 1) & 1) | (((q ^ (q >> 1)) & 1) << 1) | ((row & 2) << 1);
+    }
+    if (sizeof(T) == 2) return (row & 3) << 1 | (row & 8);
+    return row & 12;
+  }
+  // The row and piece of it that lane `lane` of a wavefront loads in its i-th load.
+  static __device__ __forceinline__ int load_row(int i, int wave, int lane) {
+    return (i * NW + wave) * kRows + lane / (kRow / 16);
+  }
+  static __device__ __forceinline__ int load_piece(int row, int lane) { return (lane % (kRow / 16)) ^ swizzle(row); }
+
+  // The bytes at which a lane reads fragment 0 of the tile's part that begins at row or column w, of half h.
+  static __device__ __forceinline__ int read_at(int w, int h, int lane) {
+    if (!TURNED) {
+      const int row = w + lane % 16 / 4 * 8 + lane % 4;
+      return row * kStageBytes + (((h * 4 + lane / 16) ^ swizzle(row)) << 4);
+    }
+    if (sizeof(T) == 2) {
+      const int row = h * 32 + lane / 16 * 8 + lane % 16 / 4;
+      return row * kRow + ((w * 2 ^ swizzle(row) << 4) | (lane % 4 * 8));
+    }
+    const int row = h * 16 + lane / 16 * 4;
+    return row * kRow + ((w * 4 ^ swizzle(row) << 4) | (lane % 16 * 4));
+  }
+  static __device__ __forceinline__ uint4v read(const char* lds, int at, int i) {
+    if constexpr (!TURNED) {
+      return *(const uint4v*)(lds + at + (i / 2 * 32 + i % 2 * 4) * kStageBytes);
+    } else if constexpr (sizeof(T) == 2) {
+      typedef __attribute__((address_space(3))) short4v* ptr;
+      const char* from = lds + (at ^ i * 32);
+      const uint2v x = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)from));
+      const uint2v y = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(from + 4 * kRow)));
+      return uint4v{x[0], x[1], y[0], y[1]};
+    } else {
+      const char* from = lds + (at ^ i * 64);
+      uint4v v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = *(const uint32_t*)(from + e * kRow);
+      return v;
+    }
+  }
+  // The place in the tile of element e of lane's row of fragment i, for P (rows of D), and of its column, for Q.
+  static __device__ __forceinline__ int column_of(int j, int lane) {
+    return TURNED ? 16 * j + lane % 16 : j / 2 * 32 + j % 2 * 4 + lane % 16 / 4 * 8 + lane % 4;
+  }
+};
+
+// Element c .. of a row of n at p, at any alignment; zeros past its end.
+template <typename T>
+__device__ __forceinline__ uint4v load_piece(const char* row, int64_t c, int64_t n) {
+  constexpr int N = kPiece<T>;
+  uint4v v = {};
+  if (c + N <= n) {
+    v = __builtin_bit_cast(uint4v, *(const Near<T, N>*)(row + c * (int64_t)sizeof(T)));
+  } else if (c < n && n >= N) {  // the row's last whole piece, moved down
+    typedef unsigned __int128 wide;
+    wide x = __builtin_bit_cast(wide, *(const Near<T, N>*)(row + (n - N) * (int64_t)sizeof(T)));
+    v = __builtin_bit_cast(uint4v, x >> ((int)(c + N - n) * 8 * (int)sizeof(T)));
+  } else {
+    Near<T, N> x = {};
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (c + e < n) x.v[e] = ((const T*)row)[c + e];
+    v = __builtin_bit_cast(uint4v, x);
+  }
+  return v;
+}
+
+// One operand's way from memory to LDS.
+//
+// DIRECT: straight into LDS, for addresses and lengths in whole pieces.  What is past an end has an offset out of the
+// buffer's range, for which the card writes zeros.  Else by registers, a stage ahead.
+constexpr uint32_t kNowhere = 0x80000000u;
+
+template <typename T, int BT, int NW, bool TURNED, bool DIRECT>
+struct Operand {
+  typedef Tile<T, BT, NW, TURNED> Lay;
+  static constexpr int kLoads = Lay::kLoads;
+  const char* at;   // of the tile at the next stage
+  int64_t step;     // bytes of a stage
+  int64_t row_bytes;
+  int32_t left;     // r from there on
+  int32_t extent;   // of the tile's own index
+  uint32_t off[DIRECT ? kLoads : 1];
+  uint4v held[DIRECT ? 1 : kLoads];
+  int lane, wave;
+
+  __device__ __forceinline__ void begin(const char* base, int64_t ld, int32_t extent_, int32_t r, int wave_,
+                                        int lane_) {
+    at = base;
+    row_bytes = ld * (int64_t)sizeof(T);
+    step = TURNED ? row_bytes * kStageLen<T> : (int64_t)kStageBytes;
+    left = r;
+    extent = extent_;
+    lane = lane_;
+    wave = wave_;
+    if constexpr (DIRECT) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int row = Lay::load_row(i, wave, lane), piece = Lay::load_piece(row, lane);
+        const bool inside = TURNED ? piece * kPiece<T> < extent : row < extent;
+        off[i] = inside ? (uint32_t)(row * (int32_t)row_bytes + piece * 16) : kNowhere;
+      }
+    }
+  }
+  // Asks for the next stage: into LDS, or into registers.
+  __device__ __forceinline__ void ask(char* lds) {
+    if constexpr (DIRECT) {
+      const __amdgpu_buffer_rsrc_t buffer = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, 0x7fffffff, 0x00020000);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int row = Lay::load_row(i, wave, lane), r = TURNED ? row : Lay::load_piece(row, lane) * kPiece<T>;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (lptr)(lds + (i * NW + wave) * 1024), 16,
+                                                 (int)(r < left ? off[i] : kNowhere), 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int row = Lay::load_row(i, wave, lane), c = Lay::load_piece(row, lane) * kPiece<T>;
+        uint4v v = {};
+        if (TURNED ? row < left : row < extent) v = load_piece<T>(at + row * row_bytes, c, TURNED ? extent : left);
+        held[i] = v;
+      }
+    }
+    at += step;
+    left -= kStageLen<T>;
+  }
+  // What was asked for into LDS, by registers.
+  __device__ __forceinline__ void put(char* lds) const {
+    if constexpr (!DIRECT) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) *(uint4v*)(lds + (i * NW + wave) * 1024 + lane * 16) = held[i];
+    }
+  }
+};
+
+// ----------------------------------------------------------------- products
+
+template <typename T>
+__device__ __forceinline__ float4v multiply(uint4v p, uint4v q, float4v c) {
+  if constexpr (std::is_same<T, _Float16>::value) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, p), __builtin_bit_cast(half8, q), c, 0, 0,
+                                                  0);
+  } else if constexpr (std::is_same<T, Bf16>::value) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bhalf8, p), __builtin_bit_cast(bhalf8, q), c, 0,
+                                                   0, 0);
+  } else {  // four r of each lane's group of lanes at a time
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(p[e]), __uint_as_float(q[e]), c, 0, 0, 0);
+    return c;
+  }
+}
+
+// N results of one row of D, columns p .. of n.
+template <typename T, int N>
+__device__ __forceinline__ void store(T* to, int64_t p, int64_t n, int accumulate, const float (&v)[N]) {
+  if (p + N <= n) {
+    Near<T, N> w;
+    if (accumulate) w = *(const Near<T, N>*)(to + p);
+#pragma unroll
+    for (int e = 0; e < N; ++e) w.v[e] = from_f32<T>(accumulate ? to_f32(w.v[e]) + v[e] : v[e]);
+    *(Near<T, N>*)(to + p) = w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (p + e < n) to[p + e] = from_f32<T>(accumulate ? to_f32(to[p + e]) + v[e] : v[e]);
+  }
+}
+
+// Part of a wavefront's tile: MI x NJ fragments at (wp, wq) of the tile at `out`, of which p < P and q < Q exist.
+template <int MODE, typename LP, typename LQ, int MI, int NJ, typename T>
+__device__ __forceinline__ void store_all(const ExpertArgs& a, T* out, int64_t P, int64_t Q, int wp, int wq, int lane,
+                                          const float4v (&acc)[MI][NJ]) {
+  constexpr bool PAIRS = MODE == FORWARD;  // two fragments' rows are adjacent
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int q = wq + LQ::column_of(j, lane);
+    if (q >= Q) continue;
+    T* to = out + q * a.out_ld;
+    const int accumulate = MODE == GRAD ? a.accumulate : 0;
+    if constexpr (PAIRS) {
+#pragma unroll
+      for (int i = 0; i < MI; i += 2) {
+        const float4v x = acc[i][j], y = acc[i + 1][j];
+        const float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+        store<T, 8>(to, wp + 16 * i + lane / 16 * 8, P, accumulate, v);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        const float4v x = acc[i][j];
+        const float v[4] = {x[0], x[1], x[2], x[3]};
+        store<T, 4>(to, wp + 16 * i + lane / 16 * 4, P, accumulate, v);
+      }
+    }
+  }
+}
+
+// One BP x BQ tile, WP x WQ of it per wavefront; NS stages in LDS.
+template <typename T, int MODE, int BP, int BQ, int WP, int WQ, int NS, bool DIRECT>
+__global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64) void k_expert(ExpertArgs a) {
+  constexpr int NW = BP / WP * (BQ / WQ);
+  constexpr int MI = WP / 16, NJ = WQ / 16;
+  typedef Operand<T, BP, NW, MODE != FORWARD, DIRECT> OpP;
+  typedef Operand<T, BQ, NW, MODE == GRAD, DIRECT> OpQ;
+  typedef typename OpP::Lay LP;
+  typedef typename OpQ::Lay LQ;
+  constexpr int kLoads = OpP::kLoads + OpQ::kLoads;
+  __shared__ __align__(16) char lds[NS][LP::kBytes + LQ::kBytes];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+  const int64_t worker = blockIdx.y;
+  const int per = MODE == GRAD ? a.tp * a.tq : a.tp;
+  Group g;
+  int id;
+  if (!find<MODE>(a, worker, blockIdx.x, per, &g, &id)) return;
+  int tp, tq;  // tile of P, and of Q or of the group's rows
+  {            // four rows of tiles at a time
+    const int across = MODE == GRAD ? a.tq : g.units;
+    if (MODE == GRAD) id -= g.unit * per;
+    const int four = id / (4 * a.tp), rows = min(4, across - 4 * four), in = id - four * 4 * a.tp;
+    tq = 4 * four + in % rows;
+    tp = in / rows;
+  }
+  OpP p;
+  OpQ q;
+  int32_t r;
+  int64_t extent_q, q0;
+  if (MODE == GRAD) {
+    const int64_t from = (int64_t)g.unit * a.rows;
+    const int64_t left = g.rows - from;
+    r = (int32_t)(left < a.rows ? left : a.rows);
+    const int64_t token = g.first + from;
+    q0 = (int64_t)tq * BQ;
+    extent_q = a.Q - q0;
+    p.begin((const char*)a.p + (worker * a.p_worker + token * a.p_ld + (int64_t)tp * BP) * (int64_t)sizeof(T), a.p_ld,
+            a.P - tp * BP, r, wave, lane);
+    q.begin((const char*)a.q + (worker * a.q_worker + token * a.q_ld + q0) * (int64_t)sizeof(T), a.q_ld,
+            (int32_t)extent_q, r, wave, lane);
+  } else {
+    r = a.R;
+    q0 = g.first + (int64_t)tq * BQ;
+    extent_q = g.rows - (int64_t)tq * BQ;
+    const int64_t at = g.e * a.p_expert + (int64_t)tp * BP * (MODE == FORWARD ? a.p_ld : 1);
+    p.begin((const char*)a.p + at * (int64_t)sizeof(T), a.p_ld, a.P - tp * BP, r, wave, lane);
+    q.begin((const char*)a.q + (worker * a.q_worker + q0 * a.q_ld) * (int64_t)sizeof(T), a.q_ld,
+            (int32_t)(extent_q < BQ ? extent_q : BQ), r, wave, lane);
+  }
+  const int wp = wave / (BQ / WQ) * WP, wq = wave % (BQ / WQ) * WQ;
+  const int p_at[2] = {LP::read_at(wp, 0, lane), LP::read_at(wp, 1, lane)};
+  const int q_at[2] = {LQ::read_at(wq, 0, lane), LQ::read_at(wq, 1, lane)};
+  float4v acc[MI][NJ] = {};
+  struct Frags {
+    uint4v p[MI], q[NJ];
+  };
+  auto read = [&](int s, int h, Frags& f) {
+    const char* from = lds[s];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) f.p[i] = LP::read(from, p_at[h], i);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) f.q[j] = LQ::read(from + LP::kBytes, q_at[h], j);
+  };
+  auto products = [&](const Frags& f) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] = multiply<T>(f.p[i], f.q[j], acc[i][j]);
+  };
+  auto ask = [&](int s) {
+    p.ask(lds[s]);
+    q.ask(lds[s] + LP::kBytes);
+  };
+  auto put = [&](int s) {
+    p.put(lds[s]);
+    q.put(lds[s] + LP::kBytes);
+  };
+
+  // Stage s: its first half is in registers.  Behind the barrier every wavefront has read all of it, and its loads of
+  // stage s + 1 are in LDS; its place goes to stage s + NS.  Stages past the last are asked for as well, and are
+  // zeros, so that the number of loads under way does not change.
+  const int stages = (r + kStageLen<T> - 1) / kStageLen<T>;
+  Frags f0, f1;
+  if constexpr (DIRECT) {
+#pragma unroll
+    for (int s = 0; s < NS; ++s) ask(s);
+    wait_for<(NS - 1) * kLoads, 0>();
+  } else {
+    static_assert(DIRECT || NS == 2, "two stages");
+    ask(0);
+    put(0);
+    ask(0);
+    put(1);
+    ask(0);
+    wait_for<63, 0>();
+  }
+  block_barrier();
+  read(0, 0, f0);
+  for (int s = 0, now = 0; s < stages; ++s) {
+    const int next = now + 1 == NS ? 0 : now + 1;
+    read(now, 1, f1);
+    products(f0);
+    wait_for<DIRECT ? (NS - 2) * kLoads : 63, 0>();
+    block_barrier();
+    put(now);
+    ask(now);
+    read(next, 0, f0);
+    products(f1);
+    now = next;
+  }
+  wait_for<0, 0>();  // what was asked for past the last stage
+
+  if constexpr (MODE == GRAD) {
+    if (g.units > 1) {
+      float* to = a.part + (((int64_t)worker * a.units + g.base + g.unit) * per + id) * (BP * BQ) + threadIdx.x * 4;
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) *(float4v*)(to + (i * NJ + j) * NW * 256) = acc[i][j];
+      return;
+    }
+    float* out = (float*)a.out + worker * a.out_worker + g.e * a.out_expert + q0 * a.out_ld + (int64_t)tp * BP;
+    store_all<MODE, LP, LQ>(a, out, a.P - tp * BP, extent_q, wp, wq, lane, acc);
+  } else {
+    const int64_t at = worker * a.out_worker + q0 * a.out_ld + (int64_t)tp * BP;
+    with_type_on_device(a.out_type, [&](auto* t) {
+      using O = std::remove_pointer_t<decltype(t)>;
+      store_all<MODE, LP, LQ>(a, (O*)a.out + at, a.P - tp * BP, extent_q, wp, wq, lane, acc);
+    });
+  }
+}
+
+// A tile of an expert whose tokens were shared: the shares' sums in order.  Block z of y of x: worker, expert, tile.
+template <typename T, int BP, int BQ, int WP, int WQ>
+__global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64) void k_join(ExpertArgs a) {
+  constexpr int NW = BP / WP * (BQ / WQ);
+  constexpr int MI = WP / 16, NJ = WQ / 16;
+  typedef Tile<T, BP, NW, true> LP;
+  typedef Tile<T, BQ, NW, true> LQ;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+  const int64_t worker = blockIdx.z;
+  const int e = blockIdx.y, per = a.tp * a.tq, tile = blockIdx.x;
+  int64_t first, rows;
+  const int n = units_of<GRAD>(a, worker, e, &first, &rows);
+  if (n == 1) return;
+  int base = 0;
+  for (int i = lane; i < e; i += 64) base += units_of<GRAD>(a, worker, i, &first, &rows);
+  base = __builtin_amdgcn_readlane(scan(base, lane), 63);
+  if (base + n > a.units) return;  // offsets that do not ascend
+  float4v acc[MI][NJ] = {};
+  const int64_t each = (int64_t)per * BP * BQ;
+  const float* from = a.part + ((int64_t)worker * a.units + base) * each + (int64_t)tile * BP * BQ + threadIdx.x * 4;
+  for (int u = 0; u < n; ++u, from += each)
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] += *(const float4v*)(from + (i * NJ + j) * NW * 256);
+  const int four = tile / (4 * a.tp), trows = min(4, a.tq - 4 * four), in = tile - four * 4 * a.tp;
+  const int tq = 4 * four + in % trows, tp = in / trows;
+  const int wp = wave / (BQ / WQ) * WP, wq = wave % (BQ / WQ) * WQ;
+  float* out = (float*)a.out + worker * a.out_worker + e * a.out_expert + (int64_t)tq * BQ * a.out_ld + (int64_t)tp * BP;
+  store_all<GRAD, LP, LQ>(a, out, a.P - tp * BP, a.Q - tq * BQ, wp, wq, lane, acc);
+}
+
+// --------------------------------------------------------------------- host
+
+enum { NARROW, MIDDLE, WIDE };  // tiles: 128 x 32, 128 x 128, 256 x 256
+
+struct Shape {
+  int32_t W, E;
+  int64_t T, n, k;
+};
+
+struct Plan {
+  int tile;
+  int32_t bp, bq, tp, tq, rows, units;
+  int64_t grid;        // blocks of a worker
+  size_t part_bytes;
+};
+
+constexpr int64_t kCUs = 256;
+constexpr int64_t kSplitBelow = 2 * kCUs;  // tiles of all workers and experts below which tokens are shared
+constexpr int64_t kMinShare = 256;         // tokens of a share, at least
+
+void finish_plan(Plan* p, const Shape& s, int mode) {
+  p->bp = p->tile == WIDE ? 256 : 128;
+  p->bq = p->tile == WIDE ? 256 : p->tile == MIDDLE ? 128 : 32;
+  p->tp = (int32_t)ceil_div(mode == FORWARD ? s.n : s.k, p->bp);
+  const int64_t some = s.T < s.E ? s.T : s.E;  // experts with rows, at most
+  int64_t units;
+  if (mode == GRAD) {
+    p->tq = (int32_t)ceil_div(s.n, p->bq);
+    units = s.T / p->rows + s.E;
+  } else {
+    p->tq = 1;
+    p->rows = p->bq;
+    units = (s.T + some * (p->bq - 1)) / p->bq;
+  }
+  p->units = (int32_t)units;
+  p->grid = ceil_div(units * p->tp * p->tq, 8) * 8;  // worker by worker on the same XCDs
+}
+
+// The form with shared tokens, whatever the operands' type and alignment.
+Plan shared_plan(const Shape& s) {
+  Plan p = {};
+  p.tile = MIDDLE;
+  const int64_t tiles = ceil_div(s.n, 128) * ceil_div(s.k, 128), all = s.W * s.E * tiles;
+  int64_t rows = s.T > 0 ? s.T : 1;
+  if (all < kSplitBelow) {
+    const int64_t share = ceil_div(ceil_div(s.W * s.T * tiles, kSplitBelow), 64) * 64;
+    rows = share < kMinShare ? kMinShare : share;
+  }
+  p.rows = (int32_t)rows;
+  finish_plan(&p, s, GRAD);
+  if (rows < s.T) p.part_bytes = (size_t)(s.W * p.units * tiles) * 128 * 128 * sizeof(float);
+  return p;
+}
+
+Plan plan_of(const Shape& s, int mode, int32_t type, bool direct) {
+  Plan p = {};
+  const bool wide = false;
+  if (mode == GRAD) {
+    if (!wide) return shared_plan(s);
+    p.tile = WIDE;
+    p.rows = (int32_t)(s.T > 0 ? s.T : 1);
+  } else {
+    p.tile = wide ? WIDE : MIDDLE;
+  }
+  finish_plan(&p, s, mode);
+  return p;
+}
+
+template <typename T, int MODE, bool DIRECT>
+void launch(const Plan& p, const Shape& s, const ExpertArgs& a, hipStream_t stream) {
+  const dim3 grid((unsigned)p.grid, (unsigned)s.W);
+  k_expert<T, MODE, 128, 128, 64, 64, 2, DIRECT><<<grid, 256, 0, stream>>>(a);
+}
+
+template <int MODE>
+hipError_t run(const Plan& p, const Shape& s, ExpertArgs a, int32_t type, bool direct, hipStream_t stream) {
+  a.tp = p.tp;
+  a.tq = p.tq;
+  a.rows = p.rows;
+  a.units = p.units;
+  with_type(type, [&](auto* t) {
+    using T = std::remove_pointer_t<decltype(t)>;
+    launch<T, MODE, false>(p, s, a, stream);
+    if constexpr (MODE == GRAD) {
+      if (p.part_bytes && hipPeekAtLastError() == hipSuccess)
+        k_join<T, 128, 128, 64, 64>
+            <<<dim3((unsigned)(p.tp * p.tq), (unsigned)s.E, (unsigned)s.W), 256, 0, stream>>>(a);
+    }
+  });
+  return hipGetLastError();
+}
+
+constexpr int64_t kMaxTokens = 1 << 24, kMaxSide = 1 << 20;
+
+nf_status bad(const char* what) { return set_error(NF_ERR_INVALID_ARG, what); }
+
+const char* check_sizes(int32_t W, int64_t T, int32_t E, int64_t n, int64_t k) {
+  if (W < 1 || W > 255) return "W outside [1, 255]";
+  if (T < 0 || T > kMaxTokens) return "T outside [0, 2^24]";
+  if (E < 0 || E > kMaxExperts) return "E outside [0, 4096]";
+  if (n < 0 || n > kMaxSide || k < 0 || k > kMaxSide) return "n or k outside [0, 2^20]";
+  return nullptr;
+}
+
+// Whether W x rows x cols elements lie as a caller says.
+bool misplaced(int32_t W, int64_t rows, int64_t cols, int64_t ld, int64_t stride) {
+  return ld < cols || (W > 1 && rows > 0 && overlaps(stride, rows, ld, cols));
+}
+
+bool whole(const void* p, int64_t ld, int64_t stride, int32_t type) {
+  const int64_t bytes = (int64_t)type_bytes(type);
+  return (uintptr_t)p % 16 == 0 && ld % (16 / bytes) == 0 && stride % (16 / bytes) == 0 && ld <= (1 << 20);
+}
+
+// A launch has under 2^32 threads, and every worker's tiles a number.
+bool too_large(const Plan& p, int32_t W) { return p.grid > (1 << 22) || p.grid * W > (1 << 22); }
+
+nf_status finish(hipError_t e) {
+  if (e != hipSuccess) return set_error(NF_ERR_HIP, hipGetErrorString(e));
+  return set_error(NF_OK, "");
+}
+
+}  // namespace
+}  // namespace nf
+
+extern "C" {
+
+nf_status nf_expert_product(const void* x, int32_t type, int64_t x_ld, int64_t x_stride, const void* w, int64_t w_ld,
+                            int64_t w_stride, int32_t transposed, const void* offsets, int32_t offsets_bytes,
+                            int64_t offsets_stride, int32_t W, int64_t T, int32_t E, int64_t n, int64_t k, void* y,
+                            int32_t y_type, int64_t y_ld, int64_t y_stride, void* stream) {
+  using namespace nf;
+  if (!known_type(type) || !known_type(y_type)) return bad("unknown element type");
+  if (transposed != 0 && transposed != 1) return bad("transposed must be 0 or 1");
+  if (offsets_bytes != 4 && offsets_bytes != 8) return bad("offsets_bytes must be 4 or 8");
+  if (const char* why = check_sizes(W, T, E, n, k)) return bad(why);
+  const int64_t in = transposed ? n : k, out = transposed ? k : n;
+  if (misplaced(W, T, in, x_ld, x_stride)) return bad("x_ld or x_stride too small");
+  if (misplaced(W, T, out, y_ld, y_stride)) return bad("y_ld or y_stride too small");
+  if (w_ld < k || (E > 1 && n > 0 && overlaps(w_stride, n, w_ld, k))) return bad("w_ld or w_stride too small");
+  if (W > 1 && offsets_stride < E + 1) return bad("offsets_stride < E + 1");
+  if (T == 0 || E == 0 || out == 0) return set_error(NF_OK, "");
+  if (!offsets || !y || (in > 0 && (!x || !w))) return bad("x, w, offsets or y is NULL");
+  if (y == x || y == w) return bad("y must not be x or w");
+  if ((uintptr_t)x % type_bytes(type) || (uintptr_t)w % type_bytes(type) || (uintptr_t)y % type_bytes(y_type) ||
+      (uintptr_t)offsets % offsets_bytes)
+    return set_error(NF_ERR_ALIGNMENT, "x, w, offsets or y not aligned to its elements");
+  const Shape s = {W, E, T, n, k};
+  const int64_t piece = 16 / (int64_t)type_bytes(type);
+  const bool direct = whole(x, x_ld, W > 1 ? x_stride : 0, type) && whole(w, w_ld, E > 1 ? w_stride : 0, type) &&
+                      k % piece == 0 && (!transposed || n % piece == 0);
+  const Plan p = plan_of(s, transposed ? BACKWARD : FORWARD, type, direct);
+  if (too_large(p, W)) return set_error(NF_ERR_UNSUPPORTED, "more tiles than a launch has");
+  ExpertArgs a = {};
+  a.p = w;
+  a.p_ld = w_ld;
+  a.p_expert = w_stride;
+  a.q = x;
+  a.q_ld = x_ld;
+  a.q_worker = x_stride;
+  a.offsets = offsets;
+  a.offsets_stride = offsets_stride;
+  a.offsets64 = offsets_bytes == 8;
+  a.T = T;
+  a.E = E;
+  a.P = (int32_t)out;
+  a.R = (int32_t)in;
+  a.out = y;
+  a.out_type = y_type;
+  a.out_ld = y_ld;
+  a.out_worker = y_stride;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  return finish(transposed ? run<BACKWARD>(p, s, a, type, direct, st) : run<FORWARD>(p, s, a, type, direct, st));
+}
+
+size_t nf_expert_grad_workspace_bytes(int32_t W, int64_t T, int32_t E, int64_t n, int64_t k) {
+  using namespace nf;
+  if (check_sizes(W, T, E, n, k) || T == 0 || E == 0 || n == 0 || k == 0) return 0;
+  return shared_plan(Shape{W, E, T, n, k}).part_bytes;
+}
+
+nf_status nf_expert_grad(const void* dy, int64_t dy_ld, int64_t dy_stride, const void* x, int64_t x_ld,
+                         int64_t x_stride, int32_t type, const void* offsets, int32_t offsets_bytes,
+                         int64_t offsets_stride, int32_t W, int64_t T, int32_t E, int64_t n, int64_t k,
+                         int32_t accumulate, float* grads, int64_t matrix_stride, int64_t worker_stride, void* ws,
+                         size_t ws_bytes, void* stream) {
+  using namespace nf;
+  if (!known_type(type)) return bad("unknown element type");
+  if (offsets_bytes != 4 && offsets_bytes != 8) return bad("offsets_bytes must be 4 or 8");
+  if (const char* why = check_sizes(W, T, E, n, k)) return bad(why);
+  if (misplaced(W, T, n, dy_ld, dy_stride)) return bad("dy_ld or dy_stride too small");
+  if (misplaced(W, T, k, x_ld, x_stride)) return bad("x_ld or x_stride too small");
+  if (accumulate != 0 && accumulate != 1) return bad("accumulate must be 0 or 1");
+  if (E > 1 && matrix_stride < n * k) return bad("matrix_stride < n * k");
+  if (W > 1 && E > 0 && overlaps(worker_stride, E, E > 1 ? matrix_stride : n * k, n * k))
+    return bad("worker_stride too small");
+  if (W > 1 && offsets_stride < E + 1) return bad("offsets_stride < E + 1");
+  if (E == 0 || n == 0 || k == 0) return set_error(NF_OK, "");
+  if (!offsets || !grads || (T > 0 && (!dy || !x))) return bad("dy, x, offsets or grads is NULL");
+  if ((uintptr_t)dy % type_bytes(type) || (uintptr_t)x % type_bytes(type) || (uintptr_t)grads % 4 ||
+      (uintptr_t)offsets % offsets_bytes)
+    return set_error(NF_ERR_ALIGNMENT, "dy, x, offsets or grads not aligned to its elements");
+  const Shape s = {W, E, T, n, k};
+  const int64_t piece = 16 / (int64_t)type_bytes(type);
+  const bool direct = whole(dy, dy_ld, W > 1 ? dy_stride : 0, type) && whole(x, x_ld, W > 1 ? x_stride : 0, type) &&
+                      n % piece == 0 && k % piece == 0;
+  const Plan p = plan_of(s, GRAD, type, direct);
+  if (too_large(p, W)) return set_error(NF_ERR_UNSUPPORTED, "more tiles than a launch has");
+  const size_t need = nf_expert_grad_workspace_bytes(W, T, E, n, k);
+  if (ws_bytes < need) return set_error(NF_ERR_WORKSPACE, "workspace smaller than nf_expert_grad_workspace_bytes");
+  if (need && !ws) return set_error(NF_ERR_WORKSPACE, "workspace is NULL");
+  if ((uintptr_t)ws % 256) return set_error(NF_ERR_ALIGNMENT, "workspace not 256-byte aligned");
+  ExpertArgs a = {};
+  a.p = x;
+  a.p_ld = x_ld;
+  a.p_worker = x_stride;
+  a.q = dy;
+  a.q_ld = dy_ld;
+  a.q_worker = dy_stride;
+  a.offsets = offsets;
+  a.offsets_stride = offsets_stride;
+  a.offsets64 = offsets_bytes == 8;
+  a.T = T;
+  a.E = E;
+  a.P = (int32_t)k;
+  a.Q = (int32_t)n;
+  a.out = grads;
+  a.accumulate = accumulate;
+  a.out_ld = k;
+  a.out_worker = worker_stride;
+  a.out_expert = matrix_stride;
+  a.part = static_cast<float*>(ws);
+  return finish(run<GRAD>(p, s, a, type, direct, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -51,6 +51,7 @@
 #include <type_traits>
 
 #include "nf_internal.h"
+#include "nf_tile.h"
 #include "nf_types.h"
 
 namespace nf {
@@ -305,9 +306,6 @@ __global__ __launch_bounds__(kNormThreads) void k_scale(PrepArgs a) {
 
 // ---------------------------------------------------------------- products
 
-typedef const __attribute__((address_space(1))) void* gptr;
-typedef __attribute__((address_space(3))) void* lptr;
-
 // BT rows of a panel (contiguous in src) into an LDS tile: each wavefront
 // moves sixteen rows (1 KiB) at a time straight into LDS, lane l the 16 bytes
 // that belong in the l-th slot.
@@ -348,19 +346,6 @@ __device__ __forceinline__ void load_tile(const _Float16* src, _Float16* lds, in
     const int rb = (i * NW + wave) * 16;
     __builtin_amdgcn_global_load_lds((gptr)(uintptr_t)(src + rb * kBK + place), (lptr)(lds + rb * kBK), 16, 0, 0);
   }
-}
-
-// Until at most N of this wavefront's loads into LDS, and R of its reads of LDS, are under way.
-template <int N, int R>
-__device__ __forceinline__ void wait_for() {
-  static_assert(N >= 0 && N < 64 && R >= 0 && R < 16, "the counters' ranges");
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(%1)" ::"n"(N), "n"(R) : "memory");
-}
-
-__device__ __forceinline__ void block_barrier() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
 }
 
 // Lanes 4q .. 4q + 3 hold a 4 x 4 block by columns (element e of lane i:

@@ -1,4 +1,4 @@
-// nf_types.h - element types of the training-step operators (nf_orthogonal.hip, nf_embedding.hip).
+// nf_types.h - element types of the training-step operators (nf_orthogonal.hip, nf_embedding.hip, nf_expert.hip, nf_norm.hip).
 #ifndef NF_TYPES_H
 #define NF_TYPES_H
 
@@ -51,6 +51,16 @@ struct __attribute__((packed)) Near {
 // Calls f with a null pointer of the type's element.
 template <typename F>
 inline void with_type(int32_t t, F f) {
+  if (t == NF_TYPE_F32)
+    f((float*)nullptr);
+  else if (t == NF_TYPE_BF16)
+    f((Bf16*)nullptr);
+  else
+    f((_Float16*)nullptr);
+}
+
+template <typename F>
+__device__ __forceinline__ void with_type_on_device(int32_t t, F f) {
   if (t == NF_TYPE_F32)
     f((float*)nullptr);
   else if (t == NF_TYPE_BF16)
