@@ -579,14 +579,21 @@ Plan shared_plan(const Shape& s) {
 }
 
 Plan plan_of(const Shape& s, int mode, int32_t type, bool direct) {
-  Plan p = {};
-  const bool wide = false;
+  const int64_t rows = s.T / (s.E > 0 ? s.E : 1);  // of an expert, on average
+  const int64_t len = mode == GRAD || mode == BACKWARD ? s.k : s.n;
+  const int64_t other = mode == GRAD ? s.n : rows;
+  bool wide = direct && type != NF_TYPE_F32 && len >= 192 && other >= 192;
   if (mode == GRAD) {
-    if (!wide) return shared_plan(s);
+    const Plan shared = shared_plan(s);
+    if (!wide || s.W * s.E * ceil_div(s.n, 256) * ceil_div(s.k, 256) < kCUs) return shared;
+  }
+  Plan p = {};
+  if (mode == GRAD) {
     p.tile = WIDE;
     p.rows = (int32_t)(s.T > 0 ? s.T : 1);
   } else {
-    p.tile = wide ? WIDE : MIDDLE;
+    wide = wide && ceil_div(s.T, 256) * s.W * ceil_div(len, 256) >= kCUs;
+    p.tile = wide ? WIDE : rows <= 48 ? NARROW : MIDDLE;
   }
   finish_plan(&p, s, mode);
   return p;
@@ -595,6 +602,18 @@ Plan plan_of(const Shape& s, int mode, int32_t type, bool direct) {
 template <typename T, int MODE, bool DIRECT>
 void launch(const Plan& p, const Shape& s, const ExpertArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)p.grid, (unsigned)s.W);
+  if constexpr (DIRECT && sizeof(T) == 2) {
+    if (p.tile == WIDE) {
+      k_expert<T, MODE, 256, 256, 128, 64, 2, true><<<grid, 512, 0, stream>>>(a);
+      return;
+    }
+  }
+  if constexpr (MODE != GRAD) {
+    if (p.tile == NARROW) {
+      k_expert<T, MODE, 128, 32, 32, 32, DIRECT ? 4 : 2, DIRECT><<<grid, 256, 0, stream>>>(a);
+      return;
+    }
+  }
   k_expert<T, MODE, 128, 128, 64, 64, 2, DIRECT><<<grid, 256, 0, stream>>>(a);
 }
 
@@ -606,7 +625,10 @@ hipError_t run(const Plan& p, const Shape& s, ExpertArgs a, int32_t type, bool d
   a.units = p.units;
   with_type(type, [&](auto* t) {
     using T = std::remove_pointer_t<decltype(t)>;
-    launch<T, MODE, false>(p, s, a, stream);
+    if (direct)
+      launch<T, MODE, true>(p, s, a, stream);
+    else
+      launch<T, MODE, false>(p, s, a, stream);
     if constexpr (MODE == GRAD) {
       if (p.part_bytes && hipPeekAtLastError() == hipSuccess)
         k_join<T, 128, 128, 64, 64>
