@@ -58,6 +58,7 @@ struct ExpertArgs {
   int64_t out_ld, out_worker, out_expert;
   float* part;                     // GRAD: sums of shares, [worker][unit][tile][elements]
   int32_t units;                   // most units of a worker: rounds up what any sizes need
+  int32_t spread;                  // GRAD: see find()
 };
 
 // ------------------------------------------------------------ groups of rows
@@ -104,6 +105,26 @@ template <int MODE>
 __device__ __forceinline__ bool find(const ExpertArgs& a, int64_t worker, int block, int per, Group* g, int* id) {
   const int lane = threadIdx.x % 64, each = (a.E + 63) / 64;
   int64_t first, rows;
+  if (MODE == GRAD && a.spread) {
+    // Tiles of long and short experts cost their tokens: every XCD takes an eighth of each expert's tiles, longest first.
+    const int x = block & 7, j = block >> 3, lo = x * per >> 3, n = ((x + 1) * per >> 3) - lo, u = j / n;
+    if (u >= a.E) return false;
+    units_of<MODE>(a, worker, min(lane, a.E - 1), &first, &rows);
+    const int mine = lane < a.E ? (int)rows : -1;
+    int rank = 0;
+    for (int m = 0; m < a.E; ++m) {
+      const int other = __builtin_amdgcn_readlane(mine, m);
+      rank += other > mine || (other == mine && m < lane);
+    }
+    const int at = __builtin_ctzll(__ballot(lane < a.E && rank == u));
+    g->e = at;
+    g->unit = g->base = 0;
+    g->units = 1;
+    g->first = __builtin_amdgcn_readlane((int)first, at);
+    g->rows = __builtin_amdgcn_readlane(mine, at);
+    *id = lo + j - u * n;
+    return true;
+  }
   int mine = 0;
   for (int j = 0; j < each; ++j)
     if (lane * each + j < a.E) mine += units_of<MODE>(a, worker, lane * each + j, &first, &rows);
@@ -150,18 +171,19 @@ constexpr int kStageLen = kStageBytes / (int)sizeof(T);  // r of a stage
 // which a transposing read gives each lane four rows of one, from 32 bytes of each of four rows; those go to slots
 // that differ in the eight rows that are read at a time.  FP32 elements are read one by one, 64 bytes of four rows
 // four apart.
-template <typename T, int BT, int NW, bool TURNED>
+template <typename T, int BT, int NW, bool TURNED, bool PAIRS = false>
 struct Tile {
   static constexpr int kBytes = BT * kStageBytes;
   static constexpr int kLoads = BT / 8 / NW;  // of a wavefront, 1 KiB each
   static constexpr int kRow = TURNED ? BT * (int)sizeof(T) : kStageBytes;
   static constexpr int kRows = 1024 / kRow;  // of one load
+  static constexpr int kReads = !TURNED ? 1 : sizeof(T) == 2 ? 2 : 4;  // of LDS, a fragment
   static_assert(BT % (8 * NW) == 0 && kRow <= 1024, "whole loads");
 
   static __device__ __forceinline__ int swizzle(int row) {
     if (!TURNED) {
       const int q = row >> 3;
-      return ((q >> 1) & 1) | (((q ^ (q >> 1)) & 1) << 1) | ((row & 2) << 1);
+      return PAIRS ? ((q >> 1) & 1) | (((q ^ (q >> 1)) & 1) << 1) | ((row & 2) << 1) : (row >> 1) & 7;
     }
     if (sizeof(T) == 2) return (row & 3) << 1 | (row & 8);
     return row & 12;
@@ -172,39 +194,43 @@ struct Tile {
   }
   static __device__ __forceinline__ int load_piece(int row, int lane) { return (lane % (kRow / 16)) ^ swizzle(row); }
 
-  // The bytes at which a lane reads fragment 0 of the tile's part that begins at row or column w, of half h.
-  static __device__ __forceinline__ int read_at(int w, int h, int lane) {
+  // The bytes at which a lane reads fragment 0, first half, of the tile's part that begins at row or column w.
+  static __device__ __forceinline__ uint32_t read_at(int w, int lane) {
     if (!TURNED) {
-      const int row = w + lane % 16 / 4 * 8 + lane % 4;
-      return row * kStageBytes + (((h * 4 + lane / 16) ^ swizzle(row)) << 4);
+      const int row = w + (PAIRS ? lane % 16 / 4 * 8 + lane % 4 : lane % 16);
+      return row * kStageBytes + ((lane / 16 ^ swizzle(row)) << 4);
     }
     if (sizeof(T) == 2) {
-      const int row = h * 32 + lane / 16 * 8 + lane % 16 / 4;
+      const int row = lane / 16 * 8 + lane % 16 / 4;
       return row * kRow + ((w * 2 ^ swizzle(row) << 4) | (lane % 4 * 8));
     }
-    const int row = h * 16 + lane / 16 * 4;
+    const int row = lane / 16 * 4;
     return row * kRow + ((w * 4 ^ swizzle(row) << 4) | (lane % 16 * 4));
   }
-  static __device__ __forceinline__ uint4v read(const char* lds, int at, int i) {
+  // Fragment i of half h; `at`: read_at's place in LDS.  What a fragment adds to it is a constant, or changes bits that
+  // the rows' beginnings leave zero.
+  static __device__ __forceinline__ uint4v read(uint32_t at, int i, int h) {
     if constexpr (!TURNED) {
-      return *(const uint4v*)(lds + at + (i / 2 * 32 + i % 2 * 4) * kStageBytes);
+      typedef const __attribute__((address_space(3))) uint4v* ptr;
+      return *(ptr)(uintptr_t)((at ^ h * 64) + (PAIRS ? i / 2 * 32 + i % 2 * 4 : i * 16) * kStageBytes);
     } else if constexpr (sizeof(T) == 2) {
       typedef __attribute__((address_space(3))) short4v* ptr;
-      const char* from = lds + (at ^ i * 32);
-      const uint2v x = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)from));
-      const uint2v y = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(from + 4 * kRow)));
+      const uint32_t from = (at ^ i * 32) + h * 32 * kRow;
+      const uint2v x = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(uintptr_t)from));
+      const uint2v y = __builtin_bit_cast(uint2v, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(uintptr_t)(from + 4 * kRow)));
       return uint4v{x[0], x[1], y[0], y[1]};
     } else {
-      const char* from = lds + (at ^ i * 64);
+      typedef const __attribute__((address_space(3))) uint32_t* ptr;
+      const uint32_t from = (at ^ i * 64) + h * 16 * kRow;
       uint4v v;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = *(const uint32_t*)(from + e * kRow);
+      for (int e = 0; e < 4; ++e) v[e] = *(ptr)(uintptr_t)(from + e * kRow);
       return v;
     }
   }
   // The place in the tile of element e of lane's row of fragment i, for P (rows of D), and of its column, for Q.
   static __device__ __forceinline__ int column_of(int j, int lane) {
-    return TURNED ? 16 * j + lane % 16 : j / 2 * 32 + j % 2 * 4 + lane % 16 / 4 * 8 + lane % 4;
+    return 16 * j + lane % 16;
   }
 };
 
@@ -229,15 +255,32 @@ __device__ __forceinline__ uint4v load_piece(const char* row, int64_t c, int64_t
   return v;
 }
 
+__device__ __forceinline__ uint64_t uniform(uint64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+  return (uint64_t)hi << 32 | lo;
+}
+
 // One operand's way from memory to LDS.
 //
 // DIRECT: straight into LDS, for addresses and lengths in whole pieces.  What is past an end has an offset out of the
 // buffer's range, for which the card writes zeros.  Else by registers, a stage ahead.
 constexpr uint32_t kNowhere = 0x80000000u;
 
-template <typename T, int BT, int NW, bool TURNED, bool DIRECT>
+// 16 bytes a lane from base + off to LDS, lane after lane from `lds` on; zeros for off = kNowhere.  Written out
+// because the compiler, where it knows of such a load, waits for it before each transposing read of LDS.  It has no
+// result in registers, and who reads what it brings waits by wait_for().
+__device__ __forceinline__ void load_to_lds(const char* base, uint32_t lds, uint32_t off) {
+  typedef uint32_t uint4s __attribute__((ext_vector_type(4)));
+  const uint64_t at = (uint64_t)(uintptr_t)base;
+  const uint4s buffer = {(uint32_t)at, (uint32_t)(at >> 32), 0x7fffffffu, 0x00020000u};
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off),
+               "s"(buffer)
+               : "memory");
+}
+
+template <typename T, int BT, int NW, bool TURNED, bool PAIRS, bool DIRECT>
 struct Operand {
-  typedef Tile<T, BT, NW, TURNED> Lay;
+  typedef Tile<T, BT, NW, TURNED, PAIRS> Lay;
   static constexpr int kLoads = Lay::kLoads;
   const char* at;   // of the tile at the next stage
   int64_t step;     // bytes of a stage
@@ -250,11 +293,11 @@ struct Operand {
 
   __device__ __forceinline__ void begin(const char* base, int64_t ld, int32_t extent_, int32_t r, int wave_,
                                         int lane_) {
-    at = base;
+    at = (const char*)uniform((uint64_t)(uintptr_t)base);
     row_bytes = ld * (int64_t)sizeof(T);
     step = TURNED ? row_bytes * kStageLen<T> : (int64_t)kStageBytes;
-    left = r;
-    extent = extent_;
+    left = __builtin_amdgcn_readfirstlane(r);
+    extent = __builtin_amdgcn_readfirstlane(extent_);
     lane = lane_;
     wave = wave_;
     if constexpr (DIRECT) {
@@ -264,35 +307,46 @@ struct Operand {
         const bool inside = TURNED ? piece * kPiece<T> < extent : row < extent;
         off[i] = inside ? (uint32_t)(row * (int32_t)row_bytes + piece * 16) : kNowhere;
       }
+      if (left < kStageLen<T>) shorten();
     }
   }
-  // Asks for the next stage: into LDS, or into registers.
-  __device__ __forceinline__ void ask(char* lds) {
-    if constexpr (DIRECT) {
-      const __amdgpu_buffer_rsrc_t buffer = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, 0x7fffffff, 0x00020000);
+  // The stage that is next ends before its place does.
+  __device__ __forceinline__ void shorten() {
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int row = Lay::load_row(i, wave, lane), r = TURNED ? row : Lay::load_piece(row, lane) * kPiece<T>;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (lptr)(lds + (i * NW + wave) * 1024), 16,
-                                                 (int)(r < left ? off[i] : kNowhere), 0, 0, 0);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int row = Lay::load_row(i, wave, lane), c = Lay::load_piece(row, lane) * kPiece<T>;
-        uint4v v = {};
-        if (TURNED ? row < left : row < extent) v = load_piece<T>(at + row * row_bytes, c, TURNED ? extent : left);
-        held[i] = v;
-      }
+    for (int i = 0; i < kLoads; ++i) {
+      const int row = Lay::load_row(i, wave, lane);
+      if ((TURNED ? row : Lay::load_piece(row, lane) * kPiece<T>) >= left) off[i] = kNowhere;
     }
+  }
+  // Asks for the next stage: into LDS, or into registers.  In parts, for the loads to be placed one by one: load i of
+  // the stage, and on to the next one.
+  __device__ __forceinline__ void ask(uint32_t lds, int i) {
+    if constexpr (DIRECT) {
+      load_to_lds(at, lds + (i * NW + wave) * 1024, off[i]);
+    } else {
+      const int row = Lay::load_row(i, wave, lane), c = Lay::load_piece(row, lane) * kPiece<T>;
+      uint4v v = {};
+      if (TURNED ? row < left : row < extent) v = load_piece<T>(at + row * row_bytes, c, TURNED ? extent : left);
+      held[i] = v;
+    }
+  }
+  __device__ __forceinline__ void on() {
     at += step;
     left -= kStageLen<T>;
+    if constexpr (DIRECT)
+      if (left < kStageLen<T>) shorten();
+  }
+  __device__ __forceinline__ void ask(uint32_t lds) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) ask(lds, i);
+    on();
   }
   // What was asked for into LDS, by registers.
-  __device__ __forceinline__ void put(char* lds) const {
+  __device__ __forceinline__ void put(uint32_t lds) const {
+    typedef __attribute__((address_space(3))) uint4v* ptr;
     if constexpr (!DIRECT) {
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) *(uint4v*)(lds + (i * NW + wave) * 1024 + lane * 16) = held[i];
+      for (int i = 0; i < kLoads; ++i) *(ptr)(uintptr_t)(lds + (i * NW + wave) * 1024 + lane * 16) = held[i];
     }
   }
 };
@@ -312,6 +366,21 @@ __device__ __forceinline__ float4v multiply(uint4v p, uint4v q, float4v c) {
     for (int e = 0; e < 4; ++e)
       c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(p[e]), __uint_as_float(q[e]), c, 0, 0, 0);
     return c;
+  }
+}
+
+template <typename T>
+constexpr int kMfmas = sizeof(T) == 2 ? 1 : 4;  // of multiply
+
+// Asks the compiler to spread READS reads of LDS evenly between MFMAS matrix instructions, so that neither waits for a
+// burst of the other.
+template <int READS, int MFMAS>
+__device__ __forceinline__ void spread() {
+  constexpr int kEach = MFMAS / READS > 0 ? MFMAS / READS : 1;
+#pragma unroll
+  for (int i = 0; i < READS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
   }
 }
 
@@ -362,15 +431,15 @@ __device__ __forceinline__ void store_all(const ExpertArgs& a, T* out, int64_t P
 
 // One BP x BQ tile, WP x WQ of it per wavefront; NS stages in LDS.
 template <typename T, int MODE, int BP, int BQ, int WP, int WQ, int NS, bool DIRECT>
-__global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64) void k_expert(ExpertArgs a) {
+__global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, BP / WP * (BQ / WQ) == 8 ? 1 : 2) void k_expert(ExpertArgs a) {
   constexpr int NW = BP / WP * (BQ / WQ);
   constexpr int MI = WP / 16, NJ = WQ / 16;
-  typedef Operand<T, BP, NW, MODE != FORWARD, DIRECT> OpP;
-  typedef Operand<T, BQ, NW, MODE == GRAD, DIRECT> OpQ;
+  typedef Operand<T, BP, NW, MODE != FORWARD, true, DIRECT> OpP;
+  typedef Operand<T, BQ, NW, MODE == GRAD, false, DIRECT> OpQ;
   typedef typename OpP::Lay LP;
   typedef typename OpQ::Lay LQ;
   constexpr int kLoads = OpP::kLoads + OpQ::kLoads;
-  __shared__ __align__(16) char lds[NS][LP::kBytes + LQ::kBytes];
+  __shared__ __align__(1024) char lds[NS * (LP::kBytes + LQ::kBytes)];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   const int64_t worker = blockIdx.y;
   const int per = MODE == GRAD ? a.tp * a.tq : a.tp;
@@ -409,66 +478,96 @@ __global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64) void k_expert(ExpertArgs 
     q.begin((const char*)a.q + (worker * a.q_worker + q0 * a.q_ld) * (int64_t)sizeof(T), a.q_ld,
             (int32_t)(extent_q < BQ ? extent_q : BQ), r, wave, lane);
   }
-  const int wp = wave / (BQ / WQ) * WP, wq = wave % (BQ / WQ) * WQ;
-  const int p_at[2] = {LP::read_at(wp, 0, lane), LP::read_at(wp, 1, lane)};
-  const int q_at[2] = {LQ::read_at(wq, 0, lane), LQ::read_at(wq, 1, lane)};
+  const int wp = wave % (BP / WP) * WP, wq = wave / (BP / WP) * WQ;
+  constexpr int kStage = LP::kBytes + LQ::kBytes;
+  const uint32_t lds_at = (uint32_t)(uintptr_t)(lptr)lds;
+  const uint32_t p_at = lds_at + LP::read_at(wp, lane), q_at = lds_at + LP::kBytes + LQ::read_at(wq, lane);
   float4v acc[MI][NJ] = {};
   struct Frags {
     uint4v p[MI], q[NJ];
   };
-  auto read = [&](int s, int h, Frags& f) {
-    const char* from = lds[s];
+  auto read = [&](uint32_t stage, int h, Frags& f) {
 #pragma unroll
-    for (int i = 0; i < MI; ++i) f.p[i] = LP::read(from, p_at[h], i);
+    for (int i = 0; i < MI; ++i) f.p[i] = LP::read(p_at + stage, i, h);
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) f.q[j] = LQ::read(from + LP::kBytes, q_at[h], j);
+    for (int j = 0; j < NJ; ++j) f.q[j] = LQ::read(q_at + stage, j, h);
   };
-  auto products = [&](const Frags& f) {
+  constexpr int kAll = MI * NJ;
+  auto products = [&](const Frags& f, int from, int to) {
 #pragma unroll
-    for (int i = 0; i < MI; ++i)
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) acc[i][j] = multiply<T>(f.p[i], f.q[j], acc[i][j]);
+    for (int m = from; m < to; ++m) acc[m / NJ][m % NJ] = multiply<T>(f.p[m / NJ], f.q[m % NJ], acc[m / NJ][m % NJ]);
   };
-  auto ask = [&](int s) {
-    p.ask(lds[s]);
-    q.ask(lds[s] + LP::kBytes);
+  auto ask = [&](uint32_t stage) {
+    p.ask(lds_at + stage);
+    q.ask(lds_at + stage + LP::kBytes);
   };
-  auto put = [&](int s) {
-    p.put(lds[s]);
-    q.put(lds[s] + LP::kBytes);
+  auto put = [&](uint32_t stage) {
+    p.put(lds_at + stage);
+    q.put(lds_at + stage + LP::kBytes);
   };
 
   // Stage s: its first half is in registers.  Behind the barrier every wavefront has read all of it, and its loads of
   // stage s + 1 are in LDS; its place goes to stage s + NS.  Stages past the last are asked for as well, and are
   // zeros, so that the number of loads under way does not change.
-  const int stages = (r + kStageLen<T> - 1) / kStageLen<T>;
+  const int stages = __builtin_amdgcn_readfirstlane((r + kStageLen<T> - 1) / kStageLen<T>);
   Frags f0, f1;
   if constexpr (DIRECT) {
 #pragma unroll
-    for (int s = 0; s < NS; ++s) ask(s);
+    for (int s = 0; s < NS; ++s) ask(s * kStage);
     wait_for<(NS - 1) * kLoads, 0>();
   } else {
     static_assert(DIRECT || NS == 2, "two stages");
     ask(0);
     put(0);
     ask(0);
-    put(1);
+    put(kStage);
     ask(0);
     wait_for<63, 0>();
   }
   block_barrier();
-  read(0, 0, f0);
-  for (int s = 0, now = 0; s < stages; ++s) {
-    const int next = now + 1 == NS ? 0 : now + 1;
-    read(now, 1, f1);
-    products(f0);
-    wait_for<DIRECT ? (NS - 2) * kLoads : 63, 0>();
-    block_barrier();
-    put(now);
-    ask(now);
-    read(next, 0, f0);
-    products(f1);
-    now = next;
+  uint32_t now = 0;
+  if (wq >= extent_q) {  // none of this wavefront's rows exist: it only loads
+    for (int s = 0; s < stages; ++s) {
+      wait_for<DIRECT ? (NS - 2) * kLoads : 63, 0>();
+      block_barrier();
+      put(now);
+      ask(now);
+      now = now + kStage == NS * kStage ? 0 : now + kStage;
+    }
+  } else {
+    read(0, 0, f0);
+    for (int s = 0; s < stages; ++s) {
+      const uint32_t next = now + kStage == NS * kStage ? 0 : now + kStage;
+      read(now, 1, f1);
+      products(f0, 0, kAll);
+      spread<(LP::kReads * MI + LQ::kReads * NJ), kAll * kMfmas<T>>();
+      __builtin_amdgcn_sched_barrier(0);
+      wait_for<DIRECT ? (NS - 2) * kLoads : 63, 0>();
+      block_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      constexpr int kSome = kAll >= 2 * kLoads ? kLoads : 0;  // products between the loads
+      if constexpr (DIRECT) {
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) {
+          if (n < OpP::kLoads)
+            p.ask(lds_at + now, n);
+          else
+            q.ask(lds_at + now + LP::kBytes, n - OpP::kLoads);
+          if (kSome) products(f1, n, n + 1);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        p.on();
+        q.on();
+      } else {
+        put(now);
+        ask(now);
+      }
+      read(next, 0, f0);
+      products(f1, DIRECT ? kSome : 0, kAll);
+      if (DIRECT) spread<(LP::kReads * MI + LQ::kReads * NJ), (kAll - kSome) * kMfmas<T>>();
+      __builtin_amdgcn_sched_barrier(0);
+      now = next;
+    }
   }
   wait_for<0, 0>();  // what was asked for past the last stage
 
@@ -519,7 +618,7 @@ __global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64) void k_join(ExpertArgs a)
       for (int j = 0; j < NJ; ++j) acc[i][j] += *(const float4v*)(from + (i * NJ + j) * NW * 256);
   const int four = tile / (4 * a.tp), trows = min(4, a.tq - 4 * four), in = tile - four * 4 * a.tp;
   const int tq = 4 * four + in % trows, tp = in / trows;
-  const int wp = wave / (BQ / WQ) * WP, wq = wave % (BQ / WQ) * WQ;
+  const int wp = wave % (BP / WP) * WP, wq = wave / (BP / WP) * WQ;
   float* out = (float*)a.out + worker * a.out_worker + e * a.out_expert + (int64_t)tq * BQ * a.out_ld + (int64_t)tp * BP;
   store_all<GRAD, LP, LQ>(a, out, a.P - tp * BP, a.Q - tq * BQ, wp, wq, lane, acc);
 }
@@ -535,7 +634,7 @@ struct Shape {
 
 struct Plan {
   int tile;
-  int32_t bp, bq, tp, tq, rows, units;
+  int32_t bp, bq, tp, tq, rows, units, spread;
   int64_t grid;        // blocks of a worker
   size_t part_bytes;
 };
@@ -552,14 +651,16 @@ void finish_plan(Plan* p, const Shape& s, int mode) {
   int64_t units;
   if (mode == GRAD) {
     p->tq = (int32_t)ceil_div(s.n, p->bq);
-    units = s.T / p->rows + s.E;
+    units = p->rows < s.T ? s.T / p->rows + s.E : s.E;
   } else {
     p->tq = 1;
     p->rows = p->bq;
     units = (s.T + some * (p->bq - 1)) / p->bq;
   }
   p->units = (int32_t)units;
-  p->grid = ceil_div(units * p->tp * p->tq, 8) * 8;  // worker by worker on the same XCDs
+  const int64_t per = (int64_t)p->tp * p->tq;
+  p->spread = mode == GRAD && units == s.E && s.E <= 64 && per >= 16;
+  p->grid = p->spread ? 8 * s.E * ceil_div(per, 8) : ceil_div(units * per, 8) * 8;  // workers begin on the same XCD
 }
 
 // The form with shared tokens, whatever the operands' type and alignment.
@@ -623,6 +724,7 @@ hipError_t run(const Plan& p, const Shape& s, ExpertArgs a, int32_t type, bool d
   a.tq = p.tq;
   a.rows = p.rows;
   a.units = p.units;
+  a.spread = p.spread;
   with_type(type, [&](auto* t) {
     using T = std::remove_pointer_t<decltype(t)>;
     if (direct)

@@ -91,6 +91,19 @@ def test_product(W, E, T, n, k, extra, kind, out, back):
                   offsets=torch.int64 if T % 2 else torch.int32)
 
 
+@pytest.mark.parametrize("kind,out", [("bf16", "bf16"), ("f16", "f32")])
+@pytest.mark.parametrize("W,E,T,n,k,back", [
+    (1, 4, 16_500, 1032, 264, False), (1, 4, 16_500, 264, 1032, True), (2, 3, 9_000, 1024, 200, False),
+    (2, 3, 9_000, 72, 1024, True), (1, 2, 66_000, 192, 64, False), (1, 30, 8_000, 2056, 320, False)])
+def test_product_wide_tiles(W, E, T, n, k, back, kind, out):
+    """Sizes that take tiles of 256, their lengths ending inside stages and tiles; an expert of a single row."""
+    g = torch.Generator().manual_seed(T)
+    sizes = random_sizes(g, W, E, T - 300)
+    sizes[0][0] = 1 if E > 2 else 40_000 if T > 60_000 else sizes[0][0]
+    assert all(sum(row) <= T for row in sizes)
+    check_product(W, E, T, n, k, back, kind, out, sizes=sizes, seed=1)
+
+
 @pytest.mark.parametrize("back", [False, True])
 def test_sizes_at_the_edges_of_tiles(back):
     for sizes in ([0, 0, 0, 0], [31, 32, 33, 1], [127, 0, 128, 129], [255, 256, 257, 0], [0, 0, 513, 0], [1, 1, 1, 1]):
@@ -178,6 +191,14 @@ GRADS = [  # W, E, T, n, k, extra, lead, gap
 def test_grad(W, E, T, n, k, extra, lead, gap, kind, accumulate):
     check_grad(W, E, T, n, k, kind, extra=extra, lead=lead, gap=gap, accumulate=accumulate, seed=T + n,
                offsets=torch.int64 if T % 2 else torch.int32)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("W,E,T,n,k", [(1, 4, 900, 2056, 2040), (2, 33, 300, 1032, 1048), (1, 64, 500, 512, 520)])
+def test_grad_wide_tiles(W, E, T, n, k, kind, accumulate):
+    """Sizes that take tiles of 256: experts by length over all XCDs, and (few tiles an expert) one after the other."""
+    check_grad(W, E, T, n, k, kind, lead=3, accumulate=accumulate, seed=E)
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
