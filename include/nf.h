@@ -801,6 +801,80 @@ nf_status nf_expert_grad(const void* dy, int64_t dy_ld, int64_t dy_stride, const
                          size_t ws_bytes, void* stream);
 
 /*
+ * Norms over many tensors, each of one group's tensors (a worker's gradients,
+ * a kind of parameter), and the tensors scaled by them (no paper
+ * counterpart).  With ||g|| the 2-norm of all elements of group g:
+ *   norms[g] = ||g||
+ *   dst = min(1, max_norm / (norms[g] + eps)) src    (1 where norms[g] + eps = 0)
+ * Squares and their sums are FP64 in a fixed order, a norm is rounded once to
+ * FP32; the factor is rounded to FP32 and the product taken in FP32 and
+ * rounded once to dst's type.  An infinity in a group makes its norm infinite
+ * and the factor zero, which leaves zeros, and NaN where the infinities were;
+ * a NaN makes the norm and all of dst NaN.  A group without elements has the
+ * norm 0.
+ *
+ * A tensor is rows x cols elements, those of a row adjacent, rows src_ld
+ * (dst_ld) apart; of more dimensions it is several of these.  dst may be
+ * another place and type than src (a gradient into its place in the worker's
+ * FP32 row), the same (in place: a factor of 1 then neither reads nor
+ * writes), or NULL where only norms are asked for.
+ */
+typedef struct {
+  const void* src;
+  void* dst;
+  int64_t rows, cols, src_ld, dst_ld;  /* the ld of one row is not read        */
+  int32_t src_type, dst_type;          /* NF_TYPE_*                            */
+  int32_t group;                       /* in [0, groups)                       */
+  int32_t reserved;
+} nf_norm_tensor;
+
+typedef struct {
+  int64_t pieces, blocks;
+  int32_t groups;
+  int32_t writes;          /* every tensor has a dst                           */
+  size_t table_bytes, workspace_bytes;
+} nf_norm_plan;
+
+/*
+ * What the tensors of a model need, and the device table that the kernels
+ * find them by, built once for as long as they stay where they are:
+ *   nf_norm_plan_init   checks the tensors and fills in the plan (host only)
+ *   nf_norm_table_init  builds the table on the host and copies it into
+ *                       `table` (device, caller-owned, 256-byte aligned, at
+ *                       least plan.table_bytes), then synchronises `stream`:
+ *                       a set-up call, not for the step loop
+ * NF_ERR_INVALID_ARG: count outside [0, 2^20], groups outside [0, 2^16], a
+ * group outside [0, groups), sizes < 0, an ld < cols with rows > 1, src NULL,
+ * an element that is written belonging to two tensors or to two places of one
+ * (a tensor that is listed twice may be read, and counts twice), a plan of
+ * other tensors.  NF_ERR_ALIGNMENT: a pointer not aligned to its elements.
+ * NF_ERR_UNSUPPORTED: more than 2^24 pieces (of up to 2^15 elements, or a row
+ * of more) or 2^22 rows of tensors that lie between one another's rows.
+ */
+nf_status nf_norm_plan_init(const nf_norm_tensor* tensors_host, int64_t count, int32_t groups,
+                            nf_norm_plan* plan_host);
+nf_status nf_norm_table_init(const nf_norm_tensor* tensors_host, int64_t count, const nf_norm_plan* plan_host,
+                             void* table, size_t table_bytes, void* stream);
+
+/*
+ *   nf_grad_norm       norms only
+ *   nf_grad_clip       dst only, by norms that the caller has (of all ranks
+ *                      of a sharded model, say)
+ *   nf_grad_norm_clip  both
+ * norms: `groups` FP32 device values.  The workspace (plan.workspace_bytes,
+ * 256-byte aligned) holds nothing from call to call; the table is only read.
+ * The table must be of this plan (not checked on the device).
+ * NF_ERR_INVALID_ARG: max_norm or eps negative or not finite, a plan whose
+ * tensors have no dst where one is written.  groups = 0 launches nothing.
+ */
+nf_status nf_grad_norm(const void* table, const nf_norm_plan* plan_host, float* norms, void* ws, size_t ws_bytes,
+                       void* stream);
+nf_status nf_grad_clip(const void* table, const nf_norm_plan* plan_host, const float* norms, float max_norm, float eps,
+                       void* stream);
+nf_status nf_grad_norm_clip(const void* table, const nf_norm_plan* plan_host, float max_norm, float eps, float* norms,
+                            void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Profiling hook (no paper counterpart).  When set on the calling thread,
  * nf_route_bucket and nf_route_buckets record these hipEvent_t handles (each
  * passed as void*) on their stream: before pass 1, after pass 1, after the

@@ -42,7 +42,8 @@ EXPORTS = ["nf_abi_version", "nf_last_error", "nf_mask_from_segments", "nf_works
            "nf_slice_scales", "nf_compact_signcount_reduce",
            "nf_embedding_lookup", "nf_embedding_workspace_bytes", "nf_embedding_grad",
            "nf_orthogonal_workspace_bytes", "nf_orthogonal_path", "nf_orthogonalize", "nf_orthogonal_update",
-           "nf_expert_product", "nf_expert_grad_workspace_bytes", "nf_expert_grad"]
+           "nf_expert_product", "nf_expert_grad_workspace_bytes", "nf_expert_grad",
+           "nf_norm_plan_init", "nf_norm_table_init", "nf_grad_norm", "nf_grad_clip", "nf_grad_norm_clip"]
 NF_TYPE_F32, NF_TYPE_BF16, NF_TYPE_F16 = 0, 1, 2
 NF_PRODUCTS_SINGLE, NF_PRODUCTS_SPLIT = 0, 1
 NF_ORTHOGONAL_MAX_STEPS = 12
@@ -107,6 +108,17 @@ class nf_orthogonal_path_info(ctypes.Structure):
 class nf_matrix_step(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("momentum", ctypes.c_float), ("weight_decay", ctypes.c_float),
                 ("scale", ctypes.c_float), ("nesterov", ctypes.c_int32)]
+
+
+class nf_norm_tensor(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("src_ld", ctypes.c_int64), ("dst_ld", ctypes.c_int64), ("src_type", ctypes.c_int32),
+                ("dst_type", ctypes.c_int32), ("group", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class nf_norm_plan(ctypes.Structure):
+    _fields_ = [("pieces", ctypes.c_int64), ("blocks", ctypes.c_int64), ("groups", ctypes.c_int32),
+                ("writes", ctypes.c_int32), ("table_bytes", ctypes.c_size_t), ("workspace_bytes", ctypes.c_size_t)]
 
 
 STATS_DTYPE = np.dtype([("nonfinite", "<u8"), ("sum_abs_elig", "<f8"), ("sum_sq", "<f8")])
@@ -202,6 +214,11 @@ def load(path=None):
         "nf_expert_grad_workspace_bytes": (_SZ, [_I32, _I64, _I32, _I64, _I64]),
         "nf_expert_grad": (ctypes.c_int, [_P, _I64, _I64, _P, _I64, _I64, _I32, _P, _I32, _I64, _I32, _I64, _I32, _I64,
                                           _I64, _I32, _P, _I64, _I64, _P, _SZ, _P]),
+        "nf_norm_plan_init": (ctypes.c_int, [_P, _I64, _I32, _P]),
+        "nf_norm_table_init": (ctypes.c_int, [_P, _I64, _P, _P, _SZ, _P]),
+        "nf_grad_norm": (ctypes.c_int, [_P, _P, _P, _P, _SZ, _P]),
+        "nf_grad_clip": (ctypes.c_int, [_P, _P, _P, ctypes.c_float, ctypes.c_float, _P]),
+        "nf_grad_norm_clip": (ctypes.c_int, [_P, _P, ctypes.c_float, ctypes.c_float, _P, _P, _SZ, _P]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -841,6 +858,110 @@ def nf_expert_grad(dy, x, offsets, grads, offset, ws, accumulate=False, matrix_s
     _check(load().nf_expert_grad(dp, dld, dst, xp, xld, xst, _type(dy, "dy"), op, obytes, ost, W, T, E, n, k,
                                  1 if accumulate else 0, g + 4 * offset, each, stride,
                                  _dev_ptr(ws, torch.uint8, "ws"), ws.numel(), _stream(stream)))
+
+
+# ------------------------------------------------------------------ norms
+
+NORM_MAX_PARTS = 1 << 16  # of a tensor whose dimensions do not lie in rows
+
+
+def _parts(src, dst, name):
+    """(rows, cols, src_ld, dst_ld, [(element offsets in src and dst)]) of a
+    pair of one shape: rows of adjacent elements, in as many parts as the other
+    dimensions make."""
+    pairs = [(n, a, b) for n, a, b in zip(src.shape, src.stride(), (dst if dst is not None else src).stride()) if n > 1]
+    if any(a == 0 or b == 0 for _, a, b in pairs):
+        raise ValueError(f"{name}: an expanded tensor")
+    dims = []  # outermost first, neighbours that lie in one run joined
+    for n, a, b in sorted(pairs, key=lambda d: -d[1]):
+        if dims and dims[-1][1] == n * a and dims[-1][2] == n * b:
+            n, a, b = n * dims.pop()[0], a, b
+        dims.append((n, a, b))
+    cols = dims.pop()[0] if dims and dims[-1][1:] == (1, 1) else 1
+    rows, src_ld, dst_ld = dims.pop() if dims else (1, cols, cols)
+    at = [(0, 0)]
+    for n, a, b in dims:
+        if n * len(at) > NORM_MAX_PARTS:
+            raise ValueError(f"{name}: more than {NORM_MAX_PARTS} parts of rows")
+        at = [(x + i * a, y + i * b) for x, y in at for i in range(n)]
+    return rows, cols, src_ld, dst_ld, at
+
+
+class NormPlan:
+    """The tensors of nf_grad_norm and nf_grad_clip and their device table, for
+    as long as they stay where they are; keeps them alive.  Made by
+    norm_plan."""
+
+    def __init__(self, tensors, groups, keep, stream):
+        self.keep = keep
+        self.plan = nf_norm_plan()
+        entries = (nf_norm_tensor * max(1, len(tensors)))(*tensors)
+        _check(load().nf_norm_plan_init(entries, len(tensors), groups, ctypes.byref(self.plan)))
+        self.table = empty_workspace(self.plan.table_bytes)
+        self.device = self.table.device
+        _check(load().nf_norm_table_init(entries, len(tensors), ctypes.byref(self.plan), self.table.data_ptr(),
+                                         self.table.numel(), _stream(stream)))
+
+
+def norm_plan(src, dst=None, groups=None, n_groups=None, stream=None):
+    """A plan for the tensors of src, each of a group (0 if groups is None).
+    dst: where the scaled ones go, tensors of the same shapes (src itself for in
+    place), or None for norms only.  n_groups: how many groups there are, if
+    not those that occur.  Tensors may be of any type and strides that do not
+    overlap.  Synchronises the stream: made once, not in the step loop."""
+    src = list(src)
+    dst = list(dst) if dst is not None else [None] * len(src)
+    groups = [0] * len(src) if groups is None else [int(g) for g in groups]
+    if len(dst) != len(src) or len(groups) != len(src):
+        raise ValueError(f"{len(src)} tensors, {len(dst)} places and {len(groups)} groups")
+    if n_groups is None:
+        n_groups = max(groups, default=0) + 1
+    _here(*src, *dst)
+    tensors = []
+    for i, (s, d, g) in enumerate(zip(src, dst, groups)):
+        name = f"tensor {i}"
+        if d is not None and d.shape != s.shape:
+            raise ValueError(f"{name}: of shape {tuple(s.shape)}, its place {tuple(d.shape)}")
+        sp, dp = _dev_ptr(s, None, name), _dev_ptr(d, None, name)
+        st, dt = _type(s, name), _type(d, name) if d is not None else 0
+        if s.numel() == 0:
+            continue
+        rows, cols, sld, dld, at = _parts(s, d, name)
+        for a, b in at:
+            tensors.append(nf_norm_tensor(sp + a * s.element_size(), None if d is None else dp + b * d.element_size(),
+                                          rows, cols, sld, dld, st, dt, g, 0))
+    return NormPlan(tensors, n_groups, (src, dst), stream)
+
+
+def nf_grad_norm_workspace_bytes(plan):
+    return plan.plan.workspace_bytes
+
+
+def _norms(plan, norms):
+    if norms.numel() != plan.plan.groups or not norms.is_contiguous():
+        raise ValueError(f"norms must be {plan.plan.groups} contiguous values, got {tuple(norms.shape)}")
+    return _dev_ptr(norms, torch.float32, "norms")
+
+
+def nf_grad_norm(plan, norms, ws, stream=None):
+    """norms[g] = the 2-norm of all of group g's tensors (float32)."""
+    _here(plan.table, norms, ws)
+    _check(load().nf_grad_norm(plan.table.data_ptr(), ctypes.byref(plan.plan), _norms(plan, norms),
+                               _dev_ptr(ws, torch.uint8, "ws"), ws.numel(), _stream(stream)))
+
+
+def nf_grad_clip(plan, norms, max_norm, eps=1e-6, stream=None):
+    """dst = min(1, max_norm / (norms[g] + eps)) src for every tensor."""
+    _here(plan.table, norms)
+    _check(load().nf_grad_clip(plan.table.data_ptr(), ctypes.byref(plan.plan), _norms(plan, norms), max_norm, eps,
+                               _stream(stream)))
+
+
+def nf_grad_norm_clip(plan, max_norm, norms, ws, eps=1e-6, stream=None):
+    """nf_grad_norm and nf_grad_clip by its norms."""
+    _here(plan.table, norms, ws)
+    _check(load().nf_grad_norm_clip(plan.table.data_ptr(), ctypes.byref(plan.plan), max_norm, eps, _norms(plan, norms),
+                                    _dev_ptr(ws, torch.uint8, "ws"), ws.numel(), _stream(stream)))
 
 
 # ------------------------------------------------------- result decoding
