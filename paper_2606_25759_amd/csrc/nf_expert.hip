@@ -40,6 +40,9 @@ enum { FORWARD, BACKWARD, GRAD };
 
 constexpr int kStageBytes = 128;  // of a row in LDS: 64 elements of 16 bits, 32 of FP32
 constexpr int kMaxExperts = 4096;
+#ifndef NARROW_ROWS
+#define NARROW_ROWS 48
+#endif
 
 struct ExpertArgs {
   const void *p, *q;
@@ -126,6 +129,7 @@ __device__ __forceinline__ bool find(const ExpertArgs& a, int64_t worker, int bl
     return true;
   }
   int mine = 0;
+  first = rows = 0;
   for (int j = 0; j < each; ++j)
     if (lane * each + j < a.E) mine += units_of<MODE>(a, worker, lane * each + j, &first, &rows);
   const int upto = scan(mine, lane);
@@ -138,10 +142,16 @@ __device__ __forceinline__ bool find(const ExpertArgs& a, int64_t worker, int bl
   const int u = block / per;
   const int at = __builtin_ctzll(__ballot(upto > u));
   int base = __builtin_amdgcn_readlane(upto - mine, at), e = at * each, n = 0;
-  for (;; ++e) {
-    n = units_of<MODE>(a, worker, e, &first, &rows);
-    if (u < base + n || e + 1 >= a.E) break;
-    base += n;
+  if (each == 1) {
+    n = __builtin_amdgcn_readlane(mine, at);
+    first = __builtin_amdgcn_readlane((int)first, at);
+    rows = __builtin_amdgcn_readlane((int)rows, at);
+  } else {
+    for (;; ++e) {
+      n = units_of<MODE>(a, worker, e, &first, &rows);
+      if (u < base + n || e + 1 >= a.E) break;
+      base += n;
+    }
   }
   g->e = __builtin_amdgcn_readfirstlane(e);
   g->units = __builtin_amdgcn_readfirstlane(n);
@@ -234,27 +244,6 @@ struct Tile {
   }
 };
 
-// Element c .. of a row of n at p, at any alignment; zeros past its end.
-template <typename T>
-__device__ __forceinline__ uint4v load_piece(const char* row, int64_t c, int64_t n) {
-  constexpr int N = kPiece<T>;
-  uint4v v = {};
-  if (c + N <= n) {
-    v = __builtin_bit_cast(uint4v, *(const Near<T, N>*)(row + c * (int64_t)sizeof(T)));
-  } else if (c < n && n >= N) {  // the row's last whole piece, moved down
-    typedef unsigned __int128 wide;
-    wide x = __builtin_bit_cast(wide, *(const Near<T, N>*)(row + (n - N) * (int64_t)sizeof(T)));
-    v = __builtin_bit_cast(uint4v, x >> ((int)(c + N - n) * 8 * (int)sizeof(T)));
-  } else {
-    Near<T, N> x = {};
-#pragma unroll
-    for (int e = 0; e < N; ++e)
-      if (c + e < n) x.v[e] = ((const T*)row)[c + e];
-    v = __builtin_bit_cast(uint4v, x);
-  }
-  return v;
-}
-
 __device__ __forceinline__ uint64_t uniform(uint64_t x) {
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
   return (uint64_t)hi << 32 | lo;
@@ -263,7 +252,9 @@ __device__ __forceinline__ uint64_t uniform(uint64_t x) {
 // One operand's way from memory to LDS.
 //
 // DIRECT: straight into LDS, for addresses and lengths in whole pieces.  What is past an end has an offset out of the
-// buffer's range, for which the card writes zeros.  Else by registers, a stage ahead.
+// buffer's range, for which the card writes zeros.  Else by registers, a stage ahead: pieces at any element's address,
+// and of one that its row ends in the last whole piece before that end, moved down when it goes to LDS (loads that wait
+// for nothing in between: 37 us of back_odd's 37 were spent in waits for one load after the other).
 constexpr uint32_t kNowhere = 0x80000000u;
 
 // 16 bytes a lane from base + off to LDS, lane after lane from `lds` on; zeros for off = kNowhere.  Written out
@@ -287,12 +278,15 @@ struct Operand {
   int64_t row_bytes;
   int32_t left;     // r from there on
   int32_t extent;   // of the tile's own index
+  int32_t length;   // of a row in memory
+  int32_t held_end; // what `left` or `extent` was when `held` was asked for
   uint32_t off[DIRECT ? kLoads : 1];
   uint4v held[DIRECT ? 1 : kLoads];
   int lane, wave;
 
-  __device__ __forceinline__ void begin(const char* base, int64_t ld, int32_t extent_, int32_t r, int wave_,
-                                        int lane_) {
+  __device__ __forceinline__ void begin(const char* base, int64_t ld, int32_t extent_, int32_t r, int32_t length_,
+                                        int wave_, int lane_) {
+    length = length_;
     at = (const char*)uniform((uint64_t)(uintptr_t)base);
     row_bytes = ld * (int64_t)sizeof(T);
     step = TURNED ? row_bytes * kStageLen<T> : (int64_t)kStageBytes;
@@ -324,10 +318,24 @@ struct Operand {
     if constexpr (DIRECT) {
       load_to_lds(at, lds + (i * NW + wave) * 1024, off[i]);
     } else {
-      const int row = Lay::load_row(i, wave, lane), c = Lay::load_piece(row, lane) * kPiece<T>;
+      constexpr int N = kPiece<T>;
+      const int row = Lay::load_row(i, wave, lane), c = Lay::load_piece(row, lane) * N;
+      const int end = TURNED ? extent : left;
+      const char* from = at + row * row_bytes;
       uint4v v = {};
-      if (TURNED ? row < left : row < extent) v = load_piece<T>(at + row * row_bytes, c, TURNED ? extent : left);
+      if ((TURNED ? row < left : row < extent) && c < end) {
+        if (length >= N) {
+          v = __builtin_bit_cast(uint4v, *(const Near<T, N>*)(from + min(c, end - N) * (int)sizeof(T)));
+        } else {
+          Near<T, N> x = {};
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            if (c + e < end) x.v[e] = ((const T*)from)[c + e];
+          v = __builtin_bit_cast(uint4v, x);
+        }
+      }
       held[i] = v;
+      held_end = end;
     }
   }
   __device__ __forceinline__ void on() {
@@ -346,7 +354,16 @@ struct Operand {
     typedef __attribute__((address_space(3))) uint4v* ptr;
     if constexpr (!DIRECT) {
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) *(ptr)(uintptr_t)(lds + (i * NW + wave) * 1024 + lane * 16) = held[i];
+      for (int i = 0; i < kLoads; ++i) {
+        constexpr int N = kPiece<T>;
+        const int c = Lay::load_piece(Lay::load_row(i, wave, lane), lane) * N;
+        uint4v v = held[i];
+        if (c + N > held_end && c < held_end && length >= N) {
+          typedef unsigned __int128 wide;
+          v = __builtin_bit_cast(uint4v, __builtin_bit_cast(wide, v) >> ((c + N - held_end) * 8 * (int)sizeof(T)));
+        }
+        *(ptr)(uintptr_t)(lds + (i * NW + wave) * 1024 + lane * 16) = v;
+      }
     }
   }
 };
@@ -431,7 +448,7 @@ __device__ __forceinline__ void store_all(const ExpertArgs& a, T* out, int64_t P
 
 // One BP x BQ tile, WP x WQ of it per wavefront; NS stages in LDS.
 template <typename T, int MODE, int BP, int BQ, int WP, int WQ, int NS, bool DIRECT>
-__global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, BP / WP * (BQ / WQ) == 8 ? 1 : 2) void k_expert(ExpertArgs a) {
+__global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, DIRECT && BP / WP * (BQ / WQ) == 8 ? 1 : 2) void k_expert(ExpertArgs a) {
   constexpr int NW = BP / WP * (BQ / WQ);
   constexpr int MI = WP / 16, NJ = WQ / 16;
   typedef Operand<T, BP, NW, MODE != FORWARD, true, DIRECT> OpP;
@@ -466,17 +483,18 @@ __global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, BP / WP * (BQ / WQ) == 8 
     q0 = (int64_t)tq * BQ;
     extent_q = a.Q - q0;
     p.begin((const char*)a.p + (worker * a.p_worker + token * a.p_ld + (int64_t)tp * BP) * (int64_t)sizeof(T), a.p_ld,
-            a.P - tp * BP, r, wave, lane);
+            a.P - tp * BP, r, a.P, wave, lane);
     q.begin((const char*)a.q + (worker * a.q_worker + token * a.q_ld + q0) * (int64_t)sizeof(T), a.q_ld,
-            (int32_t)extent_q, r, wave, lane);
+            (int32_t)extent_q, r, a.Q, wave, lane);
   } else {
     r = a.R;
     q0 = g.first + (int64_t)tq * BQ;
     extent_q = g.rows - (int64_t)tq * BQ;
     const int64_t at = g.e * a.p_expert + (int64_t)tp * BP * (MODE == FORWARD ? a.p_ld : 1);
-    p.begin((const char*)a.p + at * (int64_t)sizeof(T), a.p_ld, a.P - tp * BP, r, wave, lane);
+    p.begin((const char*)a.p + at * (int64_t)sizeof(T), a.p_ld, a.P - tp * BP, r,
+            MODE == FORWARD ? r : a.P, wave, lane);
     q.begin((const char*)a.q + (worker * a.q_worker + q0 * a.q_ld) * (int64_t)sizeof(T), a.q_ld,
-            (int32_t)(extent_q < BQ ? extent_q : BQ), r, wave, lane);
+            (int32_t)(extent_q < BQ ? extent_q : BQ), r, r, wave, lane);
   }
   const int wp = wave % (BP / WP) * WP, wq = wave / (BP / WP) * WQ;
   constexpr int kStage = LP::kBytes + LQ::kBytes;
@@ -573,11 +591,12 @@ __global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, BP / WP * (BQ / WQ) == 8 
 
   if constexpr (MODE == GRAD) {
     if (g.units > 1) {
-      float* to = a.part + (((int64_t)worker * a.units + g.base + g.unit) * per + id) * (BP * BQ) + threadIdx.x * 4;
+      float* to = a.part + (((int64_t)worker * a.units + g.base + g.unit) * per + id) * (BP * BQ);
 #pragma unroll
-      for (int i = 0; i < MI; ++i)
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) *(float4v*)(to + (i * NJ + j) * NW * 256) = acc[i][j];
+        for (int i = 0; i < MI; ++i)
+          *(float4v*)(to + (wq + LQ::column_of(j, lane)) * BP + wp + 16 * i + lane / 16 * 4) = acc[i][j];
       return;
     }
     float* out = (float*)a.out + worker * a.out_worker + g.e * a.out_expert + q0 * a.out_ld + (int64_t)tp * BP;
@@ -591,16 +610,16 @@ __global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, BP / WP * (BQ / WQ) == 8 
   }
 }
 
-// A tile of an expert whose tokens were shared: the shares' sums in order.  Block z of y of x: worker, expert, tile.
-template <typename T, int BP, int BQ, int WP, int WQ>
-__global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64) void k_join(ExpertArgs a) {
-  constexpr int NW = BP / WP * (BQ / WQ);
-  constexpr int MI = WP / 16, NJ = WQ / 16;
-  typedef Tile<T, BP, NW, true> LP;
-  typedef Tile<T, BQ, NW, true> LQ;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+// Elements of an expert's matrix whose tokens were shared: the shares' sums in order.  Block z of y of x: worker,
+// expert, 1024 elements of a tile (a tile a block took 71 us for grad_long's 60 shares, where this takes TIME).
+constexpr int kJoinThreads = 256;
+constexpr int kJoinBlocks = 128 * 128 / 4 / kJoinThreads;  // of a tile
+
+__global__ __launch_bounds__(kJoinThreads) void k_join(ExpertArgs a) {
+  constexpr int B = 128, U = 8;
+  const int lane = threadIdx.x % 64;
   const int64_t worker = blockIdx.z;
-  const int e = blockIdx.y, per = a.tp * a.tq, tile = blockIdx.x;
+  const int e = blockIdx.y, per = a.tp * a.tq, tile = blockIdx.x / kJoinBlocks;
   int64_t first, rows;
   const int n = units_of<GRAD>(a, worker, e, &first, &rows);
   if (n == 1) return;
@@ -608,19 +627,24 @@ __global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64) void k_join(ExpertArgs a)
   for (int i = lane; i < e; i += 64) base += units_of<GRAD>(a, worker, i, &first, &rows);
   base = __builtin_amdgcn_readlane(scan(base, lane), 63);
   if (base + n > a.units) return;  // offsets that do not ascend
-  float4v acc[MI][NJ] = {};
-  const int64_t each = (int64_t)per * BP * BQ;
-  const float* from = a.part + ((int64_t)worker * a.units + base) * each + (int64_t)tile * BP * BQ + threadIdx.x * 4;
-  for (int u = 0; u < n; ++u, from += each)
+  const int at = (blockIdx.x % kJoinBlocks * kJoinThreads + threadIdx.x) * 4;
+  const int64_t each = (int64_t)per * B * B;
+  const float* from = a.part + ((int64_t)worker * a.units + base) * each + (int64_t)tile * B * B + at;
+  float4v sum = {};
+  for (int u = 0; u < n; u += U) {
+    float4v v[U];
 #pragma unroll
-    for (int i = 0; i < MI; ++i)
+    for (int i = 0; i < U; ++i) v[i] = *(const float4v*)(from + min(u + i, n - 1) * each);
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) acc[i][j] += *(const float4v*)(from + (i * NJ + j) * NW * 256);
+    for (int i = 0; i < U; ++i)
+      if (u + i < n) sum += v[i];
+  }
   const int four = tile / (4 * a.tp), trows = min(4, a.tq - 4 * four), in = tile - four * 4 * a.tp;
-  const int tq = 4 * four + in % trows, tp = in / trows;
-  const int wp = wave % (BP / WP) * WP, wq = wave / (BP / WP) * WQ;
-  float* out = (float*)a.out + worker * a.out_worker + e * a.out_expert + (int64_t)tq * BQ * a.out_ld + (int64_t)tp * BP;
-  store_all<GRAD, LP, LQ>(a, out, a.P - tp * BP, a.Q - tq * BQ, wp, wq, lane, acc);
+  const int64_t q = (int64_t)(4 * four + in % trows) * B + at / B, p = (int64_t)(in / trows) * B + at % B;
+  if (q >= a.Q || p >= a.P) return;
+  float* out = (float*)a.out + worker * a.out_worker + e * a.out_expert + q * a.out_ld + p;
+  const float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+  store<float, 4>(out, 0, a.P - p, a.accumulate, v);
 }
 
 // --------------------------------------------------------------------- host
@@ -694,7 +718,7 @@ Plan plan_of(const Shape& s, int mode, int32_t type, bool direct) {
     p.rows = (int32_t)(s.T > 0 ? s.T : 1);
   } else {
     wide = wide && ceil_div(s.T, 256) * s.W * ceil_div(len, 256) >= kCUs;
-    p.tile = wide ? WIDE : rows <= 48 ? NARROW : MIDDLE;
+    p.tile = wide ? WIDE : rows <= NARROW_ROWS ? NARROW : MIDDLE;
   }
   finish_plan(&p, s, mode);
   return p;
@@ -715,7 +739,10 @@ void launch(const Plan& p, const Shape& s, const ExpertArgs& a, hipStream_t stre
       return;
     }
   }
-  k_expert<T, MODE, 128, 128, 64, 64, 2, DIRECT><<<grid, 256, 0, stream>>>(a);
+  if constexpr (DIRECT)
+    k_expert<T, MODE, 128, 128, 64, 64, 2, true><<<grid, 256, 0, stream>>>(a);
+  else
+    k_expert<T, MODE, 128, 128, 64, 32, 2, false><<<grid, 512, 0, stream>>>(a);
 }
 
 template <int MODE>
@@ -733,8 +760,7 @@ hipError_t run(const Plan& p, const Shape& s, ExpertArgs a, int32_t type, bool d
       launch<T, MODE, false>(p, s, a, stream);
     if constexpr (MODE == GRAD) {
       if (p.part_bytes && hipPeekAtLastError() == hipSuccess)
-        k_join<T, 128, 128, 64, 64>
-            <<<dim3((unsigned)(p.tp * p.tq), (unsigned)s.E, (unsigned)s.W), 256, 0, stream>>>(a);
+        k_join<<<dim3((unsigned)(p.tp * p.tq * kJoinBlocks), (unsigned)s.E, (unsigned)s.W), kJoinThreads, 0, stream>>>(a);
     }
   });
   return hipGetLastError();
