@@ -793,22 +793,38 @@ def nf_orthogonal_update(grad, momentum, weight, step, params, ws, stream=None):
 
 def _here(*tensors):
     """Refuses tensors of another device than the current one, whose stream the call would run on."""
+    here = torch.cuda.current_device() if torch.cuda.is_initialized() else -1
     for t in tensors:
-        if t is not None and t.is_cuda and t.device.index != torch.cuda.current_device():
-            raise ValueError(f"a tensor on {t.device} while the current device is cuda:{torch.cuda.current_device()}")
+        if t is not None and t.is_cuda and t.get_device() != here:
+            raise ValueError(f"a tensor on {t.device} while the current device is cuda:{here}")
 
 
 def _worker_rows(t, name):
     """(pointer, row stride, worker stride, W, T, columns) of a [T, columns] or [W, T, columns] tensor."""
-    p, ld, stride = _matrices(t, None, name)
-    return p, ld, stride, t.shape[0] if t.dim() == 3 else 1, t.shape[-2], t.shape[-1]
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 3:
+        W, T, cols = shape
+        far, ld, one = stride
+    elif len(shape) == 2:
+        (T, cols), (ld, one), W, far = shape, stride, 1, 0
+    else:
+        raise ValueError(f"{name} must be [T, columns] or [W, T, columns], got {tuple(shape)}")
+    if one != 1 and cols > 1:
+        raise ValueError(f"{name} must have unit stride in the last dimension")
+    ld = ld if T > 1 else max(cols, 1)
+    return _dev_ptr(t, None, name), ld, far if W > 1 else T * ld, W, T, cols
 
 
 def _offsets_of(offsets, W, E):
-    p, size = _ids(offsets, "offsets")
-    if tuple(offsets.shape) not in ((W, E + 1),) + (((E + 1,),) if W == 1 else ()):
-        raise ValueError(f"offsets must be [{W}, {E + 1}], got {tuple(offsets.shape)}")
-    return p, size, offsets.stride(0) if offsets.dim() == 2 and W > 1 else E + 1
+    shape, size = offsets.shape, _ID_BYTES.get(offsets.dtype)
+    if size is None:
+        raise ValueError(f"offsets must be int32 or int64, got {offsets.dtype}")
+    if not (shape == (W, E + 1) or (W == 1 and shape == (E + 1,))):
+        raise ValueError(f"offsets must be [{W}, {E + 1}], got {tuple(shape)}")
+    stride = offsets.stride()
+    if stride[-1] != 1 and E > 0:
+        raise ValueError("offsets must have unit stride in the last dimension")
+    return _dev_ptr(offsets, None, "offsets"), size, stride[0] if W > 1 else E + 1
 
 
 def nf_expert_product(x, w, offsets, y, transposed=False, stream=None):
@@ -819,8 +835,7 @@ def nf_expert_product(x, w, offsets, y, transposed=False, stream=None):
     _here(x, w, offsets, y)
     if w.dim() != 3:
         raise ValueError("w must be [E, n, k]")
-    E, n, k = w.shape
-    wp, wld, wst = _matrices(w, None, "w")
+    wp, wld, wst, E, n, k = _worker_rows(w, "w")
     xp, xld, xst, W, T, cols = _worker_rows(x, "x")
     yp, yld, yst, yW, yT, ycols = _worker_rows(y, "y")
     if w.dtype != x.dtype:
