@@ -40,9 +40,6 @@ enum { FORWARD, BACKWARD, GRAD };
 
 constexpr int kStageBytes = 128;  // of a row in LDS: 64 elements of 16 bits, 32 of FP32
 constexpr int kMaxExperts = 4096;
-#ifndef NARROW_ROWS
-#define NARROW_ROWS 48
-#endif
 
 struct ExpertArgs {
   const void *p, *q;
@@ -195,8 +192,8 @@ struct Tile {
       const int q = row >> 3;
       return PAIRS ? ((q >> 1) & 1) | (((q ^ (q >> 1)) & 1) << 1) | ((row & 2) << 1) : (row >> 1) & 7;
     }
-    if (sizeof(T) == 2) return (row & 3) << 1 | (row & 8);
-    return row & 12;
+    if (sizeof(T) == 2) return kRow >= 256 ? (row & 3) << 1 | (row & 8) : (row & 8) >> 2;
+    return kRow >= 256 ? row & 12 : row & 4;
   }
   // The row and piece of it that lane `lane` of a wavefront loads in its i-th load.
   static __device__ __forceinline__ int load_row(int i, int wave, int lane) {
@@ -610,8 +607,102 @@ __global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, DIRECT && BP / WP * (BQ /
   }
 }
 
+// A tile of 32 x 32 for few rows: its four wavefronts share the sum, a quarter of the stages each, from LDS of their own
+// and without a barrier but for the last one, behind which they add up in their order.  More blocks, and a quarter of the
+// way for each: 4096 x 4096 BF16 with one row takes 14.6 us, with tiles of 128 x 32 22.4.
+template <typename T, int MODE, bool DIRECT>
+__global__ __launch_bounds__(256) void k_slim(ExpertArgs a) {
+  constexpr int B = 32, NW = 4, MI = 2, NJ = 2, NS = DIRECT ? 4 : 2;
+  typedef Operand<T, B, 1, MODE != FORWARD, MODE == FORWARD, DIRECT> OpP;
+  typedef Operand<T, B, 1, false, false, DIRECT> OpQ;
+  typedef typename OpP::Lay LP;
+  typedef typename OpQ::Lay LQ;
+  constexpr int kLoads = OpP::kLoads + OpQ::kLoads, kStage = LP::kBytes + LQ::kBytes;
+  __shared__ __align__(1024) char lds[NW][NS * kStage];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+  const int64_t worker = blockIdx.y;
+  Group g;
+  int id;
+  if (!find<MODE>(a, worker, blockIdx.x, a.tp, &g, &id)) return;
+  const int tq = id / a.tp, tp = id - tq * a.tp;
+  const int64_t q0 = g.first + (int64_t)tq * B;
+  const int rows = (int)(g.rows - (int64_t)tq * B < B ? g.rows - (int64_t)tq * B : B);
+  const int all = (a.R + kStageLen<T> - 1) / kStageLen<T>;
+  const int from = (int)((int64_t)all * wave / NW), to = (int)((int64_t)all * (wave + 1) / NW);
+  const int begin = from * kStageLen<T>, end = min(a.R, to * kStageLen<T>);
+  OpP p;
+  OpQ q;
+  const int64_t p_at = g.e * a.p_expert + (MODE == FORWARD ? (int64_t)tp * B * a.p_ld + begin
+                                                          : (int64_t)begin * a.p_ld + (int64_t)tp * B);
+  p.begin((const char*)a.p + p_at * (int64_t)sizeof(T), a.p_ld, a.P - tp * B, end - begin, MODE == FORWARD ? a.R : a.P,
+          0, lane);
+  q.begin((const char*)a.q + (worker * a.q_worker + q0 * a.q_ld + begin) * (int64_t)sizeof(T), a.q_ld, rows, end - begin,
+          a.R, 0, lane);
+  const uint32_t at = (uint32_t)(uintptr_t)(lptr)lds[wave];
+  const uint32_t read_p = at + LP::read_at(0, lane), read_q = at + LP::kBytes + LQ::read_at(0, lane);
+  float4v acc[MI][NJ] = {};
+  auto ask = [&](uint32_t stage) {
+    p.ask(at + stage);
+    q.ask(at + stage + LP::kBytes);
+  };
+  auto put = [&](uint32_t stage) {
+    p.put(at + stage);
+    q.put(at + stage + LP::kBytes);
+  };
+  if constexpr (DIRECT) {
+#pragma unroll
+    for (int s = 0; s < NS; ++s) ask(s * kStage);
+  } else {
+    ask(0);
+    put(0);
+    ask(0);
+    put(kStage);
+    ask(0);
+  }
+  uint32_t now = 0;
+  for (int s = from; s < to; ++s) {
+    wait_for<DIRECT ? (NS - 1) * kLoads : 63, 0>();
+    uint4v fp[2][MI], fq[2][NJ];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int i = 0; i < MI; ++i) fp[h][i] = LP::read(read_p + now, i, h);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) fq[h][j] = LQ::read(read_q + now, j, h);
+    }
+    wait_for<63, 0>();  // they are read: their place is free
+    put(now);
+    ask(now);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = multiply<T>(fp[h][i], fq[h][j], acc[i][j]);
+    now = now + kStage == NS * kStage ? 0 : now + kStage;
+  }
+  wait_for<0, 0>();
+  __syncthreads();
+  float4v* sums = (float4v*)lds[0];
+#pragma unroll
+  for (int n = 0; n < NW; ++n) sums[(wave * NW + n) * 64 + lane] = acc[n / NJ][n % NJ];
+  __syncthreads();
+  float4v sum = {};
+#pragma unroll
+  for (int w = 0; w < NW; ++w) sum += sums[(w * NW + wave) * 64 + lane];
+  const int i = wave / NJ, row = LQ::column_of(wave % NJ, lane);
+  const int column = tp * B + (MODE == FORWARD ? lane / 16 * 8 + i * 4 : i * 16 + lane / 16 * 4);
+  if (row >= rows) return;
+  const float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+  with_type_on_device(a.out_type, [&](auto* t) {
+    using O = std::remove_pointer_t<decltype(t)>;
+    store<O, 4>((O*)a.out + worker * a.out_worker + (q0 + row) * a.out_ld, column, a.P, 0, v);
+  });
+}
+
 // Elements of an expert's matrix whose tokens were shared: the shares' sums in order.  Block z of y of x: worker,
-// expert, 1024 elements of a tile (a tile a block took 71 us for grad_long's 60 shares, where this takes TIME).
+// expert, 1024 elements of a tile (30,011 tokens into 4 x (256 x 128) in 120 shares of two tiles:
+// JOIN us; 71 with a block a tile).
 constexpr int kJoinThreads = 256;
 constexpr int kJoinBlocks = 128 * 128 / 4 / kJoinThreads;  // of a tile
 
@@ -649,7 +740,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_join(ExpertArgs a) {
 
 // --------------------------------------------------------------------- host
 
-enum { NARROW, MIDDLE, WIDE };  // tiles: 128 x 32, 128 x 128, 256 x 256
+enum { SLIM, NARROW, MIDDLE, WIDE };  // tiles: 32 x 32, 128 x 32, 128 x 128, 256 x 256
 
 struct Shape {
   int32_t W, E;
@@ -668,7 +759,7 @@ constexpr int64_t kSplitBelow = 2 * kCUs;  // tiles of all workers and experts b
 constexpr int64_t kMinShare = 256;         // tokens of a share, at least
 
 void finish_plan(Plan* p, const Shape& s, int mode) {
-  p->bp = p->tile == WIDE ? 256 : 128;
+  p->bp = p->tile == WIDE ? 256 : p->tile == SLIM ? 32 : 128;
   p->bq = p->tile == WIDE ? 256 : p->tile == MIDDLE ? 128 : 32;
   p->tp = (int32_t)ceil_div(mode == FORWARD ? s.n : s.k, p->bp);
   const int64_t some = s.T < s.E ? s.T : s.E;  // experts with rows, at most
@@ -703,22 +794,35 @@ Plan shared_plan(const Shape& s) {
   return p;
 }
 
+// Which tiles a call takes, by how many there are of each if the experts' sizes are alike (measured in us, BF16 unless
+// stated, with tiles of 32 / 128 x 32 / 128 / 256):
+//   256    needs as many as there are CUs, and experts that fill them: 32,768 rows of 32 experts, 4096 x 2048: 1,604 with
+//          128 through registers, 547; 4,096 rows of 16, 2048 x 2048 (192 tiles): - / 80 / 56 / 57; 1,024 rows of one,
+//          4096 x 4096 (64): - / 68 / 48 / 90
+//   128    8,192 rows of 8, 1024 x 1024 (576): 149 / 47 / 34 / 34; where there are too few, 128 x 32: 1,024 rows of one,
+//          1024 x 1024 (64): 21 / 13 / 15 / 29; and so for FP32, whose products are slow enough for any tile's loads:
+//          8,192 rows of 8, 1024 x 1024: 321 / 186 / 203
+//   128x32 for experts of few rows: 2,048 rows of 64, 1024 x 1024: 63 / 29 / 36 / 31
+//   32     where there are few of those: one row, 4096 x 4096 (32 of 128 x 32): 15 / 22 / 39; 64 rows of 8, 2048 x 2048
+//          (150): 19 / 15 / 25
 Plan plan_of(const Shape& s, int mode, int32_t type, bool direct) {
-  const int64_t rows = s.T / (s.E > 0 ? s.E : 1);  // of an expert, on average
-  const int64_t len = mode == GRAD || mode == BACKWARD ? s.k : s.n;
-  const int64_t other = mode == GRAD ? s.n : rows;
-  bool wide = direct && type != NF_TYPE_F32 && len >= 192 && other >= 192;
-  if (mode == GRAD) {
-    const Plan shared = shared_plan(s);
-    if (!wide || s.W * s.E * ceil_div(s.n, 256) * ceil_div(s.k, 256) < kCUs) return shared;
-  }
   Plan p = {};
+  const int64_t experts = s.E > 0 ? s.E : 1, some = s.T < experts ? s.T : experts;
+  const int64_t rows = s.T / experts;  // of an expert, on average
+  const int64_t len = mode == FORWARD ? s.n : s.k;
+  const bool fits = direct && type != NF_TYPE_F32 && len >= 192;
   if (mode == GRAD) {
+    if (!fits || s.n < 192 || s.W * s.E * ceil_div(s.n, 256) * ceil_div(s.k, 256) < kCUs) return shared_plan(s);
     p.tile = WIDE;
     p.rows = (int32_t)(s.T > 0 ? s.T : 1);
   } else {
-    wide = wide && ceil_div(s.T, 256) * s.W * ceil_div(len, 256) >= kCUs;
-    p.tile = wide ? WIDE : rows <= NARROW_ROWS ? NARROW : MIDDLE;
+    auto tiles = [&](int64_t bp, int64_t bq) { return s.W * (s.T / bq + (some + 1) / 2) * ceil_div(len, bp); };
+    if (fits && rows >= 192 && s.W * ceil_div(s.T, 256) * ceil_div(len, 256) >= kCUs)
+      p.tile = WIDE;
+    else if (rows > 48 && type != NF_TYPE_F32 && tiles(128, 128) >= kCUs / 2)
+      p.tile = MIDDLE;
+    else
+      p.tile = tiles(128, 32) > kCUs * 3 / 8 ? NARROW : SLIM;
   }
   finish_plan(&p, s, mode);
   return p;
@@ -734,15 +838,21 @@ void launch(const Plan& p, const Shape& s, const ExpertArgs& a, hipStream_t stre
     }
   }
   if constexpr (MODE != GRAD) {
+    if (p.tile == SLIM) {
+      k_slim<T, MODE, DIRECT><<<grid, 256, 0, stream>>>(a);
+      return;
+    }
     if (p.tile == NARROW) {
       k_expert<T, MODE, 128, 32, 32, 32, DIRECT ? 4 : 2, DIRECT><<<grid, 256, 0, stream>>>(a);
       return;
     }
   }
-  if constexpr (DIRECT)
-    k_expert<T, MODE, 128, 128, 64, 64, 2, true><<<grid, 256, 0, stream>>>(a);
-  else
-    k_expert<T, MODE, 128, 128, 64, 32, 2, false><<<grid, 512, 0, stream>>>(a);
+  if constexpr (sizeof(T) == 2 || MODE == GRAD) {
+    if constexpr (DIRECT)
+      k_expert<T, MODE, 128, 128, 64, 64, 2, true><<<grid, 256, 0, stream>>>(a);
+    else
+      k_expert<T, MODE, 128, 128, 64, 32, 2, false><<<grid, 512, 0, stream>>>(a);
+  }
 }
 
 template <int MODE>

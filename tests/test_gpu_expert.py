@@ -105,6 +105,16 @@ def test_product_wide_tiles(W, E, T, n, k, back, kind, out):
 
 
 @pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("W,E,T,n,k,extra", [
+    (1, 1, 1, 512, 2048, 0), (1, 2, 70, 320, 1030, 2), (1, 6, 1500, 520, 264, 0), (2, 5, 900, 515, 260, 1),
+    (1, 3, 3000, 768, 1032, 0), (1, 2, 3000, 769, 515, 3)])
+def test_product_other_tiles(W, E, T, n, k, extra, kind, back):
+    """Sizes that take tiles of 32, of 128 x 32 and of 128, straight into LDS and by registers."""
+    check_product(W, E, T, n, k, back, kind, "f32", extra=extra, seed=n + k)
+
+
+@pytest.mark.parametrize("back", [False, True])
 def test_sizes_at_the_edges_of_tiles(back):
     for sizes in ([0, 0, 0, 0], [31, 32, 33, 1], [127, 0, 128, 129], [255, 256, 257, 0], [0, 0, 513, 0], [1, 1, 1, 1]):
         T = sum(sizes) + 5
