@@ -771,8 +771,8 @@ nf_status nf_orthogonal_update(const void* grad, int32_t grad_type, int64_t grad
  * NF_ERR_INVALID_ARG: W outside [1, 255], T outside [0, 2^24], E outside
  * [0, 4096], n or k outside [0, 2^20], an ld below the columns, a stride too
  * small with W > 1 (w_stride with E > 1), y at x or w.  NF_ERR_UNSUPPORTED:
- * more than 2^22 tiles of 128 x 32 or more.  T, E or the columns of y = 0
- * launches nothing.
+ * more than 2^22 tiles (of 128 x 128 or 256 x 256, 128 x 32 for experts of
+ * few rows and FP32).  T, E or the columns of y = 0 launches nothing.
  */
 nf_status nf_expert_product(const void* x, int32_t type, int64_t x_ld, int64_t x_stride, const void* w, int64_t w_ld,
                             int64_t w_stride, int32_t transposed, const void* offsets, int32_t offsets_bytes,

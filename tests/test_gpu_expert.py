@@ -152,6 +152,33 @@ def test_infinities_and_nan_stay_in_their_rows(kind, back):
         assert torch.equal(torch.nan_to_num(y[0], nan=-5.0), torch.nan_to_num(want, nan=-5.0))
 
 
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_smallest_and_largest_elements(kind):
+    """Subnormal elements count, and sums of the largest FP16 ones do not overflow on the way."""
+    t = TYPES[kind]
+    small, large = torch.finfo(t).tiny / 4, 2.0 ** 100 if kind != "f16" else 2.0 ** 15
+    for T, n, k in ((3, 32, 64), (300, 256, 128), (70, 33, 17)):
+        x = torch.full((T, k), small, dtype=t, device=DEV)
+        w = torch.full((1, n, k), large, dtype=t, device=DEV)
+        off = torch.tensor([0, T], dtype=torch.int32, device=DEV)
+        y = torch.empty(T, n, device=DEV)
+        nf.nf_expert_product(x, w, off, y)
+        assert torch.equal(y, torch.full_like(y, k * small * large))
+        dx = torch.empty(T, k, device=DEV)
+        nf.nf_expert_product(torch.full((T, n), small, dtype=t, device=DEV), w, off, dx, transposed=True)
+        assert torch.equal(dx, torch.full_like(dx, n * small * large))
+        rows = torch.empty(1, n * k, device=DEV)
+        nf.nf_expert_grad(torch.full((T, n), large, dtype=t, device=DEV), x, off, rows, 0,
+                          nf.empty_workspace(nf.nf_expert_grad_workspace_bytes(1, T, 1, n, k)))
+        assert torch.equal(rows, torch.full_like(rows, T * small * large))
+    x = torch.full((4, 64), 60_000.0, dtype=t, device=DEV)
+    y = torch.empty(4, 32, device=DEV)
+    w = torch.full((1, 32, 64), 60_000.0, dtype=t, device=DEV)
+    nf.nf_expert_product(x, w, torch.tensor([0, 4], dtype=torch.int32, device=DEV), y)
+    want = 64 * float(x[0, 0]) * float(w[0, 0, 0])
+    assert bool(((y.double() - want).abs() <= 66 * 2.0 ** -23 * want).all())
+
+
 def check_grad(W, E, T, n, k, kind="bf16", sizes=None, offsets=torch.int32, extra=0, lead=0, gap=0, accumulate=False,
                start=0, seed=0):
     g = torch.Generator().manual_seed(seed)
