@@ -250,9 +250,9 @@ __device__ __forceinline__ uint64_t uniform(uint64_t x) {
 //
 // DIRECT: straight into LDS, for addresses and lengths in whole pieces.  What is past an end has an offset out of the
 // buffer's range, for which the card writes zeros.  Else by registers, a stage ahead: pieces at any element's address,
-// and of one that its row ends in the last whole piece before that end, moved down when it goes to LDS (loads that wait
-// for nothing in between: 3,001 rows of 515 by 7 FP16 matrices of 515 x 1003 took 37 us with branches around each load, 20
-// without).
+// and of one that its row ends in the last whole piece before that end, moved down when it goes to LDS.  Stages that
+// exist as a whole are loaded without a branch (8,192 FP32 rows by 8 matrices of 1023 x 1021: 268 us, 226 so), and in no
+// stage does one load wait for another (3,001 FP16 rows of 515 by 7 of 515 x 1003: 37, 20 so).
 constexpr uint32_t kNowhere = 0x80000000u;
 
 // 16 bytes a lane from base + off to LDS, lane after lane from `lds` on; zeros for off = kNowhere.  Written out
@@ -279,6 +279,7 @@ struct Operand {
   int32_t left;     // r from there on
   int32_t extent;   // of the tile's own index
   int32_t length;   // of a row in memory
+  bool held_whole;
   int32_t held_end; // what `left` or `extent` was when `held` was asked for
   uint32_t off[DIRECT ? kLoads : 1];
   uint4v held[DIRECT ? 1 : kLoads];
@@ -317,10 +318,28 @@ struct Operand {
   __device__ __forceinline__ void ask(uint32_t lds, int i) {
     if constexpr (DIRECT) {
       load_to_lds(at, lds + (i * NW + wave) * 1024, off[i]);
-    } else {
-      constexpr int N = kPiece<T>;
+    }
+  }
+  // Whether all of the next stage exists.
+  __device__ __forceinline__ bool whole() const {
+    return TURNED ? left >= kStageLen<T> && extent >= BT : extent >= BT && left >= kStageLen<T>;
+  }
+  __device__ __forceinline__ void ask_held() {
+    constexpr int N = kPiece<T>;
+    const int end = TURNED ? extent : left;
+    held_whole = whole();
+    held_end = end;
+    if (held_whole) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int row = Lay::load_row(i, wave, lane), c = Lay::load_piece(row, lane) * N;
+        held[i] = __builtin_bit_cast(uint4v, *(const Near<T, N>*)(at + row * row_bytes + c * (int)sizeof(T)));
+      }
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
       const int row = Lay::load_row(i, wave, lane), c = Lay::load_piece(row, lane) * N;
-      const int end = TURNED ? extent : left;
       const char* from = at + row * row_bytes;
       uint4v v = {};
       if ((TURNED ? row < left : row < extent) && c < end) {
@@ -335,7 +354,6 @@ struct Operand {
         }
       }
       held[i] = v;
-      held_end = end;
     }
   }
   __device__ __forceinline__ void on() {
@@ -345,8 +363,12 @@ struct Operand {
       if (left < kStageLen<T>) shorten();
   }
   __device__ __forceinline__ void ask(uint32_t lds) {
+    if constexpr (DIRECT) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) ask(lds, i);
+      for (int i = 0; i < kLoads; ++i) ask(lds, i);
+    } else {
+      ask_held();
+    }
     on();
   }
   // What was asked for into LDS, by registers.
@@ -358,7 +380,7 @@ struct Operand {
         constexpr int N = kPiece<T>;
         const int c = Lay::load_piece(Lay::load_row(i, wave, lane), lane) * N;
         uint4v v = held[i];
-        if (c + N > held_end && c < held_end && length >= N) {
+        if (!held_whole && c + N > held_end && c < held_end && length >= N) {
           typedef unsigned __int128 wide;
           v = __builtin_bit_cast(uint4v, __builtin_bit_cast(wide, v) >> ((c + N - held_end) * 8 * (int)sizeof(T)));
         }
@@ -448,7 +470,7 @@ __device__ __forceinline__ void store_all(const ExpertArgs& a, T* out, int64_t P
 
 // One BP x BQ tile, WP x WQ of it per wavefront; NS stages in LDS.
 template <typename T, int MODE, int BP, int BQ, int WP, int WQ, int NS, bool DIRECT>
-__global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, DIRECT && BP / WP * (BQ / WQ) == 8 ? 1 : 2) void k_expert(ExpertArgs a) {
+__global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, DIRECT ? (BP / WP * (BQ / WQ) == 8 ? 1 : 2) : 4) void k_expert(ExpertArgs a) {
   constexpr int NW = BP / WP * (BQ / WQ);
   constexpr int MI = WP / 16, NJ = WQ / 16;
   typedef Operand<T, BP, NW, MODE != FORWARD, true, DIRECT> OpP;
@@ -552,6 +574,18 @@ __global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, DIRECT && BP / WP * (BQ /
       ask(now);
       now = now + kStage == NS * kStage ? 0 : now + kStage;
     }
+  } else if constexpr (!DIRECT) {  // by registers: more wavefronts a CU instead of fragments ahead of their use
+    for (int s = 0; s < stages; ++s) {
+      read(now, 0, f0);
+      products(f0, 0, kAll);
+      read(now, 1, f0);
+      products(f0, 0, kAll);
+      wait_for<63, 0>();
+      block_barrier();
+      put(now);
+      ask(now);
+      now ^= kStage;
+    }
   } else {
     read(0, 0, f0);
     for (int s = 0; s < stages; ++s) {
@@ -560,29 +594,24 @@ __global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, DIRECT && BP / WP * (BQ /
       products(f0, 0, kAll);
       spread<(LP::kReads * MI + LQ::kReads * NJ), kAll * kMfmas<T>>();
       __builtin_amdgcn_sched_barrier(0);
-      wait_for<DIRECT ? (NS - 2) * kLoads : 63, 0>();
+      wait_for<(NS - 2) * kLoads, 0>();
       block_barrier();
       __builtin_amdgcn_sched_barrier(0);
       constexpr int kSome = kAll >= 2 * kLoads ? kLoads : 0;  // products between the loads
-      if constexpr (DIRECT) {
 #pragma unroll
-        for (int n = 0; n < kLoads; ++n) {
-          if (n < OpP::kLoads)
-            p.ask(lds_at + now, n);
-          else
-            q.ask(lds_at + now + LP::kBytes, n - OpP::kLoads);
-          if (kSome) products(f1, n, n + 1);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        p.on();
-        q.on();
-      } else {
-        put(now);
-        ask(now);
+      for (int n = 0; n < kLoads; ++n) {
+        if (n < OpP::kLoads)
+          p.ask(lds_at + now, n);
+        else
+          q.ask(lds_at + now + LP::kBytes, n - OpP::kLoads);
+        if (kSome) products(f1, n, n + 1);
+        __builtin_amdgcn_sched_barrier(0);
       }
+      p.on();
+      q.on();
       read(next, 0, f0);
-      products(f1, DIRECT ? kSome : 0, kAll);
-      if (DIRECT) spread<(LP::kReads * MI + LQ::kReads * NJ), (kAll - kSome) * kMfmas<T>>();
+      products(f1, kSome, kAll);
+      spread<(LP::kReads * MI + LQ::kReads * NJ), (kAll - kSome) * kMfmas<T>>();
       __builtin_amdgcn_sched_barrier(0);
       now = next;
     }
@@ -758,8 +787,8 @@ struct Plan {
 };
 
 constexpr int64_t kCUs = 256;
-constexpr int64_t kSplitBelow = 2 * kCUs;  // tiles of all workers and experts below which tokens are shared
-constexpr int64_t kMinShare = 256;         // tokens of a share, at least
+constexpr int64_t kSlots = 2 * kCUs;  // blocks of tiles of 128 that the card holds at once
+constexpr int64_t kMinShare = 256;       // tokens of a share, at least (128: 38 us where 30,011 of 4 take 34)
 
 void finish_plan(Plan* p, const Shape& s, int mode) {
   p->bp = p->tile == WIDE ? 256 : p->tile == SLIM ? 32 : 128;
@@ -782,14 +811,24 @@ void finish_plan(Plan* p, const Shape& s, int mode) {
 }
 
 // The form with shared tokens, whatever the operands' type and alignment.
+//
+// Tokens are shared where that saves more than it costs, in us: a tile's loop takes 0.012 a token, an expert may have
+// twice the average, and what is above an even share of all tiles' tokens is saved; a second launch and its latency
+// cost 8, a share of a tile written and read again 0.026.  BF16, shared and not: 32,768 tokens of 16 experts into 512 x
+// 512: 50 and 86; 2,048 of 4 into 1024 x 1024: 37 and 17; 3,001 of 7 into 515 x 1003: 41 and 24; the rule takes the slower
+// form of 32,768 tokens of 20 into 512 x 512 (48 and 60) and of 6 into 1024 x 1024 (115 and 91), where the experts' sizes
+// decide, which the host does not know.
 Plan shared_plan(const Shape& s) {
   Plan p = {};
   p.tile = MIDDLE;
   const int64_t tiles = ceil_div(s.n, 128) * ceil_div(s.k, 128), all = s.W * s.E * tiles;
   int64_t rows = s.T > 0 ? s.T : 1;
-  if (all < kSplitBelow) {
-    const int64_t share = ceil_div(ceil_div(s.W * s.T * tiles, kSplitBelow), 64) * 64;
-    rows = share < kMinShare ? kMinShare : share;
+  if (all < kSlots && s.T > 0) {
+    int64_t share = ceil_div(ceil_div(s.W * s.T * tiles, kSlots), 64) * 64;
+    share = share < kMinShare ? kMinShare : share;
+    const double saved = 0.012 * (2.0 * s.T / s.E - (double)s.W * s.T * tiles / kSlots);
+    const double cost = 8.0 + 0.026 * s.W * (double)(s.T / share + s.E) * tiles;
+    if (saved > cost) rows = share;
   }
   p.rows = (int32_t)rows;
   finish_plan(&p, s, GRAD);
