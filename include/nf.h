@@ -801,6 +801,24 @@ nf_status nf_expert_grad(const void* dy, int64_t dy_ld, int64_t dy_stride, const
                          size_t ws_bytes, void* stream);
 
 /*
+ * Profiling query (no paper counterpart): the kernel that a call of these
+ * sizes runs.  whole = 1 where rows can be read 16 bytes at a time: tensors
+ * 16-byte aligned, their strides (up to 2^20 between rows) and the lengths of
+ * rows whole multiples of 16 bytes (n of the product's x need not be).  All
+ * zeros where nothing is launched.  Errors as for the calls.  Pure host
+ * function.
+ */
+enum { NF_EXPERT_PRODUCT = 0, NF_EXPERT_TRANSPOSED = 1, NF_EXPERT_GRAD = 2 };
+typedef struct {
+  int32_t tile_columns;  /* columns of the result that a block takes: 32, 128, 256 */
+  int32_t tile_rows;     /* rows of it                                             */
+  int32_t direct;        /* loads straight into LDS, else by registers             */
+  int32_t share;         /* GRAD: tokens of a share, 0 where none are shared       */
+} nf_expert_path_info;
+nf_status nf_expert_path(int32_t op, int32_t type, int32_t W, int64_t T, int32_t E, int64_t n, int64_t k,
+                         int32_t whole, nf_expert_path_info* info_host);
+
+/*
  * Norms over many tensors, each of one group's tensors (a worker's gradients,
  * a kind of parameter), and the tensors scaled by them (no paper
  * counterpart).  With ||g|| the 2-norm of all elements of group g:

@@ -42,11 +42,12 @@ EXPORTS = ["nf_abi_version", "nf_last_error", "nf_mask_from_segments", "nf_works
            "nf_slice_scales", "nf_compact_signcount_reduce",
            "nf_embedding_lookup", "nf_embedding_workspace_bytes", "nf_embedding_grad",
            "nf_orthogonal_workspace_bytes", "nf_orthogonal_path", "nf_orthogonalize", "nf_orthogonal_update",
-           "nf_expert_product", "nf_expert_grad_workspace_bytes", "nf_expert_grad",
+           "nf_expert_product", "nf_expert_grad_workspace_bytes", "nf_expert_path", "nf_expert_grad",
            "nf_norm_plan_init", "nf_norm_table_init", "nf_grad_norm", "nf_grad_clip", "nf_grad_norm_clip"]
 NF_TYPE_F32, NF_TYPE_BF16, NF_TYPE_F16 = 0, 1, 2
 NF_PRODUCTS_SINGLE, NF_PRODUCTS_SPLIT = 0, 1
 NF_ORTHOGONAL_MAX_STEPS = 12
+NF_EXPERT_PRODUCT, NF_EXPERT_TRANSPOSED, NF_EXPERT_GRAD = 0, 1, 2
 NF_SUP_WARMUP, NF_SUP_LOWBIT, NF_SUP_COOLDOWN, NF_SUP_GUARD = 0, 1, 2, 3
 
 
@@ -108,6 +109,10 @@ class nf_orthogonal_path_info(ctypes.Structure):
 class nf_matrix_step(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("momentum", ctypes.c_float), ("weight_decay", ctypes.c_float),
                 ("scale", ctypes.c_float), ("nesterov", ctypes.c_int32)]
+
+
+class nf_expert_path_info(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("tile_columns", "tile_rows", "direct", "share")]
 
 
 class nf_norm_tensor(ctypes.Structure):
@@ -214,6 +219,7 @@ def load(path=None):
         "nf_expert_grad_workspace_bytes": (_SZ, [_I32, _I64, _I32, _I64, _I64]),
         "nf_expert_grad": (ctypes.c_int, [_P, _I64, _I64, _P, _I64, _I64, _I32, _P, _I32, _I64, _I32, _I64, _I32, _I64,
                                           _I64, _I32, _P, _I64, _I64, _P, _SZ, _P]),
+        "nf_expert_path": (ctypes.c_int, [_I32, _I32, _I32, _I64, _I32, _I64, _I64, _I32, _P]),
         "nf_norm_plan_init": (ctypes.c_int, [_P, _I64, _I32, _P]),
         "nf_norm_table_init": (ctypes.c_int, [_P, _I64, _P, _P, _SZ, _P]),
         "nf_grad_norm": (ctypes.c_int, [_P, _P, _P, _P, _SZ, _P]),
@@ -849,6 +855,13 @@ def nf_expert_product(x, w, offsets, y, transposed=False, stream=None):
 
 def nf_expert_grad_workspace_bytes(W, T, E, n, k):
     return int(load().nf_expert_grad_workspace_bytes(W, T, E, n, k))
+
+
+def nf_expert_path(op, type, W, T, E, n, k, whole=True):
+    """The kernel that a call of these sizes runs (profiling)."""
+    info = nf_expert_path_info()
+    _check(load().nf_expert_path(op, type, W, T, E, n, k, 1 if whole else 0, ctypes.byref(info)))
+    return info
 
 
 def nf_expert_grad(dy, x, offsets, grads, offset, ws, accumulate=False, matrix_stride=None, stream=None):

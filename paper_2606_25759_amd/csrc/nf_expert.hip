@@ -36,7 +36,7 @@ typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
 typedef int16_t short4v __attribute__((ext_vector_type(4)));
 
-enum { FORWARD, BACKWARD, GRAD };
+enum { FORWARD = NF_EXPERT_PRODUCT, BACKWARD = NF_EXPERT_TRANSPOSED, GRAD = NF_EXPERT_GRAD };
 
 constexpr int kStageBytes = 128;  // of a row in LDS: 64 elements of 16 bits, 32 of FP32
 constexpr int kMaxExperts = 4096;
@@ -1005,6 +1005,26 @@ size_t nf_expert_grad_workspace_bytes(int32_t W, int64_t T, int32_t E, int64_t n
   using namespace nf;
   if (check_sizes(W, T, E, n, k) || T == 0 || E == 0 || n == 0 || k == 0) return 0;
   return shared_plan(Shape{W, E, T, n, k}).part_bytes;
+}
+
+nf_status nf_expert_path(int32_t op, int32_t type, int32_t W, int64_t T, int32_t E, int64_t n, int64_t k,
+                         int32_t whole, nf_expert_path_info* info) {
+  using namespace nf;
+  if (!info) return bad("info is NULL");
+  *info = nf_expert_path_info{};
+  if (op < NF_EXPERT_PRODUCT || op > NF_EXPERT_GRAD) return bad("unknown op");
+  if (!known_type(type)) return bad("unknown element type");
+  if (whole != 0 && whole != 1) return bad("whole must be 0 or 1");
+  if (const char* why = check_sizes(W, T, E, n, k)) return bad(why);
+  if (E == 0 || (op == NF_EXPERT_GRAD ? n == 0 || k == 0 : T == 0 || (op == NF_EXPERT_PRODUCT ? n : k) == 0))
+    return set_error(NF_OK, "");
+  const Plan p = plan_of(Shape{W, E, T, n, k}, op, type, whole != 0);
+  if (too_large(p, W)) return set_error(NF_ERR_UNSUPPORTED, "more tiles than a launch has");
+  info->tile_columns = p.bp;
+  info->tile_rows = p.bq;
+  info->direct = whole;
+  info->share = p.part_bytes ? p.rows : 0;
+  return set_error(NF_OK, "");
 }
 
 nf_status nf_expert_grad(const void* dy, int64_t dy_ld, int64_t dy_stride, const void* x, int64_t x_ld,

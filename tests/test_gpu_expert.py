@@ -91,10 +91,13 @@ def test_product(W, E, T, n, k, extra, kind, out, back):
                   offsets=torch.int64 if T % 2 else torch.int32)
 
 
-@pytest.mark.parametrize("kind,out", [("bf16", "bf16"), ("f16", "f32")])
-@pytest.mark.parametrize("W,E,T,n,k,back", [
+WIDE_PRODUCTS = [  # W, E, T, n, k, back
     (1, 4, 16_500, 1032, 264, False), (1, 4, 16_500, 264, 1032, True), (2, 3, 9_000, 1024, 200, False),
-    (2, 3, 9_000, 72, 1024, True), (1, 2, 66_000, 192, 64, False), (1, 30, 8_000, 2056, 320, False)])
+    (2, 3, 9_000, 72, 1024, True), (1, 2, 66_000, 192, 64, False), (1, 30, 8_000, 2056, 320, False)]
+
+
+@pytest.mark.parametrize("kind,out", [("bf16", "bf16"), ("f16", "f32")])
+@pytest.mark.parametrize("W,E,T,n,k,back", WIDE_PRODUCTS)
 def test_product_wide_tiles(W, E, T, n, k, back, kind, out):
     """Sizes that take tiles of 256, their lengths ending inside stages and tiles; an expert of a single row."""
     g = torch.Generator().manual_seed(T)
@@ -104,11 +107,14 @@ def test_product_wide_tiles(W, E, T, n, k, back, kind, out):
     check_product(W, E, T, n, k, back, kind, out, sizes=sizes, seed=1)
 
 
+OTHER_PRODUCTS = [  # W, E, T, n, k, extra
+    (1, 1, 1, 512, 2048, 0), (1, 2, 70, 320, 1030, 2), (1, 6, 1500, 520, 264, 0), (2, 5, 900, 515, 260, 1),
+    (1, 3, 3000, 768, 1032, 0), (1, 2, 3000, 769, 515, 3), (1, 3, 4000, 512, 520, 0), (1, 3, 4000, 513, 515, 0)]
+
+
 @pytest.mark.parametrize("back", [False, True])
 @pytest.mark.parametrize("kind", list(TYPES))
-@pytest.mark.parametrize("W,E,T,n,k,extra", [
-    (1, 1, 1, 512, 2048, 0), (1, 2, 70, 320, 1030, 2), (1, 6, 1500, 520, 264, 0), (2, 5, 900, 515, 260, 1),
-    (1, 3, 3000, 768, 1032, 0), (1, 2, 3000, 769, 515, 3)])
+@pytest.mark.parametrize("W,E,T,n,k,extra", OTHER_PRODUCTS)
 def test_product_other_tiles(W, E, T, n, k, extra, kind, back):
     """Sizes that take tiles of 32, of 128 x 32 and of 128, straight into LDS and by registers."""
     check_product(W, E, T, n, k, back, kind, "f32", extra=extra, seed=n + k)
@@ -230,9 +236,20 @@ def test_grad(W, E, T, n, k, extra, lead, gap, kind, accumulate):
                offsets=torch.int64 if T % 2 else torch.int32)
 
 
+WIDE_GRADS = [(1, 4, 900, 2056, 2040), (2, 33, 300, 1032, 1048), (1, 64, 500, 512, 520)]  # W, E, T, n, k
+SHARED_GRADS = [(1, 2, 9000, 72, 40), (2, 1, 5000, 130, 70), (1, 3, 12_000, 129, 71)]
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("W,E,T,n,k", SHARED_GRADS)
+def test_grad_shared_tokens(W, E, T, n, k, kind):
+    check_grad(W, E, T, n, k, kind, lead=5, seed=T)
+    check_grad(W, E, T, n, k, kind, accumulate=True, seed=T)
+
+
 @pytest.mark.parametrize("accumulate", [False, True])
 @pytest.mark.parametrize("kind", ["bf16", "f16"])
-@pytest.mark.parametrize("W,E,T,n,k", [(1, 4, 900, 2056, 2040), (2, 33, 300, 1032, 1048), (1, 64, 500, 512, 520)])
+@pytest.mark.parametrize("W,E,T,n,k", WIDE_GRADS)
 def test_grad_wide_tiles(W, E, T, n, k, kind, accumulate):
     """Sizes that take tiles of 256: experts by length over all XCDs, and (few tiles an expert) one after the other."""
     check_grad(W, E, T, n, k, kind, lead=3, accumulate=accumulate, seed=E)
@@ -241,9 +258,9 @@ def test_grad_wide_tiles(W, E, T, n, k, kind, accumulate):
 @pytest.mark.parametrize("kind", list(TYPES))
 def test_grad_shares_of_uneven_experts(kind):
     """Tokens shared between blocks: experts of no share, of one, of several and of all."""
-    for sizes in ([0, 5000, 0, 3], [256, 257, 512, 513], [0, 0, 0, 2900], [1, 0, 1, 255]):
-        check_grad(1, 4, sum(sizes) + 9, 40, 72, kind, sizes=[sizes])
-        check_grad(1, 4, sum(sizes) + 9, 40, 72, kind, sizes=[sizes], start=9, accumulate=True, lead=1)
+    for sizes in ([0, 15_000, 0, 3], [256, 257, 4512, 513], [0, 0, 0, 6900], [1, 0, 1, 255]):
+        check_grad(1, 4, 16_000, 40, 72, kind, sizes=[sizes])
+        check_grad(1, 4, 16_000, 40, 72, kind, sizes=[sizes], start=9, accumulate=True, lead=1)
 
 
 def test_grad_infinities_stay_in_their_expert():
@@ -277,6 +294,20 @@ def test_offsets_that_make_no_sense_touch_nothing_else():
         nf.nf_expert_grad(x[..., :n].contiguous(), x, off, rows, 8, ws)
         assert bool((y[:10] == 3).all()) and bool((y[-10:] == 3).all())
         assert bool((rows[:, :8] == 3).all()) and bool((rows[:, -8:] == 3).all())
+    for values in ([0, 9000, 0, 9000, 0, 9000], [9000, 0, 9000, -1, 10_000, 3]):  # with shared tokens, larger tiles
+        T, n, k = 9000, 72, 40
+        off = torch.tensor(values, device=DEV)
+        need = nf.nf_expert_grad_workspace_bytes(1, T, E, n, k)
+        assert need > 0
+        ws = torch.full((need + 512,), 0x55, dtype=torch.uint8, device=DEV)
+        x, dy = torch.randn(T, k, device=DEV).half(), torch.randn(T, n, device=DEV).half()
+        rows = torch.full((1, E * n * k + 16), 3.0, device=DEV)
+        nf.nf_expert_grad(dy, x, off, rows, 8, ws[256:256 + need])
+        assert bool((rows[:, :8] == 3).all()) and bool((rows[:, -8:] == 3).all())
+        assert bool((ws[:256] == 0x55).all()) and bool((ws[256 + need:] == 0x55).all())
+        y = torch.full((T + 20, n), 3.0, device=DEV)
+        nf.nf_expert_product(x, torch.randn(E, n, k, device=DEV).half(), off, y[10:-10])
+        assert bool((y[:10] == 3).all()) and bool((y[-10:] == 3).all())
 
 
 def test_gradients_against_differences():
