@@ -5,6 +5,7 @@
 //                FORWARD   y = W x:     P = W (n x k),    Q = x rows,   r over k
 //                BACKWARD  y = W^T x:   P = W^T (k x n),  Q = x rows,   r over n
 //                GRAD      dW = dy^T x: P = x^T (k x T),  Q = dy^T,     r over tokens
+//   k_slim     FORWARD and BACKWARD for few rows: a tile's sum shared by the block's wavefronts
 //   k_join     GRAD with tokens shared between blocks: the shares' sums, in order
 //
 // Group sizes are known on the device only, so the grid is the most that any
@@ -100,13 +101,15 @@ __device__ __forceinline__ int scan(int v, int lane) {
 }
 
 // The group and unit of tile `block` of a worker, `per` tiles a unit; false past the last.  `id` becomes the tile's
-// number in its group.  Blocks go round the eight XCDs: each takes a contiguous share of the tiles.
+// number in its group.  Blocks go round the eight XCDs: each takes a contiguous share of the tiles, whose operands its
+// L2 then holds.
 template <int MODE>
 __device__ __forceinline__ bool find(const ExpertArgs& a, int64_t worker, int block, int per, Group* g, int* id) {
   const int lane = threadIdx.x % 64, each = (a.E + 63) / 64;
   int64_t first, rows;
   if (MODE == GRAD && a.spread) {
-    // Tiles of long and short experts cost their tokens: every XCD takes an eighth of each expert's tiles, longest first.
+    // Tiles of long and short experts cost their tokens: every XCD takes an eighth of each expert's tiles, longest first
+    // (32,768 tokens of 32 into 4096 x 2048: 692 us, 1,304 with a few experts an XCD).
     const int x = block & 7, j = block >> 3, lo = x * per >> 3, n = ((x + 1) * per >> 3) - lo, u = j / n;
     if (u >= a.E) return false;
     units_of<MODE>(a, worker, min(lane, a.E - 1), &first, &rows);
@@ -469,8 +472,26 @@ __device__ __forceinline__ void store_all(const ExpertArgs& a, T* out, int64_t P
 }
 
 // One BP x BQ tile, WP x WQ of it per wavefront; NS stages in LDS.
+//
+// One barrier a stage, in its middle: behind it the stage's place is free and the next one's loads have arrived.  The
+// reads of the half stage that is next, and the loads of the stage after next, are placed between the products of the
+// half that is in registers.
+//
+// What bounds it.  32,768 rows by 32 matrices of 4096 x 2048 in BF16, uneven: 528 to 554 us FORWARD (1.0 PFLOP/s), 527
+// to 551 BACKWARD, 670 to 690 GRAD; rows spread evenly over 16: 500 to 545, 450 to 490, 507 to 555, where a library's
+// one product of the sums' size takes 400, 436 and 525 (x W^T, x W, dy^T x).  Without loads the loop takes 379, with
+// loads that all hit the L2 454, with its own 492 (FORWARD, even).  LDS has no bank conflicts; the matrix cores are at
+// work 54% of the cycles, at 1.95 to 2.1 GHz (the library's product: 75% at 1.75: the card's power holds either).  What
+// did not help: panels fetched into the L2 ahead (0 to 7% slower), a second barrier that lets loads go out half a stage
+// earlier (0), four wavefronts of 128 x 128 (5 to 15% slower), 256 x 128 in two blocks a CU (0 to 15% slower), blocks
+// that stay for several tiles and load the next one's before they store (0 to 4% slower), matrix instructions of 32 x 32
+// (3 to 6% slower).  Small calls are bound by the launch and three waits for memory in a row: offsets, operands, stores;
+// few rows by the matrices: 128 rows of 64 experts, 1024 x 2048: 29 us, 8 TB/s of what the last call left in the caches,
+// 47 from memory.  FP32 is bound by its own matrix instruction: 32,768 rows by 8 of 1024 x 1024: 650 us, 0.10 of 0.15
+// PFLOP/s.
 template <typename T, int MODE, int BP, int BQ, int WP, int WQ, int NS, bool DIRECT>
-__global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, DIRECT ? (BP / WP * (BQ / WQ) == 8 ? 1 : 2) : 4) void k_expert(ExpertArgs a) {
+__global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, DIRECT ? (BP / WP * (BQ / WQ) == 8 ? 1 : 2) : 4) void k_expert(
+    ExpertArgs a) {
   constexpr int NW = BP / WP * (BQ / WQ);
   constexpr int MI = WP / 16, NJ = WQ / 16;
   typedef Operand<T, BP, NW, MODE != FORWARD, true, DIRECT> OpP;
