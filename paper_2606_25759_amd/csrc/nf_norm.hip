@@ -15,10 +15,9 @@
 // 5.95 TB/s.  The two passes of a clipping read what they scale twice; the
 // second goes through each block's pieces from the last one back, since what
 // was read last may still be in the card's cache: 1.3G BF16 into FP32 in
-// 2,004 us (10.5 GB moved, 5.25 TB/s), 25.6M FP32 in 57 to 61.  A dozen small
+// 1,990 us (10.5 GB moved, 5.3 TB/s), 25.6M FP32 in 50.  A dozen small
 // tensors are one block and one launch: 3 us, 5.4 with the call.  Blocks of
-// 1,024 threads, as many as the card holds: with two or four times as many
-// the clipping of 25.6M takes 68 or 78.
+// 1,024 threads, as many as the card holds at once.
 #include <limits.h>
 #include <math.h>
 #include <string.h>
@@ -34,6 +33,7 @@ namespace {
 
 constexpr int kNormThreads = 1024;
 constexpr int kNormWaves = kNormThreads / 64;
+constexpr int kWavesAtOnce = 8;            // a SIMD: two blocks a CU (25.6M FP32 clipped: 50 us, 57 with one)
 constexpr int64_t kMostBlocks = 512;       // what the card holds at once
 constexpr int64_t kLeastPiece = 1024, kMostPiece = 32768;  // elements
 constexpr int64_t kPieceCost = 1024;       // of a piece besides its elements, in elements
@@ -173,7 +173,7 @@ __device__ float norm_of(const NormArgs& a, int group, double* s) {
   return (float)sqrt(sum_of_block(sum, s));
 }
 
-__global__ __launch_bounds__(kNormThreads) void k_squares(NormArgs a) {
+__global__ __launch_bounds__(kNormThreads, kWavesAtOnce) void k_squares(NormArgs a) {
   __shared__ double s[kNormWaves];
   const Block b = a.blocks[blockIdx.x];
   double sum = 0.0;
@@ -201,7 +201,7 @@ __global__ __launch_bounds__(kNormThreads) void k_norms(NormArgs a) {
 
 // SUMS: the norm from the blocks' sums, else from a.norms.
 template <bool SUMS>
-__global__ __launch_bounds__(kNormThreads) void k_clip(NormArgs a) {
+__global__ __launch_bounds__(kNormThreads, kWavesAtOnce) void k_clip(NormArgs a) {
   __shared__ double s[kNormWaves];
   const Block b = a.blocks[blockIdx.x];
   float norm;
@@ -243,7 +243,7 @@ nf_status check_tensor(const nf_norm_tensor& t, int32_t groups) {
   if (!t.src) return bad("src is NULL");
   if ((uintptr_t)t.src % type_bytes(t.src_type) || (t.dst && (uintptr_t)t.dst % type_bytes(t.dst_type)))
     return set_error(NF_ERR_ALIGNMENT, "src or dst not aligned to its elements");
-  for (int i = 0; i < 2; ++i) {  // its last byte has an address
+  for (int i = 0; i < (t.dst ? 2 : 1); ++i) {  // its last byte has an address
     const __int128 ld = t.rows > 1 ? (i ? t.dst_ld : t.src_ld) : 0;
     if ((ld * (t.rows - 1) + t.cols) * 4 > (__int128)INT64_MAX / 4) return bad("a tensor is larger than memory");
   }

@@ -100,6 +100,14 @@ def test_plan_of_tensors_that_share_elements():
             assert st == status, (tensors, nf.nf_last_error())
 
 
+def test_what_is_not_read_may_be_anything():
+    """The strides of one row, and those of a place that there is not."""
+    for change in (dict(dst_ld=-1), dict(dst_ld=1 << 62, dst_type=77), dict(rows=1, src_ld=-5),
+                   dict(rows=1, src_ld=0, dst=0x20000, dst_ld=-7)):
+        st, plan = plan_of([tensor(**change)])
+        assert st == nf.NF_OK and plan.pieces == 1, change
+
+
 def test_plan_sizes():
     assert plan_of([])[0] == nf.NF_OK and plan_of([], 0)[0] == nf.NF_OK
     lib = nf.load()
