@@ -784,7 +784,7 @@ nf_status nf_expert_product(const void* x, int32_t type, int64_t x_ld, int64_t x
  *   grads[w*worker_stride + e*matrix_stride + i*k + j] =
  *       sum of dy[w][t][i] x[w][t][j] over the rows t of expert e
  * Experts without a row get zeros.  With accumulate != 0 the sums are added to
- * what the row holds.  Sums are FP32 in an order fixed by the sizes, without
+ * what the row holds, and experts without a row are left alone.  Sums are FP32 in an order fixed by the sizes, without
  * floating-point atomics: two calls give the same bits.
  * `grads` is expert 0's matrix in worker 0's row (a row's base plus the
  * matrices' offset in it), 4-byte aligned; it shares no element with dy or x.

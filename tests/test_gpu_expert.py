@@ -209,6 +209,8 @@ def check_grad(W, E, T, n, k, kind="bf16", sizes=None, offsets=torch.int32, extr
             want, size = a.t() @ b, a.abs().t() @ b.abs()
             seg = slice(lead + e * each, lead + e * each + n * k)
             got = rows[i, seg].view(n, k)
+            if accumulate and c == 0:
+                assert torch.equal(got.view(torch.int32), before[i, seg].view(n, k).view(torch.int32))
             if accumulate:
                 old = before[i, seg].view(n, k).double()
                 want, size = want + old, size + old.abs()
