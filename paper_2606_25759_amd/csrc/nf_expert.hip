@@ -553,8 +553,8 @@ __device__ __forceinline__ void store_all(const ExpertArgs& a, T* out, int64_t P
 // reads of the half stage that is next, and the loads of the stage after next, are placed between the products of the
 // half that is in registers.
 //
-// What bounds it.  32,768 rows by 32 matrices of 4096 x 2048 in BF16, uneven: 528 to 554 us FORWARD (1.0 PFLOP/s), 527
-// to 551 BACKWARD, 670 to 690 GRAD; rows spread evenly over 16: 500 to 545, 450 to 490, 507 to 555, where a library's
+// What bounds it.  32,768 rows by 32 matrices of 4096 x 2048 in BF16, uneven: 528 to 555 us FORWARD (1.0 PFLOP/s), 524
+// to 551 BACKWARD, 658 to 690 GRAD; rows spread evenly over 16: 500 to 545, 450 to 490, 507 to 555, where a library's
 // one product of the sums' size takes 400, 436 and 525 (x W^T, x W, dy^T x).  Without loads the loop takes 379, with
 // loads that all hit the L2 454, with its own 492 (FORWARD, even).  LDS has no bank conflicts; the matrix cores are at
 // work 54% of the cycles, at 1.95 to 2.1 GHz (the library's product: 75% at 1.75: the card's power holds either).  What
