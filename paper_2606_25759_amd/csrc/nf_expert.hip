@@ -553,7 +553,7 @@ __device__ __forceinline__ void store_all(const ExpertArgs& a, T* out, int64_t P
 // reads of the half stage that is next, and the loads of the stage after next, are placed between the products of the
 // half that is in registers.
 //
-// What bounds it.  32,768 rows by 32 matrices of 4096 x 2048 in BF16, uneven: 528 to 555 us FORWARD (1.0 PFLOP/s), 524
+// What bounds it.  32,768 rows by 32 matrices of 4096 x 2048 in BF16, uneven: 528 to 555 us FORWARD (1.0 PFLOP/s), 522
 // to 551 BACKWARD, 658 to 690 GRAD; rows spread evenly over 16: 500 to 545, 450 to 490, 507 to 555, where a library's
 // one product of the sums' size takes 400, 436 and 525 (x W^T, x W, dy^T x).  Without loads the loop takes 379, with
 // loads that all hit the L2 454, with its own 492 (FORWARD, even).  LDS has no bank conflicts; the matrix cores are at
@@ -563,8 +563,8 @@ __device__ __forceinline__ void store_all(const ExpertArgs& a, T* out, int64_t P
 // that stay for several tiles and load the next one's before they store (0 to 4% slower), matrix instructions of 32 x 32
 // (3 to 6% slower).  Small calls are bound by the launch and three waits for memory in a row: offsets, operands, stores;
 // few rows by the matrices: 128 rows of 64 experts, 1024 x 2048: 29 us, 8 TB/s of what the last call left in the caches,
-// 47 from memory.  FP32 is bound by its own matrix instruction: 32,768 rows by 8 of 1024 x 1024: 650 us, 0.10 of 0.15
-// PFLOP/s.
+// 47 from memory.  FP32 is bound by its own matrix instruction: 32,768 rows by 32 of 4096 x 2048: 4,064 us, 0.135 of 0.15
+// PFLOP/s; by what of tiles and rounds is empty in smaller calls.
 template <typename T, int MODE, int BP, int BQ, int WP, int WQ, int NS, bool DIRECT>
 __global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, DIRECT ? (BP / WP * (BQ / WQ) == 8 ? 1 : 2) : 4) void k_expert(
     ExpertArgs a) {
@@ -940,8 +940,10 @@ Plan shared_plan(const Shape& s) {
 //          128 through registers, 547; 4,096 rows of 16, 2048 x 2048 (192 tiles): - / 80 / 56 / 57; 1,024 rows of one,
 //          4096 x 4096 (64): - / 68 / 48 / 90
 //   128    8,192 rows of 8, 1024 x 1024 (576): 149 / 47 / 34 / 34; where there are too few, 128 x 32: 1,024 rows of one,
-//          1024 x 1024 (64): 21 / 13 / 15 / 29; and so for FP32, whose products are slow enough for any tile's loads:
-//          8,192 rows of 8, 1024 x 1024: 321 / 186 / 203
+//          1024 x 1024 (64): 21 / 13 / 15 / 29.  FP32, whose products take long enough for a part of a tile and of a round
+//          to count for more, needs two rounds and experts of 192 rows: 128 x 32 / 128: 32,768 rows of 32, 4096 x 2048:
+//          4,676 / 4,064; of 128, 256 and 512, 2048 x 1024: 1,369 / 1,297, 1,475 / 1,536, 1,735 / 2,167; 16,384 of 8,
+//          2047 x 1021: 869 / 769; 8,192 of 8, 2048 x 2048 (1,088 tiles): 692 / 663, 1024 x 1024 (544): 186 / 203
 //   128x32 for experts of few rows: 2,048 rows of 64, 1024 x 1024: 63 / 29 / 36 / 31
 //   32     where there are few of those: one row, 4096 x 4096 (32 of 128 x 32): 15 / 22 / 39; 64 rows of 8, 2048 x 2048
 //          (150): 19 / 15 / 25
@@ -959,7 +961,7 @@ Plan plan_of(const Shape& s, int mode, int32_t type, bool direct) {
     auto tiles = [&](int64_t bp, int64_t bq) { return s.W * (s.T / bq + (some + 1) / 2) * ceil_div(len, bp); };
     if (fits && rows >= 192 && s.W * ceil_div(s.T, 256) * ceil_div(len, 256) >= kCUs)
       p.tile = WIDE;
-    else if (rows > 48 && type != NF_TYPE_F32 && tiles(128, 128) >= kCUs / 2)
+    else if (type != NF_TYPE_F32 ? rows > 48 && tiles(128, 128) >= kCUs / 2 : rows >= 192 && tiles(128, 128) >= 2 * kSlots)
       p.tile = MIDDLE;
     else
       p.tile = tiles(128, 32) > kCUs * 3 / 8 ? NARROW : SLIM;
@@ -987,12 +989,10 @@ void launch(const Plan& p, const Shape& s, const ExpertArgs& a, hipStream_t stre
       return;
     }
   }
-  if constexpr (sizeof(T) == 2 || MODE == GRAD) {
-    if constexpr (DIRECT)
-      k_expert<T, MODE, 128, 128, 64, 64, 2, true><<<grid, 256, 0, stream>>>(a);
-    else
-      k_expert<T, MODE, 128, 128, 64, 32, 2, false><<<grid, 512, 0, stream>>>(a);
-  }
+  if constexpr (DIRECT)
+    k_expert<T, MODE, 128, 128, 64, 64, 2, true><<<grid, 256, 0, stream>>>(a);
+  else
+    k_expert<T, MODE, 128, 128, 64, 32, 2, false><<<grid, 512, 0, stream>>>(a);
 }
 
 template <int MODE>

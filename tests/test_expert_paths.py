@@ -32,6 +32,8 @@ def reached():
             add(nf.NF_EXPERT_GRAD, kind, W, T, E, n, k, (n, k))
         for W, E, T, n, k, back in t.WIDE_PRODUCTS if kind != "f32" else []:
             add(OPS[back], kind, W, T, E, n, k, (n, k) if back else (k,))
+        for W, E, T, n, k, back in t.F32_PRODUCTS if kind == "f32" else []:
+            add(OPS[back], kind, W, T, E, n, k, (n, k) if back else (k,))
     return {f for f in found if f[2]}
 
 
@@ -40,9 +42,7 @@ def test_every_kernel_is_tested():
     for kind in CODES:
         for direct in (0, 1):
             for op in OPS:
-                want |= {(op, kind, 32, 32, direct, False), (op, kind, 128, 32, direct, False)}
-                if kind != "f32":
-                    want.add((op, kind, 128, 128, direct, False))
+                want |= {(op, kind, c, r, direct, False) for c, r in ((32, 32), (128, 32), (128, 128))}
             want |= {(nf.NF_EXPERT_GRAD, kind, 128, 128, direct, shared) for shared in (False, True)}
         if kind != "f32":
             want |= {(op, kind, 256, 256, 1, False) for op in (*OPS, nf.NF_EXPERT_GRAD)}

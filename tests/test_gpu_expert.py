@@ -107,6 +107,18 @@ def test_product_wide_tiles(W, E, T, n, k, back, kind, out):
     check_product(W, E, T, n, k, back, kind, out, sizes=sizes, seed=1)
 
 
+F32_PRODUCTS = [  # W, E, T, n, k, back
+    (8, 3, 1024, 1664, 48, False), (8, 3, 1024, 44, 1660, True), (8, 3, 1024, 1601, 35, False), (8, 3, 1025, 37, 1603, True)]
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("W,E,T,n,k,back", F32_PRODUCTS)
+def test_product_f32_large_tiles(W, E, T, n, k, back, out):
+    """FP32 in tiles of 128, straight into LDS and by registers; uneven experts, rows of none before and behind them."""
+    check_product(W, E, T, n, k, back, "f32", out, seed=n)
+    check_product(W, E, T, n, k, back, "f32", out, sizes=[[1, 0, T - 130], [0, T, 0]] * (W // 2), start=0, seed=k)
+
+
 OTHER_PRODUCTS = [  # W, E, T, n, k, extra
     (1, 1, 1, 512, 2048, 0), (1, 2, 70, 320, 1030, 2), (1, 6, 1500, 520, 264, 0), (2, 5, 900, 515, 260, 1),
     (1, 3, 3000, 768, 1032, 0), (1, 2, 3000, 769, 515, 3), (1, 3, 4000, 512, 520, 0), (1, 3, 4000, 513, 515, 0)]
