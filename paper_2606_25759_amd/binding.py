@@ -918,7 +918,9 @@ def _parts(src, dst, name):
 class NormPlan:
     """The tensors of nf_grad_norm and nf_grad_clip and their device table, for
     as long as they stay where they are; keeps them alive.  Made by
-    norm_plan."""
+    norm_plan.  May be dropped while calls on torch's streams are under way; a
+    graph that holds such a call, or a call on a raw handle of a stream that is
+    not torch's current or default one, has to end before the plan does."""
 
     def __init__(self, tensors, groups, keep, stream):
         self.keep = keep
@@ -927,8 +929,24 @@ class NormPlan:
         _check(load().nf_norm_plan_init(entries, len(tensors), groups, ctypes.byref(self.plan)))
         self.table = empty_workspace(self.plan.table_bytes)
         self.device = self.table.device
+        handle, owner = _stream(stream), _stream(None)
+        if handle != owner:  # what its memory was used for before may still be under way there
+            torch.cuda.current_stream().synchronize()
         _check(load().nf_norm_table_init(entries, len(tensors), ctypes.byref(self.plan), self.table.data_ptr(),
-                                         self.table.numel(), _stream(stream)))
+                                         self.table.numel(), handle))
+        self.noted = {owner}  # streams that the allocator waits for before it gives the table's memory away
+
+    def stream(self, stream):
+        """The handle of a call's stream, which the allocator is told of the first time."""
+        handle = _stream(stream)
+        if handle not in self.noted and not torch.cuda.is_current_stream_capturing():
+            if not hasattr(stream, "cuda_stream"):
+                stream = (torch.cuda.current_stream() if handle == _stream(None) else
+                          torch.cuda.default_stream() if handle == 0 else None)
+            if stream is not None:
+                self.table.record_stream(stream)
+                self.noted.add(handle)
+        return handle
 
 
 def norm_plan(src, dst=None, groups=None, n_groups=None, stream=None):
@@ -975,21 +993,21 @@ def nf_grad_norm(plan, norms, ws, stream=None):
     """norms[g] = the 2-norm of all of group g's tensors (float32)."""
     _here(plan.table, norms, ws)
     _check(load().nf_grad_norm(plan.table.data_ptr(), ctypes.byref(plan.plan), _norms(plan, norms),
-                               _dev_ptr(ws, torch.uint8, "ws"), ws.numel(), _stream(stream)))
+                               _dev_ptr(ws, torch.uint8, "ws"), ws.numel(), plan.stream(stream)))
 
 
 def nf_grad_clip(plan, norms, max_norm, eps=1e-6, stream=None):
     """dst = min(1, max_norm / (norms[g] + eps)) src for every tensor."""
     _here(plan.table, norms)
     _check(load().nf_grad_clip(plan.table.data_ptr(), ctypes.byref(plan.plan), _norms(plan, norms), max_norm, eps,
-                               _stream(stream)))
+                               plan.stream(stream)))
 
 
 def nf_grad_norm_clip(plan, max_norm, norms, ws, eps=1e-6, stream=None):
     """nf_grad_norm and nf_grad_clip by its norms."""
     _here(plan.table, norms, ws)
     _check(load().nf_grad_norm_clip(plan.table.data_ptr(), ctypes.byref(plan.plan), max_norm, eps, _norms(plan, norms),
-                                    _dev_ptr(ws, torch.uint8, "ws"), ws.numel(), _stream(stream)))
+                                    _dev_ptr(ws, torch.uint8, "ws"), ws.numel(), plan.stream(stream)))
 
 
 # ------------------------------------------------------- result decoding
