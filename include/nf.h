@@ -767,10 +767,13 @@ nf_status nf_orthogonal_update(const void* grad, int32_t grad_type, int64_t grad
  * offsets that descend the results are not defined.
  * x and w of one NF_TYPE_*, y of any, aligned to their elements; rows x_ld
  * (w_ld, y_ld), workers x_stride (y_stride) and matrices w_stride elements
- * apart.  y shares no element with x or w.
+ * apart.  y shares no element with x or w; rows that lie between one another's
+ * are taken.  A call that shares one is refused where the layouts show it in a
+ * few operations: one of the two a single run of memory, or both of rows
+ * equally far apart throughout, or both beginning at the same place.
  * NF_ERR_INVALID_ARG: W outside [1, 255], T outside [0, 2^24], E outside
  * [0, 4096], n or k outside [0, 2^20], an ld below the columns, a stride too
- * small with W > 1 (w_stride with E > 1), y at x or w.  NF_ERR_UNSUPPORTED:
+ * small with W > 1 (w_stride with E > 1), y over x or w.  NF_ERR_UNSUPPORTED:
  * more than 2^22 tiles (of 128 x 128 or 256 x 256, 128 x 32 for experts of
  * few rows and FP32).  T, E or the columns of y = 0 launches nothing.
  */
@@ -787,7 +790,8 @@ nf_status nf_expert_product(const void* x, int32_t type, int64_t x_ld, int64_t x
  * what the row holds, and experts without a row are left alone.  Sums are FP32 in an order fixed by the sizes, without
  * floating-point atomics: two calls give the same bits.
  * `grads` is expert 0's matrix in worker 0's row (a row's base plus the
- * matrices' offset in it), 4-byte aligned; it shares no element with dy or x.
+ * matrices' offset in it), 4-byte aligned; it shares no element with dy or x,
+ * which is checked as there.
  * dy (n columns) and x (k columns) of one NF_TYPE_*; offsets, layouts and
  * errors as for nf_expert_product, and NF_ERR_INVALID_ARG for matrix_stride
  * < n * k with E > 1 or worker_stride below a worker's matrices with W > 1.

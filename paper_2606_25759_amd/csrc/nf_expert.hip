@@ -1033,6 +1033,43 @@ bool misplaced(int32_t W, int64_t rows, int64_t cols, int64_t ld, int64_t stride
   return ld < cols || (W > 1 && rows > 0 && overlaps(stride, rows, ld, cols));
 }
 
+// W x rows runs of cols elements, as a caller lays them out, in bytes.
+struct Runs {
+  __int128 at, count, far, each;  // far: from one run's beginning to the next one's; each: a run's length
+  bool even;                      // all runs lie `far` apart
+};
+
+Runs runs_of(const void* p, int32_t W, int64_t rows, int64_t cols, int64_t ld, int64_t stride, int32_t type) {
+  const __int128 size = (__int128)type_bytes(type);
+  Runs r = {(__int128)(uintptr_t)p, rows, ld * size, cols * size, true};
+  if (rows == 1) r.far = r.each;
+  if (W > 1) {
+    if (rows == 1) r.far = stride * size;
+    r.even = stride * size == rows * r.far;
+    if (r.even) r.count *= W;
+  }
+  if (r.even && (r.count == 1 || r.far == r.each)) {
+    r.each *= r.count;
+    r.far = r.each;
+    r.count = 1;
+  }
+  return r;
+}
+
+// Whether two tensors share an element, as far as a few divisions tell: exactly where one is a single run or their runs
+// lie equally far apart, and where they begin at the same place.
+bool share(const Runs& a, const Runs& b) {
+  if (a.count <= 0 || b.count <= 0 || a.each <= 0 || b.each <= 0) return false;
+  if (a.at == b.at) return true;
+  if (!a.even || !b.even || (a.count > 1 && b.count > 1 && a.far != b.far)) return false;
+  // runs i of a and j of b meet where b.at - a.at + j b.far - i a.far is in (-b.each, a.each); with d the run of a less
+  // that of b, of one far: the first d, rounded down, that brings b's beginning below a's end
+  const __int128 far = a.count > 1 ? a.far : b.far, between = b.at - a.at - a.each;
+  __int128 d = between / far + (between % far < 0 ? 0 : 1);
+  if (d < 1 - b.count) d = 1 - b.count;
+  return d <= a.count - 1 && b.at - a.at - d * far < a.each && b.at - a.at - d * far > -b.each;
+}
+
 bool whole(const void* p, int64_t ld, int64_t stride, int32_t type) {
   const int64_t bytes = (int64_t)type_bytes(type);
   return (uintptr_t)p % 16 == 0 && ld % (16 / bytes) == 0 && stride % (16 / bytes) == 0 && ld <= (1 << 20);
@@ -1077,6 +1114,9 @@ nf_status nf_expert_product(const void* x, int32_t type, int64_t x_ld, int64_t x
                       k % piece == 0 && (!transposed || n % piece == 0);
   const Plan p = plan_of(s, transposed ? BACKWARD : FORWARD, type, direct);
   if (too_large(p, W)) return set_error(NF_ERR_UNSUPPORTED, "more tiles than a launch has");
+  const Runs to = runs_of(y, W, T, out, y_ld, y_stride, y_type);
+  if (share(to, runs_of(x, W, T, in, x_ld, x_stride, type)) || share(to, runs_of(w, E, n, k, w_ld, w_stride, type)))
+    return bad("y shares an element with x or w");
   ExpertArgs a = {};
   a.p = w;
   a.p_ld = w_ld;
@@ -1156,6 +1196,9 @@ nf_status nf_expert_grad(const void* dy, int64_t dy_ld, int64_t dy_stride, const
   if (ws_bytes < need) return set_error(NF_ERR_WORKSPACE, "workspace smaller than nf_expert_grad_workspace_bytes");
   if (need && !ws) return set_error(NF_ERR_WORKSPACE, "workspace is NULL");
   if ((uintptr_t)ws % 256) return set_error(NF_ERR_ALIGNMENT, "workspace not 256-byte aligned");
+  const Runs to = runs_of(grads, W, E, n * k, matrix_stride, worker_stride, NF_TYPE_F32);
+  if (share(to, runs_of(dy, W, T, n, dy_ld, dy_stride, type)) || share(to, runs_of(x, W, T, k, x_ld, x_stride, type)))
+    return bad("grads shares an element with dy or x");
   ExpertArgs a = {};
   a.p = x;
   a.p_ld = x_ld;
