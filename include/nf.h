@@ -830,10 +830,12 @@ nf_status nf_expert_path(int32_t op, int32_t type, int32_t W, int64_t T, int32_t
  *   dst = min(1, max_norm / (norms[g] + eps)) src    (1 where norms[g] + eps = 0)
  * Squares and their sums are FP64 in a fixed order, a norm is rounded once to
  * FP32; the factor is rounded to FP32 and the product taken in FP32 and
- * rounded once to dst's type.  An infinity in a group makes its norm infinite
- * and the factor zero, which leaves zeros, and NaN where the infinities were;
- * a NaN makes the norm and all of dst NaN.  A group without elements has the
- * norm 0.
+ * rounded once to dst's type.  A group whose norm is above FP32's range
+ * (3.4e38) gets an infinite norm and the factor zero, which leaves zeros: no
+ * sum overflows on the way to it, but the norm itself does.  An infinity in a
+ * group does the same, with NaN where the infinities were; a NaN makes the norm
+ * and all of dst NaN.  A factor below 2^-126 has a subnormal number's bits, and
+ * below 2^-150 it is zero.  A group without elements has the norm 0.
  *
  * A tensor is rows x cols elements, those of a row adjacent, rows src_ld
  * (dst_ld) apart; of more dimensions it is several of these.  dst may be
