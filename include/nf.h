@@ -795,7 +795,8 @@ nf_status nf_expert_product(const void* x, int32_t type, int64_t x_ld, int64_t x
  * dy (n columns) and x (k columns) of one NF_TYPE_*; offsets, layouts and
  * errors as for nf_expert_product, and NF_ERR_INVALID_ARG for matrix_stride
  * < n * k with E > 1 or worker_stride below a worker's matrices with W > 1.
- * T = 0 writes zeros.  E, n or k = 0 launches nothing.
+ * T = 0 writes zeros.  E, n or k = 0 launches nothing.  The workspace, at most
+ * 64 MiB, is what a call of any type at any alignment needs.
  */
 size_t nf_expert_grad_workspace_bytes(int32_t W, int64_t T, int32_t E, int64_t n, int64_t k);
 nf_status nf_expert_grad(const void* dy, int64_t dy_ld, int64_t dy_stride, const void* x, int64_t x_ld,

@@ -21,6 +21,8 @@
 //
 // FP16 and BF16 operands go to the matrix cores as they are, FP32 operands to
 // its FP32 instruction; sums are FP32 in any case, each result rounded once.
+#include <math.h>
+
 #include <type_traits>
 
 #include "nf_internal.h"
@@ -908,15 +910,52 @@ void finish_plan(Plan* p, const Shape& s, int mode) {
   p->grid = p->spread ? 8 * s.E * ceil_div(per, 8) : ceil_div(units * per, 8) * 8;  // workers begin on the same XCD
 }
 
-// The form with shared tokens, whatever the operands' type and alignment.
+// FP32 takes six to eight times as long a stage as 16 bits, so that what of tiles and rounds is empty, or one after the
+// other, counts for more than the rules for 16 bits allow.  The two functions below estimate a call's time and leave their
+// choice where another's estimate is less by 15% and 4 us; experts' sizes, which the host does not know, move a call's
+// time by as much as that.
+bool pays(double other, double own) { return other < 0.85 * own && other < own - 4.0; }
+
+// Tokens of a share, `rows` by the rule of grad_plan.
 //
-// Tokens are shared where that saves more than it costs, in us: a tile's loop takes 0.012 a token, an expert may have
-// twice the average, and what is above an even share of all tiles' tokens is saved; a second launch and its latency
-// cost 8, a share of a tile written and read again 0.026.  BF16, shared and not: 32,768 tokens of 16 experts into 512 x
-// 512: 50 and 86; 2,048 of 4 into 1024 x 1024: 37 and 17; 3,001 of 7 into 515 x 1003: 41 and 24; the rule takes the slower
-// form of 32,768 tokens of 20 into 512 x 512 (48 and 60) and of 6 into 1024 x 1024 (115 and 91), where the experts' sizes
-// decide, which the host does not know.
-Plan shared_plan(const Shape& s) {
+// In us: a tile's loop takes 0.075 a token, by registers 0.095; blocks beyond one a CU share its rate; the largest of N
+// experts, of all workers, may have 1 + 0.4 log2 N times the average; a second launch costs 4, a share of a tile written and
+// read again 0.024.  Over 1,473 sizes of 1 to 64 experts this takes 3.3% more than the best share, the rule for 16 bits 13%,
+// and up to seven times as long.  In us, not shared and shared: 32,768 tokens of 32 into 256 x 256: 213 and 70; 16,384 of 16
+// into 512 x 512: 226 and 119; 13,462 of 42 experts and 6 workers into 116 x 23, by registers: 176 and 70.
+constexpr int64_t kMostShared = 1024;  // tiles' shares: 64 MiB of workspace
+constexpr int64_t kShares[] = {64, 128, 192, 256, 384, 512, 768, 1024, 2048, 4096, 8192};
+
+int64_t share_f32(const Shape& s, int64_t tiles, bool direct, int64_t rows) {
+  const double even = (double)s.W * s.T * tiles / kCUs;  // tokens of a CU
+  const int64_t some = s.T < s.E ? s.T : s.E;
+  const double times = (1.0 + 0.4 * log2((double)s.W * s.E)) / s.E;
+  const double largest = s.E == 1 || times > 1.0 ? s.T : times * s.T;
+  auto time = [&](int64_t share) {
+    const bool shared = share < s.T;
+    const double shares = shared ? (double)s.T / share : 0.0, each = share < largest ? share : largest;
+    double loop = each;
+    if (s.E == 1)
+      loop *= ceil_div(s.W * tiles * ceil_div(s.T, share), kCUs);
+    else if (s.W * tiles * (shares + some) > kCUs && 1.05 * even > 0.55 * each)
+      loop = 1.05 * even + 0.45 * each;
+    return (direct ? 0.075 : 0.095) * loop + (shared ? 4.0 + 0.024 * s.W * (shares + s.E) * tiles : 0.0);
+  };
+  int64_t best = s.T;
+  for (int64_t share : kShares)
+    if (share < s.T && s.W * (s.T / share + s.E) * tiles <= kMostShared && time(share) < time(best)) best = share;
+  return pays(time(best), time(rows)) ? best : rows;
+}
+
+// The gradient in tiles of 128, with shared tokens where that saves more than it costs, in us.
+//
+// 16 bits: a tile's loop takes 0.012 a token, an expert may have twice the average, and what is above an even share of
+// all tiles' tokens is saved; a second launch and its latency cost 8, a share of a tile written and read again 0.026.
+// BF16, shared and not: 32,768 tokens of 16 experts into 512 x 512: 50 and 86; 2,048 of 4 into 1024 x 1024: 37 and 17;
+// by registers, 3,001 of 7 into 515 x 1003: 41 and 24; the rule takes the slower form of 32,768 tokens of 20 into 512 x 512
+// (48 and 60) and of 6 into 1024 x 1024 (115 and 91), where the experts' sizes decide, which the host does not know.  Over
+// 1,473 sizes of 1 to 64 experts, a third of them by registers, BF16 takes 3% more than the best share.
+Plan grad_plan(const Shape& s, bool f32, bool direct) {
   Plan p = {};
   p.tile = MIDDLE;
   const int64_t tiles = ceil_div(s.n, 128) * ceil_div(s.k, 128), all = s.W * s.E * tiles;
@@ -928,10 +967,51 @@ Plan shared_plan(const Shape& s) {
     const double cost = 8.0 + 0.026 * s.W * (double)(s.T / share + s.E) * tiles;
     if (saved > cost) rows = share;
   }
+  if (f32 && s.T > 0) rows = share_f32(s, tiles, direct, rows);
   p.rows = (int32_t)rows;
   finish_plan(&p, s, GRAD);
   if (rows < s.T) p.part_bytes = (size_t)(s.W * p.units * tiles) * 128 * 128 * sizeof(float);
   return p;
+}
+
+// The tile of an FP32 product, `tile` by the rule of plan_of.
+//
+// The estimate is
+//   max(rounds x (4 + stages x alone), most blocks of a CU x stages x together) us,
+// with the times of a stage of a block alone on its CU and of one that shares it, below; a wavefront of a tile of 32 has a
+// quarter of the stages.  Over 2,136 sizes of 1 to 64 experts it takes 1.9% more than the best of the three, the rule of
+// plan_of 6%, and up to three times as long where results are narrow or few and sums long (32 / 128 x 32 / 128): 22,635
+// rows of 3 experts, 19 x 3000: 65 / 156 / 179; 3,326 rows of one, transposed, 3762 x 80, by registers: 77 / 227 / 326.
+struct StageTime {
+  int64_t blocks;  // that a CU holds
+  double alone, together;
+};
+constexpr StageTime kStageF32[2][3] = {  // [direct][tile]
+    {{2, 1.51, 1.10}, {4, 1.32, 0.87}, {2, 2.55, 2.39}},
+    {{1, 0.61, 0.61}, {2, 0.57, 0.54}, {2, 1.56, 1.84}}};
+
+int tile_f32(const Shape& s, int64_t len, int64_t r, bool direct, int tile) {
+  const int64_t all = ceil_div(r, kStageBytes / 4);
+  const double some = s.E * (1.0 - exp(-(double)s.T / s.E));  // experts with rows, if each row's is any of them
+  auto time = [&](int t) {
+    const int64_t bp = t == SLIM ? 32 : 128, bq = t == MIDDLE ? 128 : 32, stages = t == SLIM ? ceil_div(all, 4) : all;
+    const double full = (double)s.T / bq + 0.5 * some;  // last tiles are half empty
+    const bool one = s.E == 1 || s.T == 1;
+    const double units = one ? ceil_div(s.T, bq) : some > full ? some : full;
+    const StageTime& c = kStageF32[direct][t];
+    double sum = 0.0;
+    for (double off : {0.9, 1.0, 1.1}) {  // a block more than there are CUs may be one less
+      const double blocks = s.W * units * ceil_div(len, bp) * (one ? 1.0 : off);
+      const double rounds = ceil(blocks / (kCUs * c.blocks)) * (4.0 + stages * c.alone);
+      const double rate = ceil(blocks / kCUs) * stages * c.together;
+      sum += rounds > rate ? rounds : rate;
+    }
+    return sum / 3.0;
+  };
+  int best = SLIM;
+  for (int t : {NARROW, MIDDLE})
+    if (time(t) < time(best)) best = t;
+  return pays(time(best), time(tile)) ? best : tile;
 }
 
 // Which tiles a call takes, by how many there are of each if the experts' sizes are alike (measured in us, BF16 unless
@@ -943,7 +1023,8 @@ Plan shared_plan(const Shape& s) {
 //          1024 x 1024 (64): 21 / 13 / 15 / 29.  FP32, whose products take long enough for a part of a tile and of a round
 //          to count for more, needs two rounds and experts of 192 rows: 128 x 32 / 128: 32,768 rows of 32, 4096 x 2048:
 //          4,676 / 4,064; of 128, 256 and 512, 2048 x 1024: 1,369 / 1,297, 1,475 / 1,536, 1,735 / 2,167; 16,384 of 8,
-//          2047 x 1021: 869 / 769; 8,192 of 8, 2048 x 2048 (1,088 tiles): 692 / 663, 1024 x 1024 (544): 186 / 203
+//          2047 x 1021: 869 / 769; 8,192 of 8, 2048 x 2048 (1,088 tiles): 692 / 663, 1024 x 1024 (544): 186 / 203; what
+//          tile_f32 finds by its estimate goes before
 //   128x32 for experts of few rows: 2,048 rows of 64, 1024 x 1024: 63 / 29 / 36 / 31
 //   32     where there are few of those: one row, 4096 x 4096 (32 of 128 x 32): 15 / 22 / 39; 64 rows of 8, 2048 x 2048
 //          (150): 19 / 15 / 25
@@ -954,7 +1035,8 @@ Plan plan_of(const Shape& s, int mode, int32_t type, bool direct) {
   const int64_t len = mode == FORWARD ? s.n : s.k;
   const bool fits = direct && type != NF_TYPE_F32 && len >= 192;
   if (mode == GRAD) {
-    if (!fits || s.n < 192 || s.W * s.E * ceil_div(s.n, 256) * ceil_div(s.k, 256) < kCUs) return shared_plan(s);
+    if (!fits || s.n < 192 || s.W * s.E * ceil_div(s.n, 256) * ceil_div(s.k, 256) < kCUs)
+      return grad_plan(s, type == NF_TYPE_F32, direct);
     p.tile = WIDE;
     p.rows = (int32_t)(s.T > 0 ? s.T : 1);
   } else {
@@ -965,6 +1047,7 @@ Plan plan_of(const Shape& s, int mode, int32_t type, bool direct) {
       p.tile = MIDDLE;
     else
       p.tile = tiles(128, 32) > kCUs * 3 / 8 ? NARROW : SLIM;
+    if (type == NF_TYPE_F32) p.tile = tile_f32(s, len, mode == FORWARD ? s.k : s.n, direct, p.tile);
   }
   finish_plan(&p, s, mode);
   return p;
@@ -1142,7 +1225,11 @@ nf_status nf_expert_product(const void* x, int32_t type, int64_t x_ld, int64_t x
 size_t nf_expert_grad_workspace_bytes(int32_t W, int64_t T, int32_t E, int64_t n, int64_t k) {
   using namespace nf;
   if (check_sizes(W, T, E, n, k) || T == 0 || E == 0 || n == 0 || k == 0) return 0;
-  return shared_plan(Shape{W, E, T, n, k}).part_bytes;
+  const Shape s = {W, E, T, n, k};
+  size_t most = 0;  // of any type and alignment
+  for (const Plan& p : {grad_plan(s, false, true), grad_plan(s, true, true), grad_plan(s, true, false)})
+    most = p.part_bytes > most ? p.part_bytes : most;
+  return most;
 }
 
 nf_status nf_expert_path(int32_t op, int32_t type, int32_t W, int64_t T, int32_t E, int64_t n, int64_t k,
