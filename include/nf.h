@@ -817,7 +817,8 @@ enum { NF_EXPERT_PRODUCT = 0, NF_EXPERT_TRANSPOSED = 1, NF_EXPERT_GRAD = 2 };
 typedef struct {
   int32_t tile_columns;  /* columns of the result that a block takes: 32, 128, 256 */
   int32_t tile_rows;     /* rows of it                                             */
-  int32_t direct;        /* loads straight into LDS, else by registers             */
+  int32_t direct;        /* 16 bytes a lane straight into LDS; else by elements of
+                            FP32 straight into LDS, or by registers              */
   int32_t share;         /* GRAD: tokens of a share, 0 where none are shared       */
 } nf_expert_path_info;
 nf_status nf_expert_path(int32_t op, int32_t type, int32_t W, int64_t T, int32_t E, int64_t n, int64_t k,

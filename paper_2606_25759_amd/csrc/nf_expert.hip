@@ -240,10 +240,8 @@ struct Tile {
       return v;
     }
   }
-  // The place in the tile of element e of lane's row of fragment i, for P (rows of D), and of its column, for Q.
-  static __device__ __forceinline__ int column_of(int j, int lane) {
-    return 16 * j + lane % 16;
-  }
+  // The place in the tile of a lane's column of fragment j of Q.
+  static __device__ __forceinline__ int column_of(int j, int lane) { return 16 * j + lane % 16; }
 };
 
 __device__ __forceinline__ uint64_t uniform(uint64_t x) {
@@ -253,31 +251,41 @@ __device__ __forceinline__ uint64_t uniform(uint64_t x) {
 
 // One operand's way from memory to LDS.
 //
-// DIRECT: straight into LDS, for addresses and lengths in whole pieces.  What is past an end has an offset out of the
-// buffer's range, for which the card writes zeros.  Else by registers, a stage ahead: pieces at any element's address,
-// and of one that its row ends in the last whole piece before that end, moved down when it goes to LDS.  Stages that
-// exist as a whole are loaded without a branch (8,192 FP32 rows by 8 matrices of 1023 x 1021: 268 us, 226 so), and in no
+// PIECES: straight into LDS, 16 bytes a lane, for addresses and lengths in whole pieces.  ELEMENTS: the same by single
+// elements of FP32, at any of their addresses and for any lengths.  What is past an end has an offset out of the buffer's
+// range, for which the card writes zeros.  REGISTERS, a stage ahead: pieces at any element's address, and of one that its
+// row ends in the last whole piece before that end, moved down when it goes to LDS; for 16 bits, FP32 gradients of narrow
+// sides or few tokens (grad_plan), and rows so far apart that a tile's offsets would pass 32 bits.  Stages that exist as a whole are loaded without a branch, and in no
 // stage does one load wait for another (3,001 FP16 rows of 515 by 7 of 515 x 1003: 37, 20 so).
+enum { REGISTERS, ELEMENTS, PIECES };
 constexpr uint32_t kNowhere = 0x80000000u;
 
-// 16 bytes a lane from base + off to LDS, lane after lane from `lds` on; zeros for off = kNowhere.  Written out
-// because the compiler, where it knows of such a load, waits for it before each transposing read of LDS (32,768 x 4096 x
-// 2048 in 16 even experts: 580 us transposed, 490 without).  It has no result in registers, and who reads what it brings
-// waits by wait_for().  The wait states are for a base that a vector instruction has just written; M0, which a clobber list
-// cannot name, has no other use in these kernels.
+// 16 bytes a lane (4: PIECE false) from base + off to LDS, lane after lane from `lds` on; zeros for off = kNowhere.
+// Written out because the compiler, where it knows of such a load, waits for it before each transposing read of LDS (32,768 x
+// 4096 x 2048 in 16 even experts: 580 us transposed, 490 without).  It has no result in registers, and who reads what it
+// brings waits by wait_for().  The wait states are for a base that a vector instruction has just written; M0, which a clobber
+// list cannot name, has no other use in these kernels.
+template <bool PIECE>
 __device__ __forceinline__ void load_to_lds(const char* base, uint32_t lds, uint32_t off) {
   typedef uint32_t uint4s __attribute__((ext_vector_type(4)));
   const uint64_t at = (uint64_t)(uintptr_t)base;
   const uint4s buffer = {(uint32_t)at, (uint32_t)(at >> 32), 0x7fffffffu, 0x00020000u};
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off),
-               "s"(buffer)
-               : "memory");
+  if constexpr (PIECE)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off),
+                 "s"(buffer)
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(buffer)
+                 : "memory");
 }
 
-template <typename T, int BT, int NW, bool TURNED, bool PAIRS, bool DIRECT>
+template <typename T, int BT, int NW, bool TURNED, bool PAIRS, int LOAD>
 struct Operand {
   typedef Tile<T, BT, NW, TURNED, PAIRS> Lay;
-  static constexpr int kLoads = Lay::kLoads;
+  static constexpr bool DIRECT = LOAD != REGISTERS;
+  static constexpr int kEach = LOAD == ELEMENTS ? 4 : 1;  // loads of 1 KiB
+  static constexpr int kLoads = Lay::kLoads * kEach;
+  static_assert(LOAD != ELEMENTS || sizeof(T) == 4, "elements of FP32");
   const char* at;   // of the tile at the next stage
   int64_t step;     // bytes of a stage
   int64_t row_bytes;
@@ -303,32 +311,33 @@ struct Operand {
     if constexpr (DIRECT) {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        const int row = Lay::load_row(i, wave, lane), piece = Lay::load_piece(row, lane);
-        const bool inside = TURNED ? piece * kPiece<T> < extent : row < extent;
-        off[i] = inside ? (uint32_t)(row * (int32_t)row_bytes + piece * 16) : kNowhere;
+        const int row = row_of(i), c = element_of(i);
+        off[i] = (TURNED ? c : row) < extent ? (uint32_t)(row * (int32_t)row_bytes + c * (int)sizeof(T)) : kNowhere;
       }
       if (left < kStageLen<T>) shorten();
     }
   }
+  // The row and first element of it that this lane's i-th load brings: lanes take pieces, or four of them one.
+  __device__ __forceinline__ int slot(int i) const { return LOAD == ELEMENTS ? i % kEach * 16 + lane / 4 : lane; }
+  __device__ __forceinline__ int row_of(int i) const { return Lay::load_row(i / kEach, wave, slot(i)); }
+  __device__ __forceinline__ int element_of(int i) const {
+    return Lay::load_piece(row_of(i), slot(i)) * kPiece<T> + (LOAD == ELEMENTS ? lane % 4 : 0);
+  }
   // The stage that is next ends before its place does.
   __device__ __forceinline__ void shorten() {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int row = Lay::load_row(i, wave, lane);
-      if ((TURNED ? row : Lay::load_piece(row, lane) * kPiece<T>) >= left) off[i] = kNowhere;
-    }
+    for (int i = 0; i < kLoads; ++i)
+      if ((TURNED ? row_of(i) : element_of(i)) >= left) off[i] = kNowhere;
   }
   // Asks for the next stage: into LDS, or into registers.  In parts, for the loads to be placed one by one: load i of
   // the stage, and on to the next one.
   __device__ __forceinline__ void ask(uint32_t lds, int i) {
     if constexpr (DIRECT) {
-      load_to_lds(at, lds + (i * NW + wave) * 1024, off[i]);
+      load_to_lds<LOAD == PIECES>(at, lds + (i / kEach * NW + wave) * 1024 + i % kEach * 256, off[i]);
     }
   }
   // Whether all of the next stage exists.
-  __device__ __forceinline__ bool whole() const {
-    return TURNED ? left >= kStageLen<T> && extent >= BT : extent >= BT && left >= kStageLen<T>;
-  }
+  __device__ __forceinline__ bool whole() const { return left >= kStageLen<T> && extent >= BT; }
   __device__ __forceinline__ void ask_held() {
     constexpr int N = kPiece<T>;
     const int end = TURNED ? extent : left;
@@ -565,15 +574,18 @@ __device__ __forceinline__ void store_all(const ExpertArgs& a, T* out, int64_t P
 // that stay for several tiles and load the next one's before they store (0 to 4% slower), matrix instructions of 32 x 32
 // (3 to 6% slower).  Small calls are bound by the launch and three waits for memory in a row: offsets, operands, stores;
 // few rows by the matrices: 128 rows of 64 experts, 1024 x 2048: 29 us, 8 TB/s of what the last call left in the caches,
-// 47 from memory.  FP32 is bound by its own matrix instruction: 32,768 rows by 32 of 4096 x 2048: 4,064 us, 0.135 of 0.15
-// PFLOP/s; by what of tiles and rounds is empty in smaller calls.
-template <typename T, int MODE, int BP, int BQ, int WP, int WQ, int NS, bool DIRECT>
-__global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, DIRECT ? (BP / WP * (BQ / WQ) == 8 ? 1 : 2) : 4) void k_expert(
+// 47 from memory.  FP32 is bound by its own matrix instruction: 32,768 rows by 32 of 4096 x 2048: 3,970 us, 0.138 of 0.15
+// PFLOP/s; by what of tiles and rounds is empty in smaller calls.  By elements a stage of 128 x 128 is 128 loads, some 32
+// cycles each: as long as its products, which hides them if barely (16,384 rows by 8 of 2047 x 1021: 575 us, 670 by
+// registers; 8,192 of 8 into 1023 x 1021: 161, 190).
+template <typename T, int MODE, int BP, int BQ, int WP, int WQ, int NS, int LOAD>
+__global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, LOAD ? (BP / WP * (BQ / WQ) == 8 ? 1 : 2) : 4) void k_expert(
     ExpertArgs a) {
   constexpr int NW = BP / WP * (BQ / WQ);
   constexpr int MI = WP / 16, NJ = WQ / 16;
-  typedef Operand<T, BP, NW, MODE != FORWARD, true, DIRECT> OpP;
-  typedef Operand<T, BQ, NW, MODE == GRAD, false, DIRECT> OpQ;
+  constexpr bool DIRECT = LOAD != REGISTERS;
+  typedef Operand<T, BP, NW, MODE != FORWARD, true, LOAD> OpP;
+  typedef Operand<T, BQ, NW, MODE == GRAD, false, LOAD> OpQ;
   typedef typename OpP::Lay LP;
   typedef typename OpQ::Lay LQ;
   constexpr int kLoads = OpP::kLoads + OpQ::kLoads;
@@ -647,14 +659,26 @@ __global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, DIRECT ? (BP / WP * (BQ /
   };
 
   // Stage s: its first half is in registers.  Behind the barrier every wavefront has read all of it, and its loads of
-  // stage s + 1 are in LDS; its place goes to stage s + NS.  Stages past the last are asked for as well, and are
-  // zeros, so that the number of loads under way does not change.
+  // stage s + 1 are in LDS; its place goes to stage s + NS.  Pieces of stages past the last are asked for as well, and are
+  // zeros, so that the number of loads under way does not change; elements, whose loads take the most of a short sum's time,
+  // are not.
   const int stages = __builtin_amdgcn_readfirstlane((r + kStageLen<T> - 1) / kStageLen<T>);
   Frags f0, f1;
+  auto exists = [&](int s) { return LOAD != ELEMENTS || s < stages; };
+  auto wait_below = [&](int s) {  // until stage s's loads are in LDS, with those of NS - 2 stages behind it under way
+    if (exists(s + NS - 2))
+      wait_for<DIRECT ? (NS - 2) * kLoads : 63, 0>();
+    else
+      wait_for<0, 0>();
+  };
   if constexpr (DIRECT) {
 #pragma unroll
-    for (int s = 0; s < NS; ++s) ask(s * kStage);
-    wait_for<(NS - 1) * kLoads, 0>();
+    for (int s = 0; s < NS; ++s)
+      if (exists(s)) ask(s * kStage);
+    if (exists(NS - 1))
+      wait_for<(NS - 1) * kLoads, 0>();
+    else
+      wait_for<0, 0>();
   } else {
     static_assert(DIRECT || NS == 2, "two stages");
     ask(0);
@@ -668,10 +692,10 @@ __global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, DIRECT ? (BP / WP * (BQ /
   uint32_t now = 0;
   if (wq >= extent_q) {  // none of this wavefront's rows exist: it only loads
     for (int s = 0; s < stages; ++s) {
-      wait_for<DIRECT ? (NS - 2) * kLoads : 63, 0>();
+      wait_below(s + 1);
       block_barrier();
       put(now);
-      ask(now);
+      if (exists(s + NS)) ask(now);
       now = now + kStage == NS * kStage ? 0 : now + kStage;
     }
   } else if constexpr (!DIRECT) {  // by registers: more wavefronts a CU instead of fragments ahead of their use
@@ -694,21 +718,23 @@ __global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, DIRECT ? (BP / WP * (BQ /
       products(f0, 0, kAll);
       spread<(LP::kReads * MI + LQ::kReads * NJ), kAll * kMfmas<T>>();
       __builtin_amdgcn_sched_barrier(0);
-      wait_for<(NS - 2) * kLoads, 0>();
+      wait_below(s + 1);
       block_barrier();
       __builtin_amdgcn_sched_barrier(0);
-      constexpr int kSome = kAll >= 2 * kLoads ? kLoads : 0;  // products between the loads
+      constexpr int kSome = LOAD == PIECES && kAll >= 2 * kLoads ? kLoads : 0;  // products between the loads
+      if (exists(s + NS)) {
 #pragma unroll
-      for (int n = 0; n < kLoads; ++n) {
-        if (n < OpP::kLoads)
-          p.ask(lds_at + now, n);
-        else
-          q.ask(lds_at + now + LP::kBytes, n - OpP::kLoads);
-        if (kSome) products(f1, n, n + 1);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int n = 0; n < kLoads; ++n) {
+          if (n < OpP::kLoads)
+            p.ask(lds_at + now, n);
+          else
+            q.ask(lds_at + now + LP::kBytes, n - OpP::kLoads);
+          if (kSome) products(f1, n, n + 1);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        p.on();
+        q.on();
       }
-      p.on();
-      q.on();
       read(next, 0, f0);
       products(f1, kSome, kAll);
       spread<(LP::kReads * MI + LQ::kReads * NJ), (kAll - kSome) * kMfmas<T>>();
@@ -742,11 +768,12 @@ __global__ __launch_bounds__(BP / WP * (BQ / WQ) * 64, DIRECT ? (BP / WP * (BQ /
 // A tile of 32 x 32 for few rows: its four wavefronts share the sum, a quarter of the stages each, from LDS of their own
 // and without a barrier but for the last one, behind which they add up in their order.  More blocks, and a quarter of the
 // way for each: 4096 x 4096 BF16 with one row takes 14.6 us, with tiles of 128 x 32 22.4.
-template <typename T, int MODE, bool DIRECT>
+template <typename T, int MODE, int LOAD>
 __global__ __launch_bounds__(256) void k_slim(ExpertArgs a) {
-  constexpr int B = 32, NW = 4, MI = 2, NJ = 2, NS = DIRECT ? 4 : 2;
-  typedef Operand<T, B, 1, MODE != FORWARD, MODE == FORWARD, DIRECT> OpP;
-  typedef Operand<T, B, 1, false, false, DIRECT> OpQ;
+  constexpr bool DIRECT = LOAD != REGISTERS;
+  constexpr int B = 32, NW = 4, MI = 2, NJ = 2, NS = LOAD == PIECES ? 4 : 2;
+  typedef Operand<T, B, 1, MODE != FORWARD, MODE == FORWARD, LOAD> OpP;
+  typedef Operand<T, B, 1, false, false, LOAD> OpQ;
   typedef typename OpP::Lay LP;
   typedef typename OpQ::Lay LQ;
   constexpr int kLoads = OpP::kLoads + OpQ::kLoads, kStage = LP::kBytes + LQ::kBytes;
@@ -781,9 +808,11 @@ __global__ __launch_bounds__(256) void k_slim(ExpertArgs a) {
     p.put(at + stage);
     q.put(at + stage + LP::kBytes);
   };
+  auto exists = [&](int s) { return LOAD != ELEMENTS || s < to; };
   if constexpr (DIRECT) {
 #pragma unroll
-    for (int s = 0; s < NS; ++s) ask(s * kStage);
+    for (int s = 0; s < NS; ++s)
+      if (exists(from + s)) ask(s * kStage);
   } else {
     ask(0);
     put(0);
@@ -793,7 +822,10 @@ __global__ __launch_bounds__(256) void k_slim(ExpertArgs a) {
   }
   uint32_t now = 0;
   for (int s = from; s < to; ++s) {
-    wait_for<DIRECT ? (NS - 1) * kLoads : 63, 0>();
+    if (exists(s + NS - 1))
+      wait_for<DIRECT ? (NS - 1) * kLoads : 63, 0>();
+    else
+      wait_for<0, 0>();
     uint4v fp[2][MI], fq[2][NJ];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -804,7 +836,7 @@ __global__ __launch_bounds__(256) void k_slim(ExpertArgs a) {
     }
     wait_for<63, 0>();  // they are read: their place is free
     put(now);
-    ask(now);
+    if (exists(s + NS)) ask(now);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -880,7 +912,7 @@ struct Shape {
 };
 
 struct Plan {
-  int tile;
+  int tile, load;
   int32_t bp, bq, tp, tq, rows, units, spread;
   int64_t grid;        // blocks of a worker
   size_t part_bytes;
@@ -920,13 +952,13 @@ bool pays(double other, double own) { return other < 0.85 * own && other < own -
 //
 // In us: a tile's loop takes 0.075 a token, by registers 0.095; blocks beyond one a CU share its rate; the largest of N
 // experts, of all workers, may have 1 + 0.4 log2 N times the average; a second launch costs 4, a share of a tile written and
-// read again 0.024.  Over 1,473 sizes of 1 to 64 experts this takes 3.3% more than the best share, the rule for 16 bits 13%,
-// and up to seven times as long.  In us, not shared and shared: 32,768 tokens of 32 into 256 x 256: 213 and 70; 16,384 of 16
-// into 512 x 512: 226 and 119; 13,462 of 42 experts and 6 workers into 116 x 23, by registers: 176 and 70.
+// read again 0.024, and 0.08 in a row of them.  Over 1,588 sizes of 1 to 64 experts this takes 3% more than the best share,
+// the rule for 16 bits 12%, and up to six times as long.  In us, not shared and shared: 32,768 tokens of 32 into 256 x 256:
+// 213 and 67; 16,384 of 16 into 512 x 512: 226 and 119; 13,462 of 42 experts and 6 workers into 116 x 23: 176 and 70.
 constexpr int64_t kMostShared = 1024;  // tiles' shares: 64 MiB of workspace
 constexpr int64_t kShares[] = {64, 128, 192, 256, 384, 512, 768, 1024, 2048, 4096, 8192};
 
-int64_t share_f32(const Shape& s, int64_t tiles, bool direct, int64_t rows) {
+int64_t share_f32(const Shape& s, int64_t tiles, int load, int64_t rows) {
   const double even = (double)s.W * s.T * tiles / kCUs;  // tokens of a CU
   const int64_t some = s.T < s.E ? s.T : s.E;
   const double times = (1.0 + 0.4 * log2((double)s.W * s.E)) / s.E;
@@ -939,11 +971,17 @@ int64_t share_f32(const Shape& s, int64_t tiles, bool direct, int64_t rows) {
       loop *= ceil_div(s.W * tiles * ceil_div(s.T, share), kCUs);
     else if (s.W * tiles * (shares + some) > kCUs && 1.05 * even > 0.55 * each)
       loop = 1.05 * even + 0.45 * each;
-    return (direct ? 0.075 : 0.095) * loop + (shared ? 4.0 + 0.024 * s.W * (shares + s.E) * tiles : 0.0);
+    return (load == REGISTERS ? 0.095 : 0.075) * loop + (shared ? 4.0 + 0.024 * s.W * (shares + s.E) * tiles + 0.08 * largest / share : 0.0);
   };
   int64_t best = s.T;
-  for (int64_t share : kShares)
+  auto consider = [&](int64_t share) {
     if (share < s.T && s.W * (s.T / share + s.E) * tiles <= kMostShared && time(share) < time(best)) best = share;
+  };
+  for (int64_t share : kShares) consider(share);
+  if (s.E == 1) {  // whole rounds of blocks: 9,210 tokens into 704 x 2453: 350 us, 425
+    for (int64_t blocks = kCUs; blocks <= kMostShared; blocks += kCUs)
+      if (blocks >= 2 * s.W * tiles) consider(ceil_div(ceil_div(s.T, blocks / (s.W * tiles)), 64) * 64);
+  }
   return pays(time(best), time(rows)) ? best : rows;
 }
 
@@ -955,9 +993,14 @@ int64_t share_f32(const Shape& s, int64_t tiles, bool direct, int64_t rows) {
 // by registers, 3,001 of 7 into 515 x 1003: 41 and 24; the rule takes the slower form of 32,768 tokens of 20 into 512 x 512
 // (48 and 60) and of 6 into 1024 x 1024 (115 and 91), where the experts' sizes decide, which the host does not know.  Over
 // 1,473 sizes of 1 to 64 experts, a third of them by registers, BF16 takes 3% more than the best share.
-Plan grad_plan(const Shape& s, bool f32, bool direct) {
+//
+// FP32 that is not read by pieces goes by elements where sides are above 64 and an expert or share has some 96 tokens, else by
+// registers: of narrow sides most loads of elements are of none, and few tokens do not pay for them (elements / registers:
+// 8,192 tokens of 8 into 1023 x 1021: 161 / 190; 14 x 71 into 17 x 2392: 25 / 20; one into 157 x 251: 17.6 / 13.6).
+Plan grad_plan(const Shape& s, bool f32, int load) {
   Plan p = {};
   p.tile = MIDDLE;
+  p.load = load == ELEMENTS && (s.n <= 64 || s.k <= 64) ? REGISTERS : load;
   const int64_t tiles = ceil_div(s.n, 128) * ceil_div(s.k, 128), all = s.W * s.E * tiles;
   int64_t rows = s.T > 0 ? s.T : 1;
   if (all < kSlots && s.T > 0) {
@@ -967,7 +1010,8 @@ Plan grad_plan(const Shape& s, bool f32, bool direct) {
     const double cost = 8.0 + 0.026 * s.W * (double)(s.T / share + s.E) * tiles;
     if (saved > cost) rows = share;
   }
-  if (f32 && s.T > 0) rows = share_f32(s, tiles, direct, rows);
+  if (f32 && s.T > 0) rows = share_f32(s, tiles, p.load, rows);
+  if (p.load == ELEMENTS && (rows < 96 || s.T < 96 * (int64_t)s.E)) p.load = REGISTERS;
   p.rows = (int32_t)rows;
   finish_plan(&p, s, GRAD);
   if (rows < s.T) p.part_bytes = (size_t)(s.W * p.units * tiles) * 128 * 128 * sizeof(float);
@@ -979,18 +1023,19 @@ Plan grad_plan(const Shape& s, bool f32, bool direct) {
 // The estimate is
 //   max(rounds x (4 + stages x alone), most blocks of a CU x stages x together) us,
 // with the times of a stage of a block alone on its CU and of one that shares it, below; a wavefront of a tile of 32 has a
-// quarter of the stages.  Over 2,136 sizes of 1 to 64 experts it takes 1.9% more than the best of the three, the rule of
+// quarter of the stages.  Over 2,404 sizes of 1 to 64 experts it takes 1.4% more than the best of the three, the rule of
 // plan_of 6%, and up to three times as long where results are narrow or few and sums long (32 / 128 x 32 / 128): 22,635
-// rows of 3 experts, 19 x 3000: 65 / 156 / 179; 3,326 rows of one, transposed, 3762 x 80, by registers: 77 / 227 / 326.
+// rows of 3 experts, 19 x 3000: 67 / 156 / 179; by elements, 8,192 of 8, 1023 x 1021: - / 181 / 203.
 struct StageTime {
   int64_t blocks;  // that a CU holds
   double alone, together;
 };
-constexpr StageTime kStageF32[2][3] = {  // [direct][tile]
+constexpr StageTime kStageF32[3][3] = {  // [load][tile]
     {{2, 1.51, 1.10}, {4, 1.32, 0.87}, {2, 2.55, 2.39}},
+    {{2, 0.79, 0.87}, {2, 0.76, 0.56}, {2, 2.25, 1.99}},
     {{1, 0.61, 0.61}, {2, 0.57, 0.54}, {2, 1.56, 1.84}}};
 
-int tile_f32(const Shape& s, int64_t len, int64_t r, bool direct, int tile) {
+int tile_f32(const Shape& s, int64_t len, int64_t r, int load, int tile) {
   const int64_t all = ceil_div(r, kStageBytes / 4);
   const double some = s.E * (1.0 - exp(-(double)s.T / s.E));  // experts with rows, if each row's is any of them
   auto time = [&](int t) {
@@ -998,7 +1043,7 @@ int tile_f32(const Shape& s, int64_t len, int64_t r, bool direct, int tile) {
     const double full = (double)s.T / bq + 0.5 * some;  // last tiles are half empty
     const bool one = s.E == 1 || s.T == 1;
     const double units = one ? ceil_div(s.T, bq) : some > full ? some : full;
-    const StageTime& c = kStageF32[direct][t];
+    const StageTime& c = kStageF32[load][t];
     double sum = 0.0;
     for (double off : {0.9, 1.0, 1.1}) {  // a block more than there are CUs may be one less
       const double blocks = s.W * units * ceil_div(len, bp) * (one ? 1.0 : off);
@@ -1028,15 +1073,16 @@ int tile_f32(const Shape& s, int64_t len, int64_t r, bool direct, int tile) {
 //   128x32 for experts of few rows: 2,048 rows of 64, 1024 x 1024: 63 / 29 / 36 / 31
 //   32     where there are few of those: one row, 4096 x 4096 (32 of 128 x 32): 15 / 22 / 39; 64 rows of 8, 2048 x 2048
 //          (150): 19 / 15 / 25
-Plan plan_of(const Shape& s, int mode, int32_t type, bool direct) {
+Plan plan_of(const Shape& s, int mode, int32_t type, int load) {
   Plan p = {};
+  p.load = load;
   const int64_t experts = s.E > 0 ? s.E : 1, some = s.T < experts ? s.T : experts;
   const int64_t rows = s.T / experts;  // of an expert, on average
   const int64_t len = mode == FORWARD ? s.n : s.k;
-  const bool fits = direct && type != NF_TYPE_F32 && len >= 192;
+  const bool fits = load == PIECES && type != NF_TYPE_F32 && len >= 192;
   if (mode == GRAD) {
     if (!fits || s.n < 192 || s.W * s.E * ceil_div(s.n, 256) * ceil_div(s.k, 256) < kCUs)
-      return grad_plan(s, type == NF_TYPE_F32, direct);
+      return grad_plan(s, type == NF_TYPE_F32, load);
     p.tile = WIDE;
     p.rows = (int32_t)(s.T > 0 ? s.T : 1);
   } else {
@@ -1047,39 +1093,39 @@ Plan plan_of(const Shape& s, int mode, int32_t type, bool direct) {
       p.tile = MIDDLE;
     else
       p.tile = tiles(128, 32) > kCUs * 3 / 8 ? NARROW : SLIM;
-    if (type == NF_TYPE_F32) p.tile = tile_f32(s, len, mode == FORWARD ? s.k : s.n, direct, p.tile);
+    if (type == NF_TYPE_F32) p.tile = tile_f32(s, len, mode == FORWARD ? s.k : s.n, load, p.tile);
   }
   finish_plan(&p, s, mode);
   return p;
 }
 
-template <typename T, int MODE, bool DIRECT>
+template <typename T, int MODE, int LOAD>
 void launch(const Plan& p, const Shape& s, const ExpertArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)p.grid, (unsigned)s.W);
-  if constexpr (DIRECT && sizeof(T) == 2) {
+  if constexpr (LOAD == PIECES && sizeof(T) == 2) {
     if (p.tile == WIDE) {
-      k_expert<T, MODE, 256, 256, 128, 64, 2, true><<<grid, 512, 0, stream>>>(a);
+      k_expert<T, MODE, 256, 256, 128, 64, 2, PIECES><<<grid, 512, 0, stream>>>(a);
       return;
     }
   }
   if constexpr (MODE != GRAD) {
     if (p.tile == SLIM) {
-      k_slim<T, MODE, DIRECT><<<grid, 256, 0, stream>>>(a);
+      k_slim<T, MODE, LOAD><<<grid, 256, 0, stream>>>(a);
       return;
     }
     if (p.tile == NARROW) {
-      k_expert<T, MODE, 128, 32, 32, 32, DIRECT ? 4 : 2, DIRECT><<<grid, 256, 0, stream>>>(a);
+      k_expert<T, MODE, 128, 32, 32, 32, LOAD == PIECES ? 4 : LOAD == ELEMENTS ? 3 : 2, LOAD><<<grid, 256, 0, stream>>>(a);
       return;
     }
   }
-  if constexpr (DIRECT)
-    k_expert<T, MODE, 128, 128, 64, 64, 2, true><<<grid, 256, 0, stream>>>(a);
+  if constexpr (LOAD != REGISTERS)
+    k_expert<T, MODE, 128, 128, 64, 64, 2, LOAD><<<grid, 256, 0, stream>>>(a);
   else
-    k_expert<T, MODE, 128, 128, 64, 32, 2, false><<<grid, 512, 0, stream>>>(a);
+    k_expert<T, MODE, 128, 128, 64, 32, 2, LOAD><<<grid, 512, 0, stream>>>(a);
 }
 
 template <int MODE>
-hipError_t run(const Plan& p, const Shape& s, ExpertArgs a, int32_t type, bool direct, hipStream_t stream) {
+hipError_t run(const Plan& p, const Shape& s, ExpertArgs a, int32_t type, hipStream_t stream) {
   a.tp = p.tp;
   a.tq = p.tq;
   a.rows = p.rows;
@@ -1087,10 +1133,13 @@ hipError_t run(const Plan& p, const Shape& s, ExpertArgs a, int32_t type, bool d
   a.spread = p.spread;
   with_type(type, [&](auto* t) {
     using T = std::remove_pointer_t<decltype(t)>;
-    if (direct)
-      launch<T, MODE, true>(p, s, a, stream);
-    else
-      launch<T, MODE, false>(p, s, a, stream);
+    if (p.load == PIECES) {
+      launch<T, MODE, PIECES>(p, s, a, stream);
+    } else if (p.load == REGISTERS) {
+      launch<T, MODE, REGISTERS>(p, s, a, stream);
+    } else {
+      if constexpr (sizeof(T) == 4) launch<T, MODE, ELEMENTS>(p, s, a, stream);
+    }
     if constexpr (MODE == GRAD) {
       if (p.part_bytes && hipPeekAtLastError() == hipSuccess)
         k_join<<<dim3((unsigned)(p.tp * p.tq * kJoinBlocks), (unsigned)s.E, (unsigned)s.W), kJoinThreads, 0, stream>>>(a);
@@ -1155,7 +1204,13 @@ bool share(const Runs& a, const Runs& b) {
 
 bool whole(const void* p, int64_t ld, int64_t stride, int32_t type) {
   const int64_t bytes = (int64_t)type_bytes(type);
-  return (uintptr_t)p % 16 == 0 && ld % (16 / bytes) == 0 && stride % (16 / bytes) == 0 && ld <= (1 << 20);
+  return (uintptr_t)p % 16 == 0 && ld % (16 / bytes) == 0 && stride % (16 / bytes) == 0;
+}
+
+// How two operands are read: `pieces` says that their lengths and places are whole pieces of 16 bytes.
+int load_of(int32_t type, bool pieces, int64_t p_ld, int64_t q_ld) {
+  if (p_ld > kMaxSide || q_ld > kMaxSide) return REGISTERS;  // offsets of a tile's rows in 32 bits
+  return pieces ? PIECES : type == NF_TYPE_F32 ? ELEMENTS : REGISTERS;
 }
 
 // A launch has under 2^32 threads, and every worker's tiles a number.
@@ -1193,9 +1248,9 @@ nf_status nf_expert_product(const void* x, int32_t type, int64_t x_ld, int64_t x
     return set_error(NF_ERR_ALIGNMENT, "x, w, offsets or y not aligned to its elements");
   const Shape s = {W, E, T, n, k};
   const int64_t piece = 16 / (int64_t)type_bytes(type);
-  const bool direct = whole(x, x_ld, W > 1 ? x_stride : 0, type) && whole(w, w_ld, E > 1 ? w_stride : 0, type) &&
+  const bool pieces = whole(x, x_ld, W > 1 ? x_stride : 0, type) && whole(w, w_ld, E > 1 ? w_stride : 0, type) &&
                       k % piece == 0 && (!transposed || n % piece == 0);
-  const Plan p = plan_of(s, transposed ? BACKWARD : FORWARD, type, direct);
+  const Plan p = plan_of(s, transposed ? BACKWARD : FORWARD, type, load_of(type, pieces, w_ld, x_ld));
   if (too_large(p, W)) return set_error(NF_ERR_UNSUPPORTED, "more tiles than a launch has");
   const Runs to = runs_of(y, W, T, out, y_ld, y_stride, y_type);
   if (share(to, runs_of(x, W, T, in, x_ld, x_stride, type)) || share(to, runs_of(w, E, n, k, w_ld, w_stride, type)))
@@ -1219,7 +1274,7 @@ nf_status nf_expert_product(const void* x, int32_t type, int64_t x_ld, int64_t x
   a.out_ld = y_ld;
   a.out_worker = y_stride;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  return finish(transposed ? run<BACKWARD>(p, s, a, type, direct, st) : run<FORWARD>(p, s, a, type, direct, st));
+  return finish(transposed ? run<BACKWARD>(p, s, a, type, st) : run<FORWARD>(p, s, a, type, st));
 }
 
 size_t nf_expert_grad_workspace_bytes(int32_t W, int64_t T, int32_t E, int64_t n, int64_t k) {
@@ -1227,8 +1282,11 @@ size_t nf_expert_grad_workspace_bytes(int32_t W, int64_t T, int32_t E, int64_t n
   if (check_sizes(W, T, E, n, k) || T == 0 || E == 0 || n == 0 || k == 0) return 0;
   const Shape s = {W, E, T, n, k};
   size_t most = 0;  // of any type and alignment
-  for (const Plan& p : {grad_plan(s, false, true), grad_plan(s, true, true), grad_plan(s, true, false)})
-    most = p.part_bytes > most ? p.part_bytes : most;
+  for (int load : {REGISTERS, ELEMENTS, PIECES})
+    for (bool f32 : {false, true}) {
+      const Plan p = grad_plan(s, f32, load);
+      most = p.part_bytes > most ? p.part_bytes : most;
+    }
   return most;
 }
 
@@ -1243,7 +1301,7 @@ nf_status nf_expert_path(int32_t op, int32_t type, int32_t W, int64_t T, int32_t
   if (const char* why = check_sizes(W, T, E, n, k)) return bad(why);
   if (E == 0 || (op == NF_EXPERT_GRAD ? n == 0 || k == 0 : T == 0 || (op == NF_EXPERT_PRODUCT ? n : k) == 0))
     return set_error(NF_OK, "");
-  const Plan p = plan_of(Shape{W, E, T, n, k}, op, type, whole != 0);
+  const Plan p = plan_of(Shape{W, E, T, n, k}, op, type, load_of(type, whole != 0, 0, 0));
   if (too_large(p, W)) return set_error(NF_ERR_UNSUPPORTED, "more tiles than a launch has");
   info->tile_columns = p.bp;
   info->tile_rows = p.bq;
@@ -1275,9 +1333,9 @@ nf_status nf_expert_grad(const void* dy, int64_t dy_ld, int64_t dy_stride, const
     return set_error(NF_ERR_ALIGNMENT, "dy, x, offsets or grads not aligned to its elements");
   const Shape s = {W, E, T, n, k};
   const int64_t piece = 16 / (int64_t)type_bytes(type);
-  const bool direct = whole(dy, dy_ld, W > 1 ? dy_stride : 0, type) && whole(x, x_ld, W > 1 ? x_stride : 0, type) &&
+  const bool pieces = whole(dy, dy_ld, W > 1 ? dy_stride : 0, type) && whole(x, x_ld, W > 1 ? x_stride : 0, type) &&
                       n % piece == 0 && k % piece == 0;
-  const Plan p = plan_of(s, GRAD, type, direct);
+  const Plan p = plan_of(s, GRAD, type, load_of(type, pieces, x_ld, dy_ld));
   if (too_large(p, W)) return set_error(NF_ERR_UNSUPPORTED, "more tiles than a launch has");
   const size_t need = nf_expert_grad_workspace_bytes(W, T, E, n, k);
   if (ws_bytes < need) return set_error(NF_ERR_WORKSPACE, "workspace smaller than nf_expert_grad_workspace_bytes");
@@ -1306,7 +1364,7 @@ nf_status nf_expert_grad(const void* dy, int64_t dy_ld, int64_t dy_stride, const
   a.out_worker = worker_stride;
   a.out_expert = matrix_stride;
   a.part = static_cast<float*>(ws);
-  return finish(run<GRAD>(p, s, a, type, direct, static_cast<hipStream_t>(stream)));
+  return finish(run<GRAD>(p, s, a, type, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

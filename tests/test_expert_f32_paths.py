@@ -4,6 +4,7 @@ import random
 
 import paper_2606_25759_amd as nf
 from tests import test_gpu_expert_f32 as u
+from tests import test_gpu_expert_far_rows as far
 from tests.test_expert_paths import CODES, whole
 
 GRAD = nf.NF_EXPERT_GRAD
@@ -54,3 +55,10 @@ def test_workspace_holds_every_share():
                     seen += 1
         assert need <= 1024 * 128 * 128 * 4
     assert seen > 500
+
+
+def test_far_rows():
+    """The query does not know of far rows; these sizes take the same tile either way."""
+    tiles = [path(int(back), "f32", 1, T, 1, n, k, (1,))[:2] for T, n, k, back in far.MATRICES]
+    assert tiles == 2 * [(32, 32), (128, 32), (128, 128)]
+    assert path(GRAD, "f32", 1, 500, 1, 70, 96, (1,))[3] > 0 and path(GRAD, "f32", 1, 60, 1, 100, 72, (1,))[3] == 0

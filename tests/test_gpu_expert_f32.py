@@ -1,8 +1,10 @@
 """FP32 products and gradients where they go by rules of their own: results narrow and sums long, tokens shared that 16 bits
 would not share.  test_expert_f32_paths.py holds what the lists here reach."""
 import pytest
+import torch
 
-from tests.test_gpu_expert import check_grad, check_product
+import paper_2606_25759_amd as nf
+from tests.test_gpu_expert import DEV, TYPES, check_grad, check_product, close
 
 pytestmark = pytest.mark.gpu
 
@@ -25,3 +27,34 @@ F32_SHARED = [  # W, E, T, n, k: the first three are shared in FP32 only
 def test_grad_shared_tokens_of_f32(W, E, T, n, k):
     check_grad(W, E, T, n, k, "f32", lead=5, gap=3, seed=T)
     check_grad(W, E, T, n, k, "f32", accumulate=True, seed=T)
+
+
+SHIFTED = [(40, 96, 72), (900, 256, 36), (3000, 520, 264), (3000, 133, 131)]  # T, n, k of two experts
+
+
+def shifted(t, by):
+    """The same values `by` elements behind an aligned address, NaN around them."""
+    flat = torch.full((t.numel() + 8,), float("nan"), dtype=t.dtype, device=DEV)
+    flat[by:by + t.numel()] = t.reshape(-1)
+    return flat[by:by + t.numel()].view(t.shape)
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("by", [(1, 0, 0), (0, 1, 0), (0, 0, 1), (3, 2, 1)])
+@pytest.mark.parametrize("T,n,k", SHIFTED)
+def test_places_aligned_to_their_elements_only(T, n, k, by, kind):
+    g = torch.Generator().manual_seed(T)
+    rand = lambda *s: torch.randn(*s, generator=g).to(TYPES[kind]).to(DEV)  # noqa: E731
+    x, dy, w = shifted(rand(T, k), by[0]), shifted(rand(T, n), by[2]), shifted(rand(2, n, k), by[1])
+    cut = T // 3
+    off = torch.tensor([0, cut, T], dtype=torch.int32, device=DEV)
+    y, dx, rows = (torch.empty(*s, device=DEV) for s in ((T, n), (T, k), (1, 2 * n * k + 1)))
+    nf.nf_expert_product(x, w, off, y)
+    nf.nf_expert_product(dy, w, off, dx, transposed=True)
+    nf.nf_expert_grad(dy, x, off, rows, 1, nf.empty_workspace(nf.nf_expert_grad_workspace_bytes(1, T, 2, n, k)))
+    for e, at in ((0, slice(0, cut)), (1, slice(cut, T))):
+        a, b, m = x[at].double(), dy[at].double(), w[e].double()
+        turned, t = m.t().contiguous(), b.t().contiguous()
+        close(y[at], a @ turned, a.abs() @ turned.abs(), k)
+        close(dx[at], b @ m, b.abs() @ m.abs(), n)
+        close(rows[0, 1 + e * n * k:1 + (e + 1) * n * k].view(n, k), t @ a, t.abs() @ a.abs(), at.stop - at.start)
