@@ -974,15 +974,20 @@ int64_t share_f32(const Shape& s, int64_t tiles, int load, int64_t rows) {
     return (load == REGISTERS ? 0.095 : 0.075) * loop + (shared ? 4.0 + 0.024 * s.W * (shares + s.E) * tiles + 0.08 * largest / share : 0.0);
   };
   int64_t best = s.T;
+  double least = time(best);
   auto consider = [&](int64_t share) {
-    if (share < s.T && s.W * (s.T / share + s.E) * tiles <= kMostShared && time(share) < time(best)) best = share;
+    if (share >= s.T || s.W * (s.T / share + s.E) * tiles > kMostShared) return;
+    const double t = time(share);
+    if (t >= least) return;
+    least = t;
+    best = share;
   };
   for (int64_t share : kShares) consider(share);
   if (s.E == 1) {  // whole rounds of blocks: 9,210 tokens into 704 x 2453: 350 us, 425
     for (int64_t blocks = kCUs; blocks <= kMostShared; blocks += kCUs)
       if (blocks >= 2 * s.W * tiles) consider(ceil_div(ceil_div(s.T, blocks / (s.W * tiles)), 64) * 64);
   }
-  return pays(time(best), time(rows)) ? best : rows;
+  return pays(least, time(rows)) ? best : rows;
 }
 
 // The gradient in tiles of 128, with shared tokens where that saves more than it costs, in us.
@@ -1282,11 +1287,9 @@ size_t nf_expert_grad_workspace_bytes(int32_t W, int64_t T, int32_t E, int64_t n
   if (check_sizes(W, T, E, n, k) || T == 0 || E == 0 || n == 0 || k == 0) return 0;
   const Shape s = {W, E, T, n, k};
   size_t most = 0;  // of any type and alignment
-  for (int load : {REGISTERS, ELEMENTS, PIECES})
-    for (bool f32 : {false, true}) {
-      const Plan p = grad_plan(s, f32, load);
-      most = p.part_bytes > most ? p.part_bytes : most;
-    }
+  // elements have the shares of pieces or of registers
+  for (const Plan& p : {grad_plan(s, false, PIECES), grad_plan(s, true, PIECES), grad_plan(s, true, REGISTERS)})
+    most = p.part_bytes > most ? p.part_bytes : most;
   return most;
 }
 
