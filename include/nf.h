@@ -774,8 +774,9 @@ nf_status nf_orthogonal_update(const void* grad, int32_t grad_type, int64_t grad
  * NF_ERR_INVALID_ARG: W outside [1, 255], T outside [0, 2^24], E outside
  * [0, 4096], n or k outside [0, 2^20], an ld below the columns, a stride too
  * small with W > 1 (w_stride with E > 1), y over x or w.  NF_ERR_UNSUPPORTED:
- * more than 2^22 tiles (of 128 x 128 or 256 x 256, 128 x 32 for experts of
- * few rows and FP32).  T, E or the columns of y = 0 launches nothing.
+ * more than 2^22 tiles (of 32 x 32, 128 x 32, 128 x 128 or 256 x 256, by the
+ * sizes and the type: nf_expert_path).  T, E or the columns of y = 0 launches
+ * nothing.
  */
 nf_status nf_expert_product(const void* x, int32_t type, int64_t x_ld, int64_t x_stride, const void* w, int64_t w_ld,
                             int64_t w_stride, int32_t transposed, const void* offsets, int32_t offsets_bytes,
@@ -787,8 +788,11 @@ nf_status nf_expert_product(const void* x, int32_t type, int64_t x_ld, int64_t x
  *   grads[w*worker_stride + e*matrix_stride + i*k + j] =
  *       sum of dy[w][t][i] x[w][t][j] over the rows t of expert e
  * Experts without a row get zeros.  With accumulate != 0 the sums are added to
- * what the row holds, and experts without a row are left alone.  Sums are FP32 in an order fixed by the sizes, without
- * floating-point atomics: two calls give the same bits.
+ * what the row holds, and experts without a row are left alone.  Sums are FP32,
+ * without floating-point atomics, in an order fixed by the sizes, offsets, type
+ * and the tensors' layout (whether rows can be read 16 bytes at a time, and lie
+ * within 2^20 elements of one another): two calls of one layout give the same
+ * bits, those of another need not.
  * `grads` is expert 0's matrix in worker 0's row (a row's base plus the
  * matrices' offset in it), 4-byte aligned; it shares no element with dy or x,
  * which is checked as there.

@@ -917,8 +917,11 @@ def _parts(src, dst, name):
 
 class NormPlan:
     """The tensors of nf_grad_norm and nf_grad_clip and their device table, for
-    as long as they stay where they are; keeps them alive.  Made by
-    norm_plan.  May be dropped while calls on torch's streams are under way; a
+    as long as they stay where they are; keeps them alive.  The table holds
+    addresses: tensors that are allocated anew each step, as gradients are
+    after zero_grad(set_to_none=True), torch's default, are others than the
+    plan's, whose old ones a call would read and write without an error.  Made
+    by norm_plan.  May be dropped while calls on torch's streams are under way; a
     graph that holds such a call, or a call on a raw handle of a stream that is
     not torch's current or default one, has to end before the plan does."""
 
@@ -954,7 +957,9 @@ def norm_plan(src, dst=None, groups=None, n_groups=None, stream=None):
     dst: where the scaled ones go, tensors of the same shapes (src itself for in
     place), or None for norms only.  n_groups: how many groups there are, if
     not those that occur.  Tensors may be of any type and strides that do not
-    overlap.  Synchronises the stream: made once, not in the step loop."""
+    overlap.  Synchronises the stream and takes some 3 us a tensor (2,576: 7 ms,
+    where a call takes 0.3): made once, not in the step loop, for gradients that
+    keep their places (zero_grad(set_to_none=False), or views of the rows)."""
     src = list(src)
     dst = list(dst) if dst is not None else [None] * len(src)
     groups = [0] * len(src) if groups is None else [int(g) for g in groups]

@@ -16,8 +16,8 @@
 // 5.95 TB/s.  The two passes of a clipping read what they scale twice; the
 // second goes through each block's pieces from the last one back, since what
 // was read last may still be in the card's cache: 1.3G BF16 into FP32 in
-// 1,990 us (10.5 GB moved, 5.3 TB/s), 25.6M FP32 in 50.  A dozen small
-// tensors are one block and one launch: 3 us, 5.4 with the call.  Blocks of
+// 2,000 us (10.5 GB moved, 5.3 TB/s), 25.6M FP32 in 52.  A dozen small
+// tensors are one block and one launch: 3 us, 5.3 with the call.  Blocks of
 // 1,024 threads, as many as the card holds at once.
 #include <limits.h>
 #include <math.h>
@@ -34,7 +34,7 @@ namespace {
 
 constexpr int kNormThreads = 1024;
 constexpr int kNormWaves = kNormThreads / 64;
-constexpr int kWavesAtOnce = 8;            // a SIMD: two blocks a CU (25.6M FP32 clipped: 50 us, 57 with one)
+constexpr int kWavesAtOnce = 8;            // a SIMD: two blocks a CU (25.6M FP32 clipped: 12% less than with one)
 constexpr int64_t kMostBlocks = 512;       // what the card holds at once
 constexpr int64_t kLeastPiece = 1024, kMostPiece = 32768;  // elements
 constexpr int64_t kPieceCost = 1024;       // of a piece besides its elements, in elements
@@ -115,7 +115,7 @@ __device__ __forceinline__ double squares(const Piece& p) {
 }
 
 // SIZE bytes at any element's address that are not read again here: they need not displace what is (102 MB of FP32
-// clipped: 57 us, 61 with ordinary stores and eight loads under way where this has four).
+// clipped: 7% less than with ordinary stores and eight loads under way where this has four).
 template <int SIZE>
 __device__ __forceinline__ void store_past(void* to, const void* from) {
   typedef uint32_t word __attribute__((aligned(2)));
