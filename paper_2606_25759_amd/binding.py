@@ -947,7 +947,10 @@ class NormPlan:
                 stream = (torch.cuda.current_stream() if handle == _stream(None) else
                           torch.cuda.default_stream() if handle == 0 else None)
             if stream is not None:
-                self.table.record_stream(stream)
+                try:
+                    self.table.record_stream(stream)
+                except TypeError:  # a stream of somebody else's, that has a handle and no more: as a raw one
+                    return handle
                 self.noted.add(handle)
         return handle
 

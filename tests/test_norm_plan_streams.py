@@ -127,3 +127,13 @@ def test_nothing_is_noted_in_a_capture(card, which):
     card.capturing = False
     calls(plan, card, None)[which]()
     assert ("keep", SIDE) in card.log
+
+
+def test_another_librarys_stream(card):
+    """An object that has a handle and is not torch's: taken as the handle."""
+    plan = nf.norm_plan([], n_groups=1)
+    plan.table.record_stream = lambda stream: (_ for _ in ()).throw(TypeError("not a stream"))
+    del card.log[:]
+    for call in calls(plan, card, types.SimpleNamespace(cuda_stream=SIDE)):
+        call()
+    assert [e[1] for e in card.log] == [SIDE] * 3
